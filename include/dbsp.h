@@ -227,6 +227,75 @@ int sparse_attn_fwd_static(const dbsp_plan* plan, const void* q, const void* k, 
                            void* stream);
 
 /*
+ * A key/value cache: the keys and values that a program keeps between its attention calls, where it generates piece by piece
+ * (token by token, frame by frame) instead of in one pass under a block mask.  Three parts, all in the caller's memory:
+ *   - a prefix that all sequences of the batch share (the prompt, conditioning frames), read only;
+ *   - each sequence's own keys: of the `capacity` slots of sequence b the first lens[b] are used;
+ *   - optional, beside the own keys: `weights`, the attention that each key has drawn, and `positions`.
+ * G query heads share a KV head: query head h reads KV head h / G, G = H / Hk.
+ * The struct is read during the calls only and holds no state; calls that use the same cache must not overlap on the device where
+ * one of them writes what another uses (its lens, weights, positions or evicted rows).
+ */
+enum { DBSP_BF16 = 0, DBSP_FP16 = 1 };
+typedef struct dbsp_cache {
+  int32_t dtype;              /* DBSP_BF16 or DBSP_FP16: of K, V, Q and O alike */
+  int32_t B, Hk, d;           /* sequences, KV heads, head dim (64 or 128) */
+  int32_t n_prefix, capacity; /* tokens of the prefix, slots of a sequence; either may be 0 */
+  const void *prefix_k, *prefix_v; /* device, [Hk, n_prefix, d]; not looked at if n_prefix == 0 */
+  void *k, *v;                /* device, [B, Hk, capacity, d]; not looked at if capacity == 0 */
+  /* strides in elements, of the head (and before it the batch) and the token dimension; d has stride 1.  Multiples of 8, at least
+   * 0, a token's at most 2^24; the pointers are 16-byte aligned.  Eviction writes k and v: no two of their elements may share a place */
+  int64_t prefix_k_stride[2], prefix_v_stride[2], k_stride[3], v_stride[3];
+  int32_t* lens;              /* device, int32 [B]: used slots; taken as 0 below 0 and as capacity above it.  NULL only if capacity == 0 */
+  float* weights;             /* device, f32 [B, Hk, capacity] contiguous; NULL where no call uses them */
+  int32_t* positions;         /* device, int32 [B, Hk, capacity] contiguous: a key's place in its sequence; only eviction uses it, or NULL */
+} dbsp_cache;
+
+/*
+ * dbsp_cache_attn_fwd -- attention of each sequence's Nq newest tokens over the shared prefix and its own keys:
+ *   s = softmax_scale q.k,  LSE = ln(sum exp(s)),  O = sum exp(s - LSE) v,
+ * the sums over all of the prefix and over the own keys that the query sees: slots j < lens[b], and with `causal` for query t
+ * only j <= lens[b] - q_lens[b] + t (the new tokens' keys are the last used slots, written before the call).
+ * The prefix's keys are read once for the whole batch where a sequence's queries alone would not fill a tile.
+ *
+ * q:   device, [B, H, Nq, d] with strides in elements (batch, head, token; multiples of 8, d has stride 1), 16-byte aligned.
+ * o:   device, as q, written; its own strides, no two elements in one place.
+ * lse: device, f32 [B, H, Nq] contiguous, written; may be NULL.
+ * q_lens: device, int32 [B]: new tokens of each sequence, taken as 0 below 0 and as Nq above it; NULL: Nq each.  Rows t >= q_lens[b]
+ *      of o and lse are left as they were, whatever q holds there.
+ * A query without a key gets O = 0, LSE = -inf.  K and V must be finite in every used slot and in the prefix (a key that a query
+ * does not see has probability zero, which an infinite value does not survive); slots from lens[b] on are never read.
+ * softmax_scale <= 0 selects 1 / sqrt(d).  f32 accumulation; results do not depend on anything but the arguments.
+ * decay: below 0 leaves the cache's weights alone; else, for every own key in use,
+ *      weights[b, hk, j] = decay * weights[b, hk, j] + sum over the heads h of hk and t < q_lens[b] of exp(s - LSE)
+ *      (0: what was there is not read; 1: the sum over all calls), in f32; weights from lens[b] on are left as they were.
+ * workspace: device, 256-byte aligned, of at least the size that dbsp_cache_attn_workspace gives for the same cache, H, Nq and
+ *      whether decay >= 0; written by the call, holds nothing between calls.  Calls under way at the same time need one each.
+ * stream: a hipStream_t (NULL = default stream).  The call only enqueues kernels, under capture too; lens and q_lens are read on
+ * the device, so that a graph's replays follow what they hold then.
+ * Errors: DBSP_EINVAL, DBSP_ESHAPE (H is no multiple of Hk, sizes too large), DBSP_EHIP.
+ */
+int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token, void* o,
+                        int64_t o_batch, int64_t o_head, int64_t o_token, float* lse, const int32_t* q_lens, int32_t H, int32_t Nq,
+                        int32_t causal, float softmax_scale, float decay, void* workspace, int64_t workspace_bytes, void* stream);
+int dbsp_cache_attn_workspace(const dbsp_cache* cache, int32_t H, int32_t Nq, int32_t with_weights, int64_t* bytes);
+
+/*
+ * dbsp_cache_evict -- cuts every sequence with more than `budget` used slots back to `budget`, each KV head by itself: the keys
+ * of the largest weights stay (a NaN counts as -inf; of equal weights the lowest slots).  Above all weights rank the keys with
+ * positions < sinks, and those with positions >= keep_from[b] (device, int32 [B]; NULL: none).
+ * A kept key in a slot >= budget moves into a slot < budget that an evicted one leaves, both in ascending order, with its row of
+ * K and V, its weight and its position; all other slots below the budget stay as they are, so slots do not keep the order of their
+ * positions.  The weights of the slots from budget to lens[b] are set to 0 (what is appended there starts from nothing),
+ * their K, V and positions are left as they were.  lens[b] becomes min(lens[b], budget); other sequences are left alone.
+ * Needs the cache's weights and positions, budget >= 1, sinks >= 0.  workspace and stream as for dbsp_cache_attn_fwd.
+ * Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large), DBSP_EHIP.
+ */
+int dbsp_cache_evict(const dbsp_cache* cache, int32_t budget, int32_t sinks, const int32_t* keep_from, void* workspace,
+                     int64_t workspace_bytes, void* stream);
+int dbsp_cache_evict_workspace(const dbsp_cache* cache, int32_t budget, int64_t* bytes);
+
+/*
  * imbalance_ratio -- Eq. 1 on a host matrix work[periods][partitions] (row-major, int64, >= 0):
  * rho = sum_i max_g work[i][g] / (sum_{i,g} work[i][g] / partitions), in double.  Zero total
  * work gives 1.0.  Errors: DBSP_EINVAL (null pointer, non-positive size, negative entry).

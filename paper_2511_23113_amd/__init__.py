@@ -11,11 +11,14 @@ from .binding import (  # noqa: F401
     DBSP_ESHAPE,
     DBSP_OK,
     DbspError,
+    KVCache,
     MODE_BALANCED,
     MODE_NAIVE,
     MODE_REWARD,
     MODE_ROUNDS,
     Plan,
+    cache_attn_fwd,
+    cache_evict,
     fit_cost_model,
     imbalance_ratio,
     load_library,

@@ -27,6 +27,7 @@ EXPORTS = (
     "plan_sparse_attn", "plan_sparse_attn_reuse", "sparse_attn_fwd", "sparse_attn_fwd_static", "imbalance_ratio", "dbsp_plan_get", "dbsp_plan_stats",
     "dbsp_plan_busy", "dbsp_plan_tail_takes", "dbsp_plan_pair_rows", "dbsp_plan_calibrate", "dbsp_plan_destroy", "dbsp_plan_release", "dbsp_last_error",
     "dbsp_partition_heads", "dbsp_partition_blocks", "dbsp_ring_work", "dbsp_fit_cost_model", "dbsp_mfma_probe", "dbsp_plan_run_order",
+    "dbsp_cache_attn_fwd", "dbsp_cache_attn_workspace", "dbsp_cache_evict", "dbsp_cache_evict_workspace",
 )
 
 
@@ -41,6 +42,14 @@ class PlanOpts(C.Structure):
                 ("item_overhead", C.c_int32), ("flags", C.c_int32), ("locality_groups", C.c_int32),
                 ("partition_cost", C.c_void_p), ("max_batch", C.c_int32), ("dynamic_tail", C.c_int32), ("reward", C.c_double),
                 ("head_dim", C.c_int32)]
+
+
+class CacheDesc(C.Structure):
+    """dbsp_cache of dbsp.h."""
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("Hk", C.c_int32), ("d", C.c_int32), ("n_prefix", C.c_int32), ("capacity", C.c_int32),
+                ("prefix_k", C.c_void_p), ("prefix_v", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("prefix_k_stride", C.c_int64 * 2), ("prefix_v_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("lens", C.c_void_p), ("weights", C.c_void_p), ("positions", C.c_void_p)]
 
 
 _lib = None
@@ -94,6 +103,15 @@ def load_library(path: str | None = None):
     lib.dbsp_plan_pair_rows.restype = C.c_int
     lib.dbsp_plan_run_order.argtypes = [vp, vp, vp, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
     lib.dbsp_plan_run_order.restype = C.c_int
+    cache, f32 = C.POINTER(CacheDesc), C.c_float
+    lib.dbsp_cache_attn_fwd.argtypes = [cache, vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, i32, i32, i32, f32, f32, vp, i64, vp]
+    lib.dbsp_cache_attn_fwd.restype = C.c_int
+    lib.dbsp_cache_attn_workspace.argtypes = [cache, i32, i32, i32, i64p]
+    lib.dbsp_cache_attn_workspace.restype = C.c_int
+    lib.dbsp_cache_evict.argtypes = [cache, i32, i32, vp, vp, i64, vp]
+    lib.dbsp_cache_evict.restype = C.c_int
+    lib.dbsp_cache_evict_workspace.argtypes = [cache, i32, i64p]
+    lib.dbsp_cache_evict_workspace.restype = C.c_int
     lib.dbsp_plan_destroy.argtypes = [vp]
     lib.dbsp_plan_destroy.restype = None
     lib.dbsp_plan_release.argtypes = [vp]
@@ -304,6 +322,154 @@ def sparse_attn_fwd(plan: Plan, q, k, v, o=None, lse=None, softmax_scale: float 
     if rc:
         _check(rc)
     return o, lse
+
+
+def _torch_module():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+class KVCache:
+    """A key/value cache of the caller's tensors (see dbsp.h: dbsp_cache), for cache_attn_fwd and cache_evict.
+
+    k, v: [B, Hk, capacity, d], bf16 or fp16 on one GPU, d in (64, 128) dense, other strides multiples of 8 elements; the first
+    lens[b] (int32 [B] there) slots of sequence b are used.  prefix_k, prefix_v: [Hk, P, d], shared by all sequences.  Either
+    pair may be missing.  weights: f32 [B, Hk, capacity], positions: int32 [B, Hk, capacity], both contiguous.  The object keeps the
+    tensors, which the caller goes on writing; it copies nothing."""
+
+    def __init__(self, k=None, v=None, lens=None, prefix_k=None, prefix_v=None, weights=None, positions=None):
+        torch = _torch_module()
+        some = k if k is not None else prefix_k
+        if some is None or (k is None) != (v is None) or (prefix_k is None) != (prefix_v is None) or (k is None) != (lens is None):
+            raise ValueError("a cache has k, v and lens, or prefix_k and prefix_v, or all of them")
+        if some.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("keys and values are bf16 or fp16")
+        self.dtype, self.device, d = some.dtype, some.device, some.shape[-1]
+        desc = CacheDesc(dtype=0 if some.dtype == torch.bfloat16 else 1, d=d)
+        for name, x, dims in (("k", k, 4), ("v", v, 4), ("prefix_k", prefix_k, 3), ("prefix_v", prefix_v, 3)):
+            if x is None:
+                continue
+            if x.dim() != dims or x.dtype != self.dtype or not x.is_cuda or x.device != self.device or x.shape[-1] != d or x.stride(-1) != 1:
+                raise ValueError(f"{name} must be a {dims}-d tensor of the cache's type and head dim on its GPU, with a dense last dimension")
+            setattr(desc, name, x.data_ptr())
+            stride = getattr(desc, name + "_stride")
+            for i in range(dims - 1):
+                stride[i] = x.stride(i) if x.shape[i] > 1 else 0
+        if k is not None:
+            if k.shape != v.shape:
+                raise ValueError("k and v differ in shape")
+            desc.B, desc.Hk, desc.capacity = k.shape[:3]
+        if prefix_k is not None:
+            if prefix_k.shape != prefix_v.shape or (k is not None and prefix_k.shape[0] != k.shape[1]):
+                raise ValueError("prefix_k and prefix_v differ in shape, or from k in their heads")
+            desc.Hk, desc.n_prefix = prefix_k.shape[:2]
+        for name, x, dtype, shape in (("lens", lens, torch.int32, k.shape[:1] if k is not None else None),
+                                      ("weights", weights, torch.float32, k.shape[:3] if k is not None else None),
+                                      ("positions", positions, torch.int32, k.shape[:3] if k is not None else None)):
+            if x is None:
+                continue
+            if shape is None or x.dtype != dtype or x.device != self.device or x.shape != shape or not x.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dtype} tensor of {'[B]' if name == 'lens' else '[B, Hk, capacity]'} on the cache's GPU")
+            setattr(desc, name, x.data_ptr())
+        self.k, self.v, self.lens, self.prefix_k, self.prefix_v, self.weights, self.positions = k, v, lens, prefix_k, prefix_v, weights, positions
+        self.B, self.Hk, self.d, self.capacity, self.n_prefix = desc.B, desc.Hk, d, desc.capacity, desc.n_prefix
+        self._desc, self._bytes = desc, {}
+
+    def _need(self, key, ask) -> int:
+        """Workspace bytes of a call, by its sizes."""
+        n = self._bytes.get(key)
+        if n is None:
+            out = C.c_int64()
+            _check(ask(C.byref(out)))
+            n = self._bytes[key] = out.value
+        return n
+
+    def _on(self, stream):
+        """The raw stream, and whether tensors made on torch's current one are used on another."""
+        torch = _torch
+        if self.device.index != torch.cuda.current_device():
+            raise ValueError("the cache lives on another device than the current one")
+        now = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if stream is None:
+            return now, False
+        raw = stream if isinstance(stream, int) else stream.cuda_stream
+        return raw, raw != now
+
+    def _workspace(self, workspace, need, raw, elsewhere):
+        torch = _torch
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            if elsewhere:
+                workspace.record_stream(torch.cuda.ExternalStream(raw, device=self.device))
+        elif workspace.dtype != torch.uint8 or workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError("the workspace must be a contiguous uint8 tensor on the cache's GPU")
+        return workspace
+
+
+def cache_attn_fwd(cache: KVCache, q, q_lens=None, causal: bool = True, decay=None, o=None, lse=None, softmax_scale: float = 0.0,
+                   stream=None, want_lse: bool = True, workspace=None):
+    """Attention of each sequence's newest tokens, q [B, H, Nq, d], over the cache's shared prefix and its own keys (see dbsp.h:
+    dbsp_cache_attn_fwd; the new tokens' keys are written before).  q_lens: int32 [B] on the GPU, if not all Nq tokens are there;
+    the others' rows of o and lse are left as they were, so pass o and lse then.  decay: None, or the factor of what the cache's
+    weights hold, to which this call's attention is added.  Enqueues on `stream` (default: torch's current stream) and
+    returns (o, lse)."""
+    torch = _torch
+    if q.dim() != 4 or q.dtype != cache.dtype or q.device != cache.device or q.shape[-1] != cache.d or q.stride(-1) != 1:
+        raise ValueError("q must be [B, H, Nq, d] of the cache's type and head dim on its GPU, with a dense last dimension")
+    B, H, Nq, _ = q.shape
+    desc = cache._desc
+    if cache.k is None:
+        desc = CacheDesc.from_buffer_copy(desc)      # a prefix alone serves any number of sequences
+        desc.B = B
+    elif B != cache.B:
+        raise ValueError("q and the cache differ in the number of sequences")
+    raw, elsewhere = cache._on(stream)
+    if o is None:
+        o = torch.empty((B, H, Nq, cache.d), dtype=q.dtype, device=q.device)
+    elif o.shape != q.shape or o.dtype != q.dtype or o.device != q.device or o.stride(-1) != 1:
+        raise ValueError("o must be as q")
+    if lse is None:
+        if want_lse:
+            lse = torch.empty((B, H, Nq), dtype=torch.float32, device=q.device)
+    elif lse.shape != (B, H, Nq) or lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous f32 tensor of [B, H, Nq] on q's GPU")
+    if q_lens is not None and (q_lens.shape != (B,) or q_lens.dtype != torch.int32 or q_lens.device != q.device or not q_lens.is_contiguous()):
+        raise ValueError("q_lens must be a contiguous int32 tensor of [B] on q's GPU")
+    if decay is None:
+        decay = -1.0
+    elif not decay >= 0:
+        raise ValueError("decay must not be negative")
+    elif cache.weights is None:
+        raise ValueError("the cache has no weights")
+    lib, at = load_library(), C.byref(desc)
+    workspace = cache._workspace(workspace, cache._need((B, H, Nq, decay >= 0), lambda n: lib.dbsp_cache_attn_workspace(at, H, Nq, decay >= 0, n)), raw, elsewhere)
+    q_s, o_s = q.stride(), o.stride()
+    rc = lib.dbsp_cache_attn_fwd(at, q.data_ptr(), q_s[0], q_s[1], q_s[2], o.data_ptr(), o_s[0], o_s[1], o_s[2], None if lse is None else lse.data_ptr(),
+                                 None if q_lens is None else q_lens.data_ptr(), H, Nq, causal, softmax_scale, decay, workspace.data_ptr(),
+                                 workspace.numel(), raw)
+    if rc:
+        _check(rc)
+    return o, lse
+
+
+def cache_evict(cache: KVCache, budget: int, sinks: int = 0, keep_from=None, stream=None, workspace=None) -> None:
+    """Cuts the sequences with more than `budget` used slots back to the `budget` keys of the largest weights, in place, each KV
+    head by itself (see dbsp.h: dbsp_cache_evict).  Keys at positions below `sinks`, and from keep_from[b] on (int32 [B] on the
+    GPU), rank above all others.  Updates k, v, weights, positions and lens; enqueues on `stream`."""
+    torch = _torch
+    raw, elsewhere = cache._on(stream)
+    if keep_from is not None and (keep_from.shape != (cache.B,) or keep_from.dtype != torch.int32 or keep_from.device != cache.device or not keep_from.is_contiguous()):
+        raise ValueError("keep_from must be a contiguous int32 tensor of [B] on the cache's GPU")
+    if cache.k is None:
+        raise ValueError("the cache has no keys of its own")
+    lib, at = load_library(), C.byref(cache._desc)
+    workspace = cache._workspace(workspace, cache._need(budget, lambda n: lib.dbsp_cache_evict_workspace(at, budget, n)), raw, elsewhere)
+    rc = lib.dbsp_cache_evict(at, budget, sinks, None if keep_from is None else keep_from.data_ptr(), workspace.data_ptr(), workspace.numel(), raw)
+    if rc:
+        _check(rc)
 
 
 def imbalance_ratio(work) -> float:

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libdbsp.so")
 
-SOURCES = ["planner.cpp", "dual_balance.cpp", "cost_model.cpp", "api.hip", "attn_fwd.hip", "mfma_probe.hip"]
+SOURCES = ["planner.cpp", "dual_balance.cpp", "cost_model.cpp", "api.hip", "attn_fwd.hip", "mfma_probe.hip",
+           "cache_api.hip", "cache_attn.hip", "cache_evict.hip"]
 
 # Per-file extra flags.  The attention kernels never rely on NaN propagation; without NaN
 # handling the max chains of the softmax compile to v_max3_f32.  (Host-side argument checks in
@@ -22,7 +23,8 @@ SOURCES = ["planner.cpp", "dual_balance.cpp", "cost_model.cpp", "api.hip", "attn
 # The host planners' loops are fast or slow by where they begin: functions begin at multiples of 64 bytes, so that a change
 # elsewhere does not move them (partition of 26 heads, 78 x 78 blocks: 29.4 us, 30.8 with all code 32 bytes on).
 HOST_LAYOUT = ["-falign-functions=64"]
-EXTRA_FLAGS = {"planner.cpp": HOST_LAYOUT, "dual_balance.cpp": HOST_LAYOUT, "attn_fwd.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-sched-strategy=iterative-ilp", "-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA_FLAGS = {"planner.cpp": HOST_LAYOUT, "dual_balance.cpp": HOST_LAYOUT, "attn_fwd.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-sched-strategy=iterative-ilp", "-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "cache_attn.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 # Packed-FP32 VALU ops are switched off for all device code (-packed-fp32-ops removes the feature).
 HIP_FLAGS = [

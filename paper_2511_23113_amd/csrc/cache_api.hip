@@ -1,0 +1,219 @@
+// C ABI of the key/value cache's operators: argument checks, workspaces, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <string>
+
+#include "cache_params.hpp"
+#include "dbsp.h"
+#include "plan.hpp"
+
+namespace {
+
+int fail(const char* who, int code, const char* what) { return dbsp_set_error(code, std::string(who) + ": " + what); }
+
+int done(const char* who, hipError_t e) {
+  if (e == hipSuccess) return DBSP_OK;
+  (void)hipGetLastError();
+  return dbsp_set_error(DBSP_EHIP, std::string(who) + ": " + hipGetErrorString(e));
+}
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// Strides (the token's last) are ones that the kernels can go by.
+bool strides_ok(const int64_t* s, int n) {
+  for (int i = 0; i < n; ++i)
+    if (s[i] < 0 || s[i] % 8 != 0 || s[i] > (int64_t)1 << 40) return false;
+  return s[n - 1] <= (int64_t)1 << 24;
+}
+
+// No two elements of a tensor with these sizes and strides (its last dimension dense, d long) share a place: in the order of their
+// strides each dimension steps over all that the ones before it reach.
+bool distinct(const int64_t* size, const int64_t* stride, int64_t d) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+  __int128 reach = d;
+  for (int i : order) {
+    if (size[i] <= 1) continue;
+    if (stride[i] < reach) return false;
+    reach += (__int128)stride[i] * (size[i] - 1);
+  }
+  return true;
+}
+
+constexpr int64_t kMost = INT_MAX / 2;
+
+int check_cache(const char* who, const dbsp_cache* c) {
+  if (!c) return fail(who, DBSP_EINVAL, "null cache");
+  if (c->dtype != DBSP_BF16 && c->dtype != DBSP_FP16) return fail(who, DBSP_EINVAL, "dtype must be DBSP_BF16 or DBSP_FP16");
+  if (c->d != 64 && c->d != 128) return fail(who, DBSP_EINVAL, "head dim must be 64 or 128");
+  if (c->B <= 0 || c->Hk <= 0) return fail(who, DBSP_EINVAL, "B and Hk must be positive");
+  if (c->n_prefix < 0 || c->capacity < 0) return fail(who, DBSP_EINVAL, "n_prefix and capacity must not be negative");
+  if (c->n_prefix > kMost || c->capacity > 65535 * 128 || (int64_t)c->B * c->Hk > kMost) return fail(who, DBSP_ESHAPE, "the cache is too large");
+  if (c->n_prefix > 0) {
+    if (!c->prefix_k || !c->prefix_v) return fail(who, DBSP_EINVAL, "null pointer (prefix)");
+    if (!strides_ok(c->prefix_k_stride, 2) || !strides_ok(c->prefix_v_stride, 2) || !aligned(c->prefix_k, 16) || !aligned(c->prefix_v, 16))
+      return fail(who, DBSP_EINVAL, "the prefix must be 16-byte aligned, its strides multiples of 8 and a token's at most 2^24");
+  }
+  if (c->capacity > 0) {
+    if (!c->k || !c->v || !c->lens) return fail(who, DBSP_EINVAL, "null pointer (k, v or lens)");
+    if (!strides_ok(c->k_stride, 3) || !strides_ok(c->v_stride, 3) || !aligned(c->k, 16) || !aligned(c->v, 16))
+      return fail(who, DBSP_EINVAL, "k and v must be 16-byte aligned, their strides multiples of 8 and a token's at most 2^24");
+    if (!aligned(c->lens, 4) || !aligned(c->weights, 4) || !aligned(c->positions, 4))
+      return fail(who, DBSP_EINVAL, "lens, weights and positions must be 4-byte aligned");
+  }
+  return DBSP_OK;
+}
+
+struct Cut {             // how an attention call is laid out
+  dbsp_cache_attn_params p;
+  int64_t grid, row_lse_at, part_o_at, part_lse_at, bytes;
+};
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool with_weights, Cut& cut) {
+  const int rc = check_cache(who, c);
+  if (rc != DBSP_OK) return rc;
+  if (H <= 0 || Nq <= 0) return fail(who, DBSP_EINVAL, "H and Nq must be positive");
+  if (H % c->Hk != 0) return fail(who, DBSP_ESHAPE, "H must be a multiple of the cache's KV heads");
+  if (with_weights && c->capacity > 0 && !c->weights) return fail(who, DBSP_EINVAL, "the cache has no weights");
+  dbsp_cache_attn_params& p = cut.p;
+  p = {};
+  p.B = c->B; p.H = H; p.Hk = c->Hk; p.G = H / c->Hk; p.Nq = Nq; p.P = c->n_prefix; p.cap = c->capacity;
+  const int64_t rows = (int64_t)Nq * p.G, all_rows = rows * p.B, q_rows = (int64_t)p.B * Nq * H;
+  if (rows > kMost || all_rows > kMost || q_rows / 8 > kMost) return fail(who, DBSP_ESHAPE, "too many queries");
+  p.pre_tiles = (p.P + kCacheKeys - 1) / kCacheKeys;
+  p.pooled = p.P > 0 && p.B > 1 && rows < kCacheRows;
+  p.pre_row_tiles = p.pooled ? (int32_t)((all_rows + kCacheRows - 1) / kCacheRows) : 0;
+  p.own_row_tiles = (int32_t)((rows + kCacheRows - 1) / kCacheRows);
+  p.own_rows = (int32_t)std::min<int64_t>(rows, kCacheRows);
+  const int64_t unit = (int64_t)p.Hk * p.own_row_tiles, pre_unit = (int64_t)p.Hk * p.pre_row_tiles, row_tiles = unit * p.B;
+  const int64_t most_tiles = (p.pooled ? 0 : p.pre_tiles) + (p.cap + kCacheKeys - 1) / kCacheKeys;
+  p.split = p.pooled || (row_tiles < kCacheTarget && most_tiles > 1);
+  // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kCacheTarget of them
+  const int64_t pre_items = std::min(pre_unit * p.pre_tiles, kCacheTarget + pre_unit);
+  const int64_t own_items = p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), kCacheTarget + row_tiles) : row_tiles;
+  cut.grid = round_up(p.split ? std::min(pre_items + own_items, kCacheTarget + pre_unit + row_tiles) : row_tiles, 8);
+  if (cut.grid > kMost || pre_items > kMost / kCacheRows) return fail(who, DBSP_ESHAPE, "too many queries");
+  p.max_pre_items = p.pooled ? (int32_t)pre_items : 0;
+  cut.row_lse_at = round_up((2 + 2 * (int64_t)p.B) * 4, 256);
+  cut.part_o_at = cut.row_lse_at + (with_weights ? round_up(q_rows * 4, 256) : 0);
+  const int64_t part_rows = p.split ? p.max_pre_items * (int64_t)kCacheRows + own_items * p.own_rows : 0;
+  cut.part_lse_at = cut.part_o_at + part_rows * c->d * 4;
+  cut.bytes = round_up(cut.part_lse_at + part_rows * 4, 256);
+  return DBSP_OK;
+}
+
+int evict_bytes(const char* who, const dbsp_cache* c, int32_t budget, int64_t& moves, int64_t& bytes) {
+  const int rc = check_cache(who, c);
+  if (rc != DBSP_OK) return rc;
+  if (budget < 1) return fail(who, DBSP_EINVAL, "budget must be positive");
+  moves = std::min<int64_t>(budget, std::max(0, c->capacity - budget));
+  const int64_t pairs = (int64_t)c->B * c->Hk;
+  bytes = round_up(pairs * 4, 256) + 2 * round_up(pairs * moves * 4, 256);
+  return DBSP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dbsp_cache_attn_workspace(const dbsp_cache* cache, int32_t H, int32_t Nq, int32_t with_weights, int64_t* bytes) {
+  const char* who = "dbsp_cache_attn_workspace";
+  if (!bytes) return fail(who, DBSP_EINVAL, "null pointer");
+  Cut cut;
+  const int rc = lay_out(who, cache, H, Nq, with_weights != 0, cut);
+  *bytes = rc == DBSP_OK ? cut.bytes : 0;
+  return rc;
+}
+
+int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token, void* o,
+                        int64_t o_batch, int64_t o_head, int64_t o_token, float* lse, const int32_t* q_lens, int32_t H, int32_t Nq,
+                        int32_t causal, float softmax_scale, float decay, void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* who = "dbsp_cache_attn_fwd";
+  if (!(decay == decay) || decay > 3.0e38f) return fail(who, DBSP_EINVAL, "decay must be finite");
+  if (!(softmax_scale == softmax_scale) || softmax_scale > 1e30f) return fail(who, DBSP_EINVAL, "softmax_scale must be finite");
+  const bool with_weights = decay >= 0.f;
+  Cut cut;
+  const int rc = lay_out(who, cache, H, Nq, with_weights, cut);
+  if (rc != DBSP_OK) return rc;
+  if (!q || !o || !workspace) return fail(who, DBSP_EINVAL, "null pointer");
+  const int64_t size[3] = {cache->B, H, Nq}, q_stride[3] = {q_batch, q_head, q_token}, o_stride[3] = {o_batch, o_head, o_token};
+  if (!strides_ok(q_stride, 3) || !strides_ok(o_stride, 3) || !aligned(q, 16) || !aligned(o, 16))
+    return fail(who, DBSP_EINVAL, "q and o must be 16-byte aligned, their strides multiples of 8 and a token's at most 2^24");
+  if (!distinct(size, o_stride, cache->d)) return fail(who, DBSP_EINVAL, "elements of o overlap");
+  if (!aligned(lse, 4) || !aligned(q_lens, 4)) return fail(who, DBSP_EINVAL, "lse and q_lens must be 4-byte aligned");
+  if (!aligned(workspace, 256)) return fail(who, DBSP_EINVAL, "the workspace must be 256-byte aligned");
+  if (workspace_bytes < cut.bytes)
+    return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": the workspace holds " + std::to_string(workspace_bytes) + " bytes, the call needs " + std::to_string(cut.bytes));
+  dbsp_cache_attn_params& p = cut.p;
+  auto u16 = [](const void* x) { return static_cast<const uint16_t*>(x); };
+  p.q = u16(q); p.pk = u16(cache->prefix_k); p.pv = u16(cache->prefix_v); p.k = u16(cache->k); p.v = u16(cache->v);
+  p.o = static_cast<uint16_t*>(o);
+  p.lse = lse;
+  p.weights = with_weights && p.cap > 0 ? cache->weights : nullptr;
+  p.lens = p.cap > 0 ? cache->lens : nullptr;
+  p.q_lens = q_lens;
+  p.q_sb = q_batch; p.q_sh = q_head; p.q_st = q_token;
+  p.o_sb = o_batch; p.o_sh = o_head; p.o_st = o_token;
+  p.pk_sh = cache->prefix_k_stride[0]; p.pv_sh = cache->prefix_v_stride[0];
+  p.k_sb = cache->k_stride[0]; p.k_sh = cache->k_stride[1];
+  p.v_sb = cache->v_stride[0]; p.v_sh = cache->v_stride[1];
+  p.pk_st = (int32_t)(p.P > 0 ? cache->prefix_k_stride[1] * 2 : 0); p.pv_st = (int32_t)(p.P > 0 ? cache->prefix_v_stride[1] * 2 : 0);
+  p.k_st = (int32_t)(p.cap > 0 ? cache->k_stride[2] * 2 : 0); p.v_st = (int32_t)(p.cap > 0 ? cache->v_stride[2] * 2 : 0);
+  p.causal = causal != 0;
+  p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->d)) * 1.4426950408889634f;
+  p.decay = decay;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  p.table = reinterpret_cast<int32_t*>(ws);
+  p.row_lse = reinterpret_cast<float*>(ws + cut.row_lse_at);
+  p.part_o = reinterpret_cast<float*>(ws + cut.part_o_at);
+  p.part_lse = reinterpret_cast<float*>(ws + cut.part_lse_at);
+  return done(who, dbsp_launch_cache_attn(p, cache->d, cache->dtype == DBSP_FP16, (int)cut.grid, static_cast<hipStream_t>(stream)));
+}
+
+int dbsp_cache_evict_workspace(const dbsp_cache* cache, int32_t budget, int64_t* bytes) {
+  const char* who = "dbsp_cache_evict_workspace";
+  if (!bytes) return fail(who, DBSP_EINVAL, "null pointer");
+  int64_t moves = 0;
+  const int rc = evict_bytes(who, cache, budget, moves, *bytes);
+  if (rc != DBSP_OK) *bytes = 0;
+  return rc;
+}
+
+int dbsp_cache_evict(const dbsp_cache* cache, int32_t budget, int32_t sinks, const int32_t* keep_from, void* workspace,
+                     int64_t workspace_bytes, void* stream) {
+  const char* who = "dbsp_cache_evict";
+  int64_t moves = 0, bytes = 0;
+  const int rc = evict_bytes(who, cache, budget, moves, bytes);
+  if (rc != DBSP_OK) return rc;
+  if (sinks < 0) return fail(who, DBSP_EINVAL, "sinks must not be negative");
+  if (cache->capacity == 0) return DBSP_OK;
+  if (!cache->weights || !cache->positions) return fail(who, DBSP_EINVAL, "the cache has no weights or no positions");
+  const int64_t size[3] = {cache->B, cache->Hk, cache->capacity};
+  if (!distinct(size, cache->k_stride, cache->d) || !distinct(size, cache->v_stride, cache->d)) return fail(who, DBSP_EINVAL, "elements of k or v overlap");
+  if (!aligned(keep_from, 4)) return fail(who, DBSP_EINVAL, "keep_from must be 4-byte aligned");
+  if (!workspace) return fail(who, DBSP_EINVAL, "null pointer");
+  if (!aligned(workspace, 256)) return fail(who, DBSP_EINVAL, "the workspace must be 256-byte aligned");
+  if (workspace_bytes < bytes)
+    return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": the workspace holds " + std::to_string(workspace_bytes) + " bytes, the call needs " + std::to_string(bytes));
+  if (moves == 0) return DBSP_OK;          // budget >= capacity: nothing is over it
+  dbsp_cache_evict_params p = {};
+  p.k = static_cast<unsigned char*>(cache->k); p.v = static_cast<unsigned char*>(cache->v);
+  p.weights = cache->weights; p.positions = cache->positions; p.lens = cache->lens; p.keep_from = keep_from;
+  p.k_sb = cache->k_stride[0] * 2; p.k_sh = cache->k_stride[1] * 2; p.k_st = cache->k_stride[2] * 2;
+  p.v_sb = cache->v_stride[0] * 2; p.v_sh = cache->v_stride[1] * 2; p.v_st = cache->v_stride[2] * 2;
+  p.B = cache->B; p.Hk = cache->Hk; p.cap = cache->capacity; p.row_bytes = cache->d * 2;
+  p.budget = budget; p.sinks = sinks; p.max_moves = (int32_t)moves;
+  const int64_t pairs = (int64_t)p.B * p.Hk;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  p.n_moves = reinterpret_cast<int32_t*>(ws);
+  p.holes = reinterpret_cast<int32_t*>(ws + round_up(pairs * 4, 256));
+  p.fillers = reinterpret_cast<int32_t*>(ws + round_up(pairs * 4, 256) + round_up(pairs * moves * 4, 256));
+  return done(who, dbsp_launch_cache_evict(p, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,55 @@
+// Kernel argument blocks of the key/value cache's operators (device pointers and sizes only), and what host and kernels have to
+// agree on: tile sizes and the shape of the workspace.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+constexpr int kCacheRows = 128;        // queries of a workgroup: four waves of 32
+constexpr int kCacheKeys = 64;         // keys of a tile
+constexpr int kCacheTarget = 1024;     // items that a launch is cut into where there is enough to cut, see cache_attn.hip
+
+struct dbsp_cache_attn_params {
+  const uint16_t *q, *pk, *pv, *k, *v;
+  uint16_t* o;
+  float* lse;                          // f32 [B,H,Nq] or null
+  float* weights;                      // f32 [B,Hk,cap] or null
+  const int32_t *lens, *q_lens;        // [B]; null: no own keys; every sequence has Nq new tokens
+  int64_t q_sb, q_sh, q_st, o_sb, o_sh, o_st;      // strides in elements: batch, head, token
+  int64_t pk_sh, pv_sh, k_sb, k_sh, v_sb, v_sh;
+  int32_t pk_st, pv_st, k_st, v_st;                // token strides in bytes
+  int32_t B, H, Hk, G, Nq, P, cap;
+  int32_t causal;
+  int32_t pooled;                      // the prefix is read by the rows of all sequences together, own keys apart
+  int32_t split;                       // items may be parts of a row tile's keys: partial results, and a merge behind the kernel
+  int32_t pre_tiles;                   // tiles of the prefix
+  int32_t pre_row_tiles, own_row_tiles;            // row tiles of a KV head: of all sequences together (pooled), of one sequence
+  int32_t own_rows;                    // rows of an own item's partial result: min(kCacheRows, Nq * G)
+  int32_t max_pre_items;
+  float scale_log2;                    // softmax scale * log2(e)
+  float decay;
+  // workspace
+  int32_t* table;                      // [2 + 2 B] chunks and items of the prefix, then first own item and chunks of every sequence
+  float* row_lse;                      // f32 [B,H,Nq]: log2 of the sum of exp, for the weights
+  float* part_o;                       // f32 [items][rows][D], prefix items first
+  float* part_lse;                     // f32 [items][rows], base 2
+};
+
+struct dbsp_cache_evict_params {
+  unsigned char *k, *v;
+  float* weights;                      // [B,Hk,cap]
+  int32_t* positions;                  // [B,Hk,cap]
+  int32_t* lens;                       // [B]
+  const int32_t* keep_from;            // [B] or null
+  int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st;      // strides in bytes
+  int32_t B, Hk, cap, row_bytes;
+  int32_t budget, sinks;
+  int32_t max_moves;                   // min(budget, cap - budget)
+  // workspace
+  int32_t* n_moves;                    // [B Hk]
+  int32_t *holes, *fillers;            // [B Hk][max_moves]
+};
+
+hipError_t dbsp_launch_cache_attn(const dbsp_cache_attn_params& p, int d, bool fp16, int grid, hipStream_t stream);
+hipError_t dbsp_launch_cache_evict(const dbsp_cache_evict_params& p, hipStream_t stream);

@@ -1,0 +1,173 @@
+"""Eviction from a key/value cache on the GPU against the oracle (moves and whole numbers: equal bit for bit), and a program's loop
+of attention, eviction and new tokens against a float64 run of the same."""
+
+import numpy as np
+import pytest
+
+from oracle import cache as oc
+
+pytestmark = pytest.mark.gpu
+
+
+def build(B, Hk, d, cap, lens, dtype, seed, weights="spread", layout="plain"):
+    import torch
+    rng = np.random.default_rng(seed)
+    dt = {"bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+    if layout == "plain":
+        k, v = (torch.from_numpy(rng.normal(size=(B, Hk, cap, d))).to(dt).cuda() for _ in range(2))
+    else:
+        kv = torch.from_numpy(rng.normal(size=(B, cap, Hk, 2, d))).to(dt).cuda()
+        k, v = kv[:, :, :, 0].transpose(1, 2), kv[:, :, :, 1].transpose(1, 2)
+    w = rng.random((B, Hk, cap)).astype(np.float32) ** 5
+    if weights == "ties":
+        w = (rng.integers(0, 3, (B, Hk, cap)) / 2).astype(np.float32)
+    elif weights == "equal":
+        w[:] = 0.25
+    elif weights == "special":
+        pool = np.array([np.nan, -np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-42, -1e-42, 3.4e38, -3.4e38, 1.0, -1.0], np.float32)
+        w = pool[rng.integers(0, len(pool), (B, Hk, cap))]
+    positions = np.stack([rng.permutation(cap) for _ in range(B * Hk)]).reshape(B, Hk, cap).astype(np.int32)
+    return k, v, torch.from_numpy(w).cuda(), torch.from_numpy(positions).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+
+def same(a, b):
+    return np.array_equal(a.view(np.uint32) if a.dtype == np.float32 else a, b.view(np.uint32) if b.dtype == np.float32 else b)
+
+
+def check(k, v, w, positions, lens, budget, sinks=0, keep_from=None):
+    import torch
+    import paper_2511_23113_amd as dbsp
+    cap = k.shape[2]
+    host = [x.view(torch.int16).cpu().numpy() if x.element_size() == 2 else x.cpu().numpy() for x in (k, v, w, positions)]
+    used = np.clip(lens.cpu().numpy(), 0, cap)
+    dev_keep = None if keep_from is None else torch.tensor(keep_from, dtype=torch.int32, device="cuda")
+    want = oc.cache_evict(*host, used, budget, sinks, keep_from)
+    cache = dbsp.KVCache(k, v, lens, weights=w, positions=positions)
+    dbsp.cache_evict(cache, budget, sinks=sinks, keep_from=dev_keep)
+    torch.cuda.synchronize()
+    for name, x, y in zip(("k", "v", "weights", "positions"), (k, v, w, positions), want):
+        got = x.view(torch.int16).cpu().numpy() if x.element_size() == 2 else x.cpu().numpy()
+        assert same(got, y), name
+    assert lens.cpu().tolist() == want[4].tolist()
+
+
+@pytest.mark.parametrize("weights", ["spread", "ties", "equal", "special"])
+@pytest.mark.parametrize("cap, lens, budget", [(8, [8, 0, 3], 3), (70, [70, 33, 34], 33), (200, [200, 1, 129], 1), (200, [200, 199, 150], 199),
+                                               (2300, [2300, 2049, 2048], 2048), (3000, [3000, 1025, 17], 1024), (5000, [4097, 5000, 2], 100)])
+def test_against_the_oracle(cap, lens, budget, weights):
+    check(*build(3, 2, 64, cap, lens, "bf16", cap + budget, weights), budget, sinks=2, keep_from=[cap - 5, cap, 0])
+
+
+@pytest.mark.parametrize("dtype, d", [("fp16", 128), ("bf16", 128), ("fp16", 64)])
+def test_views_types_and_many_heads(dtype, d):
+    check(*build(2, 37, d, 300, [300, 211], dtype, d, "ties", "views"), 100)
+
+
+def test_a_long_cache():
+    check(*build(1, 2, 64, 70001, [69999], "bf16", 5), 9000, sinks=4, keep_from=[69900])
+
+
+def test_more_protected_than_the_budget_keeps_the_lowest_slots():
+    check(*build(2, 2, 64, 100, [100, 90], "bf16", 6), 20, sinks=60, keep_from=[0, 95])
+
+
+def test_no_positions_protect_without_sinks_and_recent_ones():
+    k, v, w, positions, lens = build(1, 1, 64, 40, [40], "bf16", 7)
+    positions.fill_(-3)
+    check(k, v, w, positions, lens, 11)
+
+
+def test_lengths_out_of_range():
+    import torch
+    import paper_2511_23113_amd as dbsp
+    k, v, w, positions, lens = build(2, 1, 64, 50, [50, 0], "bf16", 8)
+    other = [x.clone() for x in (k, v, w, positions)]
+    check(k, v, w, positions, lens, 20)
+    wild = torch.tensor([70, -4], dtype=torch.int32, device="cuda")
+    dbsp.cache_evict(dbsp.KVCache(other[0], other[1], wild, weights=other[2], positions=other[3]), 20)
+    assert all(torch.equal(a, b) for a, b in zip((k, v, w, positions), other)) and wild.tolist() == [20, -4]
+
+
+def test_a_captured_eviction_replays():
+    import torch
+    import paper_2511_23113_amd as dbsp
+    state = build(3, 4, 128, 900, [900, 500, 700], "bf16", 9)
+    lens0, keep = state[4].clone(), torch.tensor([880, 490, 10 ** 6], dtype=torch.int32, device="cuda")
+    first = [x.clone() for x in state]
+    cache = dbsp.KVCache(*state[:2], state[4], weights=state[2], positions=state[3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dbsp.cache_evict(cache, 512, sinks=4, keep_from=keep)
+    for step in range(3):
+        for x, y in zip(state, first):
+            x.copy_(y)
+        state[4].copy_(lens0 - 40 * step)
+        plain = [x.clone() for x in state]
+        graph.replay()
+        torch.cuda.synchronize()
+        dbsp.cache_evict(dbsp.KVCache(*plain[:2], plain[4], weights=plain[2], positions=plain[3]), 512, sinks=4, keep_from=keep)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(state, plain))
+
+
+def test_a_programs_loop():
+    """A causal prompt behind a shared prefix, eviction, then tokens one by one with an eviction every fourth: outputs against
+    the oracle over the cache as it stands, weights against float64 sums, evictions against the oracle's from the GPU's weights."""
+    import torch
+    import paper_2511_23113_amd as dbsp
+    B, H, Hk, d, P, cap, budget, prompt = 2, 6, 2, 64, 90, 200, 96, 150
+    rng = np.random.default_rng(10)
+    rand = lambda *s: torch.from_numpy(rng.normal(size=s)).to(torch.bfloat16).cuda()      # noqa: E731
+    pk, pv, k, v = rand(Hk, P, d), rand(Hk, P, d), torch.zeros(B, Hk, cap, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, Hk, cap, d, dtype=torch.bfloat16, device="cuda")
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    weights, positions = torch.zeros(B, Hk, cap, device="cuda"), torch.zeros(B, Hk, cap, dtype=torch.int32, device="cuda")
+    cache = dbsp.KVCache(k, v, lens, pk, pv, weights=weights, positions=positions)
+    place = [0, 0]
+    sums = np.zeros((B, Hk, cap))
+
+    def step(new, q_lens):
+        q = rand(B, H, new, d)
+        for b in range(B):
+            n, m = int(lens[b]), q_lens[b]
+            k[b, :, n:n + m], v[b, :, n:n + m] = rand(Hk, m, d), rand(Hk, m, d)
+            positions[b, :, n:n + m] = torch.arange(place[b], place[b] + m, device="cuda", dtype=torch.int32)
+            place[b] += m
+            lens[b] += m
+        o, lse = torch.zeros_like(q), torch.zeros(B, H, new, device="cuda")
+        dbsp.cache_attn_fwd(cache, q, q_lens=torch.tensor(q_lens, dtype=torch.int32, device="cuda"), decay=1.0, o=o, lse=lse)
+        h = [x.double().cpu().numpy() for x in (q, k, v, pk, pv)]
+        O, LSE, A, W = oc.cache_attention(h[0], lens.cpu().numpy(), *h[1:], q_lens=q_lens)
+        sums[:] += W
+        there = ~np.isnan(LSE)
+        got_o, got_lse = o.double().cpu().numpy(), lse.double().cpu().numpy()
+        # probabilities and O rounded to bf16 (2^-8 each), f32 scores of 64 products
+        assert (np.abs(got_o - O) <= 2.0 ** -8 * 1.01 * (A + np.abs(O)) + 1e-5)[there].all()
+        assert (np.abs(got_lse - LSE) <= 1e-4)[there].all()
+        used = np.arange(cap) < lens.cpu().numpy()[:, None, None]
+        assert (np.abs(weights.double().cpu().numpy() - sums)[np.broadcast_to(used, sums.shape)] <= 1e-4 * sums[np.broadcast_to(used, sums.shape)] + 1e-7).all()
+
+    def evict():
+        state = [x.view(torch.int16).cpu().numpy() if x.element_size() == 2 else x.cpu().numpy() for x in (k, v, weights, positions)]
+        keep = [p - 8 for p in place]
+        before = lens.cpu().numpy()
+        want = oc.cache_evict(*state, before, budget, 2, keep)
+        # the float64 sums go where the weights went
+        moved = oc.cache_evict(sums[..., None], sums[..., None], state[2], state[3], before, budget, 2, keep)[0][..., 0]
+        sums[:] = moved
+        for b in range(B):
+            if before[b] > budget:
+                sums[b, :, budget:] = 0
+        dbsp.cache_evict(cache, budget, sinks=2, keep_from=torch.tensor(keep, dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+        for x, y in zip((k, v, weights, positions), want):
+            assert same(x.view(torch.int16).cpu().numpy() if x.element_size() == 2 else x.cpu().numpy(), y)
+        assert lens.cpu().tolist() == want[4].tolist()
+
+    step(prompt, [prompt, 101])
+    evict()
+    for i in range(12):
+        step(1, [1, 1 if i % 3 else 0])
+        if i % 4 == 3:
+            evict()
+    step(7, [7, 3])
+    evict()
