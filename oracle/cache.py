@@ -64,7 +64,8 @@ def cache_evict(k, v, weights, positions, lens, budget: int, sinks: int = 0, kee
             continue
         for h in range(Hk):
             stay = keepers(weights[b, h], positions[b, h], n, budget, sinks, None if keep_from is None else int(keep_from[b]))
-            holes = [i for i in range(budget) if i not in set(stay)]
+            there = set(stay)
+            holes = [i for i in range(budget) if i not in there]
             for to, frm in zip(holes, [i for i in stay if i >= budget]):
                 for x in (k, v, weights, positions):
                     x[b, h, to] = x[b, h, frm]

@@ -107,13 +107,23 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   return DBSP_OK;
 }
 
-int evict_bytes(const char* who, const dbsp_cache* c, int32_t budget, int64_t& moves, int64_t& bytes) {
+struct Moves {           // an eviction's workspace
+  int64_t most, parts, holes_at, fillers_at, digits_at, chosen_at, parts_at, bytes;
+};
+
+int lay_out_evict(const char* who, const dbsp_cache* c, int32_t budget, Moves& m) {
   const int rc = check_cache(who, c);
   if (rc != DBSP_OK) return rc;
   if (budget < 1) return fail(who, DBSP_EINVAL, "budget must be positive");
-  moves = std::min<int64_t>(budget, std::max(0, c->capacity - budget));
+  m.most = std::min<int64_t>(budget, std::max(0, c->capacity - budget));
+  m.parts = c->capacity > kEvictWhole ? (c->capacity + kEvictPart - 1) / kEvictPart : 0;
   const int64_t pairs = (int64_t)c->B * c->Hk;
-  bytes = round_up(pairs * 4, 256) + 2 * round_up(pairs * moves * 4, 256);
+  m.holes_at = round_up(pairs * 4, 256);
+  m.fillers_at = m.holes_at + round_up(pairs * m.most * 4, 256);
+  m.digits_at = m.fillers_at + round_up(pairs * m.most * 4, 256);
+  m.chosen_at = m.digits_at + (m.parts > 0 ? pairs * 3 * 2048 * 4 : 0);
+  m.parts_at = m.chosen_at + (m.parts > 0 ? round_up(pairs * 3 * 4, 256) : 0);
+  m.bytes = round_up(m.parts_at + pairs * m.parts * 16, 256);
   return DBSP_OK;
 }
 
@@ -178,17 +188,17 @@ int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch,
 int dbsp_cache_evict_workspace(const dbsp_cache* cache, int32_t budget, int64_t* bytes) {
   const char* who = "dbsp_cache_evict_workspace";
   if (!bytes) return fail(who, DBSP_EINVAL, "null pointer");
-  int64_t moves = 0;
-  const int rc = evict_bytes(who, cache, budget, moves, *bytes);
-  if (rc != DBSP_OK) *bytes = 0;
+  Moves m;
+  const int rc = lay_out_evict(who, cache, budget, m);
+  *bytes = rc == DBSP_OK ? m.bytes : 0;
   return rc;
 }
 
 int dbsp_cache_evict(const dbsp_cache* cache, int32_t budget, int32_t sinks, const int32_t* keep_from, void* workspace,
                      int64_t workspace_bytes, void* stream) {
   const char* who = "dbsp_cache_evict";
-  int64_t moves = 0, bytes = 0;
-  const int rc = evict_bytes(who, cache, budget, moves, bytes);
+  Moves m;
+  const int rc = lay_out_evict(who, cache, budget, m);
   if (rc != DBSP_OK) return rc;
   if (sinks < 0) return fail(who, DBSP_EINVAL, "sinks must not be negative");
   if (cache->capacity == 0) return DBSP_OK;
@@ -198,21 +208,23 @@ int dbsp_cache_evict(const dbsp_cache* cache, int32_t budget, int32_t sinks, con
   if (!aligned(keep_from, 4)) return fail(who, DBSP_EINVAL, "keep_from must be 4-byte aligned");
   if (!workspace) return fail(who, DBSP_EINVAL, "null pointer");
   if (!aligned(workspace, 256)) return fail(who, DBSP_EINVAL, "the workspace must be 256-byte aligned");
-  if (workspace_bytes < bytes)
-    return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": the workspace holds " + std::to_string(workspace_bytes) + " bytes, the call needs " + std::to_string(bytes));
-  if (moves == 0) return DBSP_OK;          // budget >= capacity: nothing is over it
+  if (workspace_bytes < m.bytes)
+    return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": the workspace holds " + std::to_string(workspace_bytes) + " bytes, the call needs " + std::to_string(m.bytes));
+  if (m.most == 0) return DBSP_OK;          // budget >= capacity: nothing is over it
   dbsp_cache_evict_params p = {};
   p.k = static_cast<unsigned char*>(cache->k); p.v = static_cast<unsigned char*>(cache->v);
   p.weights = cache->weights; p.positions = cache->positions; p.lens = cache->lens; p.keep_from = keep_from;
   p.k_sb = cache->k_stride[0] * 2; p.k_sh = cache->k_stride[1] * 2; p.k_st = cache->k_stride[2] * 2;
   p.v_sb = cache->v_stride[0] * 2; p.v_sh = cache->v_stride[1] * 2; p.v_st = cache->v_stride[2] * 2;
   p.B = cache->B; p.Hk = cache->Hk; p.cap = cache->capacity; p.row_bytes = cache->d * 2;
-  p.budget = budget; p.sinks = sinks; p.max_moves = (int32_t)moves;
-  const int64_t pairs = (int64_t)p.B * p.Hk;
+  p.budget = budget; p.sinks = sinks; p.max_moves = (int32_t)m.most; p.n_parts = (int32_t)m.parts;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   p.n_moves = reinterpret_cast<int32_t*>(ws);
-  p.holes = reinterpret_cast<int32_t*>(ws + round_up(pairs * 4, 256));
-  p.fillers = reinterpret_cast<int32_t*>(ws + round_up(pairs * 4, 256) + round_up(pairs * moves * 4, 256));
+  p.holes = reinterpret_cast<int32_t*>(ws + m.holes_at);
+  p.fillers = reinterpret_cast<int32_t*>(ws + m.fillers_at);
+  p.digits = reinterpret_cast<uint32_t*>(ws + m.digits_at);
+  p.chosen = reinterpret_cast<uint32_t*>(ws + m.chosen_at);
+  p.parts = reinterpret_cast<int32_t*>(ws + m.parts_at);
   return done(who, dbsp_launch_cache_evict(p, static_cast<hipStream_t>(stream)));
 }
 

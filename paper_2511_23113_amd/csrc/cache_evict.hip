@@ -5,9 +5,15 @@
 // budget moves into the hole that an evicted one leaves in front of it, both in ascending order.  Sources (slots >= budget) and
 // destinations (slots < budget) are disjoint, so rows move in place, in parallel, and only those that have to.
 //
-// Choosing: a workgroup a (sequence, head) finds the budget-th largest of the weights' order-preserving 32-bit images, eight
-// bits at a time by counting (the counts are whole numbers: their order of arrival does not matter), lists holes and
-// fillers by a running count in slot order, and moves weights and positions.  A second launch moves the rows of K and V.
+// Choosing goes by the weights' order-preserving 32-bit images, of which the budget-th largest is the limit.
+//   * Up to 32,768 slots a workgroup has a (sequence, head), all its images in registers, read once.  The limit is built from the
+//     top, two bits at a time, by counting the images that reach each of three candidates (ballots; one exchange of the waves'
+//     counts a step), until a candidate leaves exactly the budget.  That takes as long whatever the weights are; counts by
+//     digit in the LDS, 8 bits a pass, took 46 us of 16,500 slots where these take FIXME, as weights of like size meet in a few
+//     of the counters.
+//   * Longer ones are cut into workgroups of 8192 slots: three launches count digits of 11, 11 and 10 bits, a fourth what
+//     each part keeps, a fifth lists holes and fillers.  Whole numbers are added, so their order of arrival does not matter.
+// A last launch moves the rows of K and V.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -18,8 +24,8 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int NT = 1024, WAVES = NT / 64;
 constexpr int kMovesPerGroup = 64;
+constexpr int kNT = 1024;              // threads that choose
 
 // Larger weight, larger image; what must stay comes last.
 __device__ __forceinline__ uint32_t image(float w, bool stays) {
@@ -30,97 +36,310 @@ __device__ __forceinline__ uint32_t image(float w, bool stays) {
   return (x >> 31) ? ~x : x | 0x80000000u;
 }
 
-__global__ __launch_bounds__(NT) void dbsp_cache_choose_kernel(const dbsp_cache_evict_params p) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t chosen, rank_left;
-  __shared__ int wave_equal[WAVES], wave_out[WAVES];
-  const int pair = blockIdx.x, b = pair / p.Hk, t = threadIdx.x, w = t >> 6, l = t & 63;
-  const int n = max(0, min(p.lens[b], p.cap));
-  if (n <= p.budget) {
+// Images of the slots first + j * NT + t below n, j = 0 .. R - 1; 0, which is nobody's, past them.
+template <int NT, int R>
+__device__ __forceinline__ void load_images(const dbsp_cache_evict_params& p, int pair, int first, int n, uint32_t (&x)[R]) {
+  const float* weights = p.weights + (int64_t)pair * p.cap;
+  const int32_t* positions = p.positions + (int64_t)pair * p.cap;
+  const bool recent = p.keep_from != nullptr;
+  const int keep_from = recent ? p.keep_from[pair / p.Hk] : 0;
+  float w[R];
+  int at[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    w[j] = 0.f;
+    at[j] = 0;
+    if (first + j * NT >= n) continue;
+    const int i = min(first + j * NT + (int)threadIdx.x, n - 1);
+    w[j] = weights[i];
+    at[j] = positions[i];
+  }
+#pragma unroll
+  for (int j = 0; j < R; ++j)
+    x[j] = first + j * NT + (int)threadIdx.x < n ? image(w[j], at[j] < p.sinks || (recent && at[j] >= keep_from)) : 0u;
+}
+
+__device__ __forceinline__ int used_of(const dbsp_cache_evict_params& p, int pair) { return max(0, min(p.lens[pair / p.Hk], p.cap)); }
+
+// Exclusive prefix, in slot order, of the counts that every wave has for its j-th run of 64 slots: table[j * WAVES + w].
+template <int NT, int R>
+__device__ __forceinline__ void scan_table(int (&table)[R * NT / 64 + 1]) {
+  constexpr int N = R * NT / 64, PER = (N + 63) / 64;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int l = threadIdx.x;
+    int v[PER], mine = 0;
+#pragma unroll
+    for (int y = 0; y < PER; ++y) {
+      const int i = l * PER + y;
+      v[y] = i < N ? table[i] : 0;
+      mine += v[y];
+    }
+    int upto = mine;
+    for (int s = 1; s < 64; s <<= 1) {
+      const int o = __shfl_up(upto, s);
+      if (l >= s) upto += o;
+    }
+    int before = upto - mine;
+#pragma unroll
+    for (int y = 0; y < PER; ++y) {
+      const int i = l * PER + y;
+      if (i < N) table[i] = before;
+      before += v[y];
+    }
+    if (l == 63) table[N] = upto;
+  }
+  __syncthreads();
+}
+
+// What stays, of R images a thread: those above the limit, and of its equals the first stay_equal (counted from equal_before of them
+// in front of these slots); and the ranks of holes (slots below the budget that go) and fillers (slots from it on that stay).
+template <int NT, int R, class F>
+__device__ __forceinline__ void list_moves(const uint32_t (&x)[R], int first, int n, int budget, uint32_t limit, int stay_equal, bool some_equals_go,
+                                           int equal_before, int (&table)[R * NT / 64 + 1], F&& each, int* n_holes, int* n_fillers) {
+  constexpr int WAVES = NT / 64;
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+  const uint64_t below = (1ull << l) - 1;
+  uint32_t kept = 0;
+  if (some_equals_go) {
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const uint64_t m = __builtin_amdgcn_ballot_w64(x[j] == limit);
+      if (l == 0) table[j * WAVES + w] = __popcll(m);
+    }
+    scan_table<NT, R>(table);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const uint64_t m = __builtin_amdgcn_ballot_w64(x[j] == limit);
+      const int e = equal_before + table[j * WAVES + w] + __popcll(m & below);
+      kept |= (uint32_t)(x[j] > limit || (x[j] == limit && e < stay_equal)) << j;
+    }
+    __syncthreads();                       // before the table is used again
+  } else {
+#pragma unroll
+    for (int j = 0; j < R; ++j) kept |= (uint32_t)(x[j] >= limit) << j;
+  }
+  // holes and fillers counted in one: no wave's run of 64 slots has more than 64 of either
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int i = first + j * NT + (int)threadIdx.x;
+    const bool stays = kept >> j & 1, in = i < n;
+    const uint64_t hm = __builtin_amdgcn_ballot_w64(in && i < budget && !stays), fm = __builtin_amdgcn_ballot_w64(in && i >= budget && stays);
+    if (l == 0) table[j * WAVES + w] = __popcll(hm) | __popcll(fm) << 16;
+  }
+  scan_table<NT, R>(table);
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    if (first + j * NT >= n) break;
+    const int i = first + j * NT + (int)threadIdx.x;
+    const bool stays = kept >> j & 1, in = i < n, hole = in && i < budget && !stays, filler = in && i >= budget && stays;
+    const uint64_t hm = __builtin_amdgcn_ballot_w64(hole), fm = __builtin_amdgcn_ballot_w64(filler);
+    const int before = table[j * WAVES + w];
+    each(j, i, hole, filler, in && !stays, hole ? (before & 0xffff) + __popcll(hm & below) : (before >> 16) + __popcll(fm & below));
+  }
+  *n_holes = table[R * WAVES] & 0xffff;
+  *n_fillers = table[R * WAVES] >> 16;
+}
+
+// Counts digit PASS of the `here` images that agree with `limit` above it: hist, 2048 zeros before.
+constexpr int kDigits = 2048, kShift[3] = {21, 10, 0};
+template <int PASS, int R>
+__device__ __forceinline__ void count_digits(const uint32_t (&x)[R], int here, uint32_t limit, uint32_t* hist) {
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    if (j * kNT >= here) break;
+    const bool in = x[j] != 0u && (PASS == 0 || (x[j] ^ limit) >> kShift[PASS ? PASS - 1 : 0] == 0u);
+    const uint32_t digit = x[j] >> kShift[PASS] & (PASS == 2 ? 1023 : 2047);
+    const uint64_t m = __builtin_amdgcn_ballot_w64(in);
+    if (m == 0) continue;
+    // a wave whose images all have one digit adds once (equal weights would take turns at one counter)
+    const uint32_t one = __builtin_amdgcn_readlane(digit, __builtin_ctzll(m));
+    if (__builtin_amdgcn_ballot_w64(in && digit != one) == 0) {
+      if ((threadIdx.x & 63) == 0) atomicAdd(&hist[one], (uint32_t)__popcll(m));
+    } else if (in) {
+      atomicAdd(&hist[digit], 1u);
+    }
+  }
+}
+
+// Two of a digit's 2048 counts: thread 0 has those of the largest digits.
+struct two { uint32_t hi, lo; };
+__device__ __forceinline__ two my_digits(const uint32_t* counts) { return {counts[kDigits - 1 - 2 * threadIdx.x], counts[kDigits - 2 - 2 * threadIdx.x]}; }
+
+// Of the images whose upper bits are those of `limit`: the digit below them at which `left` of them, from the largest on, are
+// reached.  limit and left are brought up to date; returns how many have the chosen digit.
+__device__ __forceinline__ uint32_t pick_digit(two counts, int shift, uint32_t& limit, uint32_t& left) {
+  __shared__ uint32_t wave_sum[kNT / 64], got[3];
+  const int t = threadIdx.x, w = t >> 6, l = t & 63;
+  const uint32_t hi = counts.hi, lo = counts.lo;
+  uint32_t upto = hi + lo;
+  for (int s = 1; s < 64; s <<= 1) {
+    const uint32_t o = __shfl_up(upto, s);
+    if (l >= s) upto += o;
+  }
+  if (l == 63) wave_sum[w] = upto;
+  __syncthreads();
+  uint32_t before = upto - hi - lo;
+#pragma unroll
+  for (int y = 0; y < kNT / 64; ++y) before += y < w ? wave_sum[y] : 0u;
+  if (before < left && left <= before + hi + lo) {
+    const bool first = left <= before + hi;
+    got[0] = kDigits - 1 - 2 * t - (first ? 0 : 1);
+    got[1] = left - before - (first ? 0 : hi);
+    got[2] = first ? hi : lo;
+  }
+  __syncthreads();
+  limit |= got[0] << shift;
+  left = got[1];
+  const uint32_t equal = got[2];
+  __syncthreads();
+  return equal;
+}
+
+template <int R>
+__global__ __launch_bounds__(kNT) void dbsp_cache_choose_kernel(const dbsp_cache_evict_params p) {
+  static_assert(R <= 32 && kNT * R <= kEvictWhole, "16 bits a count, a bit a slot");
+  __shared__ uint32_t hist[3 * kDigits];
+  __shared__ int table[R * kNT / 64 + 1];
+  const int pair = blockIdx.x, t = threadIdx.x;
+  const int n = used_of(p, pair), budget = p.budget;
+  if (n <= budget) {
     if (t == 0) p.n_moves[pair] = 0;
     return;
   }
-  float* weights = p.weights + (int64_t)pair * p.cap;
-  int32_t* positions = p.positions + (int64_t)pair * p.cap;
-  const bool recent = p.keep_from != nullptr;
-  const int keep_from = recent ? p.keep_from[b] : 0;
-  auto image_of = [&](int i) {
-    const int at = positions[i];
-    return image(weights[i], at < p.sinks || (recent && at >= keep_from));
-  };
-  // the budget-th largest image: `chosen`, and how many of its equals stay
-  uint32_t prefix = 0, left = (uint32_t)p.budget;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (t < 256) hist[t] = 0;
-    __syncthreads();
-    for (int i = t; i < n; i += NT) {
-      const uint32_t x = image_of(i);
-      if (shift == 24 || (x >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(x >> shift) & 255], 1u);
-    }
-    __syncthreads();
-    if (w == 0) {                          // lane l: digits 4 l .. 4 l + 3, counted from the largest
-      uint32_t c[4], mine = 0;
-      for (int j = 0; j < 4; ++j) mine += c[j] = hist[4 * l + j];
-      uint32_t above = mine;               // of this lane and those behind it
-      for (int s = 1; s < 64; s <<= 1) {
-        const uint32_t o = __shfl_down(above, s);
-        if (l + s < 64) above += o;
-      }
-      above -= mine;
-      for (int j = 3; j >= 0; --j) {
-        if (above < left && left <= above + c[j]) {
-          chosen = prefix | (uint32_t)(4 * l + j) << shift;
-          rank_left = left - above;
-        }
-        above += c[j];
-      }
-    }
-    __syncthreads();
-    prefix = chosen;
-    left = rank_left;
-    __syncthreads();
-  }
-  // in slot order: equals of the chosen image stay until `left` of them have
-  const uint32_t limit = prefix;
-  const int stay_equal = (int)left;
-  int32_t *holes = p.holes + (int64_t)pair * p.max_moves, *fillers = p.fillers + (int64_t)pair * p.max_moves;
-  int equal_before = 0, holes_before = 0, fillers_before = 0;
-  for (int i0 = 0; i0 < n; i0 += NT) {
-    const int i = i0 + t;
-    const uint32_t x = i < n ? image_of(i) : 0u;
-    const bool equal = i < n && x == limit;
-    const uint64_t em = __builtin_amdgcn_ballot_w64(equal), below = (1ull << l) - 1;
-    if (l == 0) wave_equal[w] = __popcll(em);
-    __syncthreads();
-    int e = equal_before + __popcll(em & below);
-    for (int y = 0; y < WAVES; ++y) {
-      if (y < w) e += wave_equal[y];
-      equal_before += wave_equal[y];
-    }
-    const bool kept = i < n && (x > limit || (equal && e < stay_equal));
-    const bool hole = i < p.budget && !kept, filler = i >= p.budget && kept;
-    const uint64_t hm = __builtin_amdgcn_ballot_w64(hole), fm = __builtin_amdgcn_ballot_w64(filler);
-    if (l == 0) wave_out[w] = __popcll(hm) | __popcll(fm) << 16;
-    __syncthreads();
-    int at_h = holes_before + __popcll(hm & below), at_f = fillers_before + __popcll(fm & below);
-    for (int y = 0; y < WAVES; ++y) {
-      const int h = wave_out[y] & 0xffff, f = wave_out[y] >> 16;
-      if (y < w) { at_h += h; at_f += f; }
-      holes_before += h;
-      fillers_before += f;
-    }
-    if (hole) holes[at_h] = i;
-    if (filler) fillers[at_f] = i;
-  }
-  __syncthreads();                         // the lists are this workgroup's own
-  for (int i = t; i < fillers_before; i += NT) {
-    const int from = fillers[i], to = holes[i];
-    weights[to] = weights[from];
-    positions[to] = positions[from];
-  }
+  uint32_t x[R];
+  load_images<kNT, R>(p, pair, 0, n, x);
+  for (int i = t; i < 3 * kDigits; i += kNT) hist[i] = 0;
   __syncthreads();
-  for (int i = p.budget + t; i < n; i += NT) weights[i] = 0.f;      // what is appended there starts from nothing
-  if (t == 0) p.n_moves[pair] = fillers_before;
+  // `left` of the `equal` images that have the limit's digits so far stay, and all above them
+  uint32_t limit = 0, left = (uint32_t)budget;
+  count_digits<0, R>(x, n, limit, hist);
+  __syncthreads();
+  uint32_t equal = pick_digit(my_digits(hist), kShift[0], limit, left);
+  if (equal != left) {
+    count_digits<1, R>(x, n, limit, hist + kDigits);
+    __syncthreads();
+    equal = pick_digit(my_digits(hist + kDigits), kShift[1], limit, left);
+  }
+  if (equal != left) {
+    count_digits<2, R>(x, n, limit, hist + 2 * kDigits);
+    __syncthreads();
+    equal = pick_digit(my_digits(hist + 2 * kDigits), kShift[2], limit, left);
+  }
+  int32_t *holes = p.holes + (int64_t)pair * p.max_moves, *fillers = p.fillers + (int64_t)pair * p.max_moves;
+  float* weights = p.weights + (int64_t)pair * p.cap;
+  int n_holes, n_fillers;
+  list_moves<kNT, R>(x, 0, n, budget, limit, (int)left, equal != left, 0, table,
+                     [&](int, int i, bool hole, bool filler, bool goes, int rank) {
+                       if (hole) holes[rank] = i;
+                       if (filler) fillers[rank] = i;
+                       if (goes && i >= budget) weights[i] = 0.f;
+                     }, &n_holes, &n_fillers);
+  if (t == 0) p.n_moves[pair] = n_fillers;
+}
+
+// Long caches, a part a workgroup.
+constexpr int kR = 8;
+static_assert(kNT * kR == kEvictPart, "slots of a part");
+
+__global__ __launch_bounds__(256) void dbsp_cache_clear_kernel(uint32_t* digits, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) digits[i] = 0;
+}
+
+// PASS 0, 1, 2: counts the digits of 11, 11 and 10 bits from the top.  PASS 3: counts what each part keeps.  PASS 4: lists.
+template <int PASS>
+__global__ __launch_bounds__(kNT) void dbsp_cache_part_kernel(const dbsp_cache_evict_params p) {
+  __shared__ uint32_t hist[PASS < 3 ? kDigits : 1];
+  __shared__ int table[PASS == 4 ? kR * kNT / 64 + 1 : 1];
+  __shared__ int sums[PASS >= 3 ? 4 : 1];
+  const int pair = blockIdx.x, part = blockIdx.y, t = threadIdx.x, first = part * kEvictPart;
+  const int n = used_of(p, pair), budget = p.budget;
+  if (n <= budget) {
+    if (PASS == 4 && part == 0 && t == 0) p.n_moves[pair] = 0;
+    return;
+  }
+  if (first >= n) return;
+  uint32_t x[kR];
+  uint32_t* digits = p.digits + (int64_t)pair * 3 * kDigits;
+  uint32_t limit = 0, left = (uint32_t)budget, equal = 0;
+  uint32_t* chosen = p.chosen + pair * 3;
+  two counts[PASS > 0 && PASS < 4 ? PASS : 1];
+  if constexpr (PASS == 4) {
+    limit = chosen[0];
+    left = chosen[1];
+    equal = chosen[2];
+  }
+#pragma unroll
+  for (int y = 0; y < PASS && PASS < 4; ++y) counts[y] = my_digits(digits + y * kDigits);
+  load_images<kNT, kR>(p, pair, first, n, x);
+#pragma unroll
+  for (int y = 0; y < PASS && PASS < 4; ++y) equal = pick_digit(counts[y], kShift[y], limit, left);
+  if (PASS == 3 && part == 0 && t == 0) {
+    chosen[0] = limit;
+    chosen[1] = left;
+    chosen[2] = equal;
+  }
+  if constexpr (PASS < 3) {
+    for (int i = t; i < kDigits; i += kNT) hist[i] = 0;
+    __syncthreads();
+    count_digits<PASS, kR>(x, n - first, limit, hist);
+    __syncthreads();
+    for (int i = t; i < kDigits; i += kNT)
+      if (hist[i]) atomicAdd(&digits[PASS * kDigits + i], hist[i]);
+  } else {
+    // above the limit and equal to it, in slots below the budget and from it on
+    int32_t* parts = p.parts + (int64_t)pair * p.n_parts * 4;
+    if (t < 4) sums[t] = 0;
+    __syncthreads();
+    if constexpr (PASS == 3) {
+      int c[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < kR; ++j) {
+        const bool late = first + j * kNT + t >= budget;
+        c[0] += __popcll(__builtin_amdgcn_ballot_w64(x[j] > limit && !late));
+        c[1] += __popcll(__builtin_amdgcn_ballot_w64(x[j] == limit && !late));
+        c[2] += __popcll(__builtin_amdgcn_ballot_w64(x[j] > limit && late));
+        c[3] += __popcll(__builtin_amdgcn_ballot_w64(x[j] == limit && late));
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        if ((t & 63) == 0) atomicAdd(&sums[y], c[y]);
+      __syncthreads();
+      if (t < 4) parts[part * 4 + t] = sums[t];
+    } else {
+      // of the parts in front of this one: equals, holes and fillers.  Equals stay in slot order, so how many of a part's do
+      // follows from the equals in front of it.
+      int eq = 0;
+      for (int y = t; y < part; y += kNT) eq += parts[y * 4 + 1] + parts[y * 4 + 3];
+      if (eq) atomicAdd(&sums[0], eq);
+      __syncthreads();
+      const int equal_before = sums[0];
+      // kept slots below the budget in front of this part, and from it on: equals that stay are the first `left`
+      int gt_early = 0, eq_early = 0, gt_late = 0;
+      for (int y = t; y < part; y += kNT) {
+        gt_early += parts[y * 4];
+        eq_early += parts[y * 4 + 1];
+        gt_late += parts[y * 4 + 2];
+      }
+      if (gt_early) atomicAdd(&sums[1], gt_early);
+      if (eq_early) atomicAdd(&sums[2], eq_early);
+      if (gt_late) atomicAdd(&sums[3], gt_late);
+      __syncthreads();
+      const int early = min(first, budget), stay_early = sums[1] + min((int)left, sums[2]);
+      const int holes_before = early - stay_early;
+      const int fillers_before = sums[3] + min((int)left, equal_before) - min((int)left, sums[2]);
+      int32_t *holes = p.holes + (int64_t)pair * p.max_moves + holes_before, *fillers = p.fillers + (int64_t)pair * p.max_moves + fillers_before;
+      float* weights = p.weights + (int64_t)pair * p.cap;
+      int n_holes, n_fillers;
+      list_moves<kNT, kR>(x, first, n, budget, limit, (int)left, equal != left, equal_before, table,
+                          [&](int, int i, bool hole, bool filler, bool goes, int rank) {
+                            if (hole) holes[rank] = i;
+                            if (filler) fillers[rank] = i;
+                            if (goes && i >= budget) weights[i] = 0.f;
+                          }, &n_holes, &n_fillers);
+      if (t == 0 && first + kEvictPart >= n) p.n_moves[pair] = fillers_before + n_fillers;
+    }
+  }
 }
 
 __global__ __launch_bounds__(256) void dbsp_cache_move_kernel(const dbsp_cache_evict_params p) {
@@ -134,15 +353,37 @@ __global__ __launch_bounds__(256) void dbsp_cache_move_kernel(const dbsp_cache_e
     const u32x4 kr = *reinterpret_cast<const u32x4*>(k + from * p.k_st), vr = *reinterpret_cast<const u32x4*>(v + from * p.v_st);
     *reinterpret_cast<u32x4*>(k + to * p.k_st) = kr;
     *reinterpret_cast<u32x4*>(v + to * p.v_st) = vr;
+    if (x == 0) {                          // (what a freed slot's next key starts from is nothing; the others' weights are cleared already)
+      const int64_t at = (int64_t)pair * p.cap;
+      p.weights[at + to] = p.weights[at + from];
+      p.positions[at + to] = p.positions[at + from];
+      p.weights[at + from] = 0.f;
+    }
   }
 }
 
 }  // namespace
 
 hipError_t dbsp_launch_cache_evict(const dbsp_cache_evict_params& p, hipStream_t stream) {
-  dbsp_cache_choose_kernel<<<p.B * p.Hk, NT, 0, stream>>>(p);
+  const int pairs = p.B * p.Hk;
+  if (p.n_parts > 0) {
+    const int64_t n = (int64_t)pairs * 3 * kDigits;
+    dbsp_cache_clear_kernel<<<(unsigned)((n + 4095) / 4096), 256, 0, stream>>>(p.digits, n);
+    const dim3 grid(pairs, p.n_parts);
+    dbsp_cache_part_kernel<0><<<grid, kNT, 0, stream>>>(p);
+    dbsp_cache_part_kernel<1><<<grid, kNT, 0, stream>>>(p);
+    dbsp_cache_part_kernel<2><<<grid, kNT, 0, stream>>>(p);
+    dbsp_cache_part_kernel<3><<<grid, kNT, 0, stream>>>(p);
+    dbsp_cache_part_kernel<4><<<grid, kNT, 0, stream>>>(p);
+  } else if (p.cap <= 4 * kNT) {
+    dbsp_cache_choose_kernel<4><<<pairs, kNT, 0, stream>>>(p);
+  } else if (p.cap <= 12 * kNT) {
+    dbsp_cache_choose_kernel<12><<<pairs, kNT, 0, stream>>>(p);
+  } else {
+    dbsp_cache_choose_kernel<32><<<pairs, kNT, 0, stream>>>(p);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  dbsp_cache_move_kernel<<<dim3(p.B * p.Hk, (p.max_moves + kMovesPerGroup - 1) / kMovesPerGroup), 256, 0, stream>>>(p);
+  dbsp_cache_move_kernel<<<dim3(pairs, (p.max_moves + kMovesPerGroup - 1) / kMovesPerGroup), 256, 0, stream>>>(p);
   return hipGetLastError();
 }

@@ -10,6 +10,9 @@ constexpr int kCacheRows = 128;        // queries of a workgroup: four waves of 
 constexpr int kCacheKeys = 64;         // keys of a tile
 constexpr int kCacheTarget = 1024;     // items that a launch is cut into where there is enough to cut, see cache_attn.hip
 
+constexpr int kEvictWhole = 32768;     // slots that a workgroup chooses among by itself, and those of a part where there are more
+constexpr int kEvictPart = 8192;
+
 struct dbsp_cache_attn_params {
   const uint16_t *q, *pk, *pv, *k, *v;
   uint16_t* o;
@@ -46,9 +49,13 @@ struct dbsp_cache_evict_params {
   int32_t B, Hk, cap, row_bytes;
   int32_t budget, sinks;
   int32_t max_moves;                   // min(budget, cap - budget)
+  int32_t n_parts;                     // parts of kEvictPart slots; 0: a workgroup takes a (sequence, head) whole
   // workspace
   int32_t* n_moves;                    // [B Hk]
   int32_t *holes, *fillers;            // [B Hk][max_moves]
+  uint32_t* digits;                    // [B Hk][3][2048] images by digit; only with parts
+  uint32_t* chosen;                    // [B Hk][3] the limit, how many of its equals stay, and how many there are
+  int32_t* parts;                      // [B Hk][n_parts][4] images above the limit and equal to it, below the budget and from it on
 };
 
 hipError_t dbsp_launch_cache_attn(const dbsp_cache_attn_params& p, int d, bool fp16, int grid, hipStream_t stream);

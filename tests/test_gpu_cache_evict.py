@@ -63,8 +63,14 @@ def test_views_types_and_many_heads(dtype, d):
     check(*build(2, 37, d, 300, [300, 211], dtype, d, "ties", "views"), 100)
 
 
-def test_a_long_cache():
-    check(*build(1, 2, 64, 70001, [69999], "bf16", 5), 9000, sinks=4, keep_from=[69900])
+@pytest.mark.parametrize("weights", ["spread", "ties", "equal", "special"])
+@pytest.mark.parametrize("cap, lens, budget", [(70001, [69999, 8193], 8192), (33000, [33000, 100], 20000), (40000, [32769, 40000], 39999)])
+def test_long_caches(cap, lens, budget, weights):
+    check(*build(2, 1, 64, cap, lens, "bf16", cap, weights), budget, sinks=4, keep_from=[cap - 100, cap])
+
+
+def test_the_largest_cache_that_one_workgroup_chooses_among():
+    check(*build(1, 2, 64, 32768, [32768], "bf16", 5), 9000, sinks=4, keep_from=[32700])
 
 
 def test_more_protected_than_the_budget_keeps_the_lowest_slots():
