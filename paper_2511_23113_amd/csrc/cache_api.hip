@@ -69,7 +69,7 @@ int check_cache(const char* who, const dbsp_cache* c) {
 
 struct Cut {             // how an attention call is laid out
   dbsp_cache_attn_params p;
-  int64_t grid, row_lse_at, part_o_at, part_lse_at, bytes;
+  int64_t grid, row_lse_at, part_o_at, part_lse_at, scores_at, bytes;
 };
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -86,13 +86,13 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   const int64_t rows = (int64_t)Nq * p.G, all_rows = rows * p.B, q_rows = (int64_t)p.B * Nq * H;
   if (rows > kMost || all_rows > kMost || q_rows / 8 > kMost) return fail(who, DBSP_ESHAPE, "too many queries");
   p.pre_tiles = (p.P + kCacheKeys - 1) / kCacheKeys;
-  p.pooled = p.P > 0 && p.B > 1 && rows < kCacheRows;
+  p.pooled = p.pre_tiles > kCacheWhole && p.B > 1 && rows < kCacheRows;
   p.pre_row_tiles = p.pooled ? (int32_t)((all_rows + kCacheRows - 1) / kCacheRows) : 0;
   p.own_row_tiles = (int32_t)((rows + kCacheRows - 1) / kCacheRows);
   p.own_rows = (int32_t)std::min<int64_t>(rows, kCacheRows);
   const int64_t unit = (int64_t)p.Hk * p.own_row_tiles, pre_unit = (int64_t)p.Hk * p.pre_row_tiles, row_tiles = unit * p.B;
   const int64_t most_tiles = (p.pooled ? 0 : p.pre_tiles) + (p.cap + kCacheKeys - 1) / kCacheKeys;
-  p.split = p.pooled || (row_tiles < kCacheTarget && most_tiles > 1);
+  p.split = p.pooled || (row_tiles < kCacheTarget && most_tiles > kCacheWhole);
   // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kCacheTarget of them
   const int64_t pre_items = std::min(pre_unit * p.pre_tiles, kCacheTarget + pre_unit);
   const int64_t own_items = p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), kCacheTarget + row_tiles) : row_tiles;
@@ -103,7 +103,10 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   cut.part_o_at = cut.row_lse_at + (with_weights ? round_up(q_rows * 4, 256) : 0);
   const int64_t part_rows = p.split ? p.max_pre_items * (int64_t)kCacheRows + own_items * p.own_rows : 0;
   cut.part_lse_at = cut.part_o_at + part_rows * c->d * 4;
-  cut.bytes = round_up(cut.part_lse_at + part_rows * 4, 256);
+  cut.scores_at = round_up(cut.part_lse_at + part_rows * 4, 256);
+  const bool keep_scores = with_weights && p.cap > 0 && rows * 128 <= kScoreRows * c->d;
+  p.score_pitch = keep_scores ? round_up(p.cap, kCacheKeys) : 0;
+  cut.bytes = round_up(cut.scores_at + (int64_t)p.B * p.Hk * rows * p.score_pitch * 4, 256);
   return DBSP_OK;
 }
 
@@ -182,6 +185,7 @@ int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch,
   p.row_lse = reinterpret_cast<float*>(ws + cut.row_lse_at);
   p.part_o = reinterpret_cast<float*>(ws + cut.part_o_at);
   p.part_lse = reinterpret_cast<float*>(ws + cut.part_lse_at);
+  p.scores = p.score_pitch > 0 ? reinterpret_cast<float*>(ws + cut.scores_at) : nullptr;
   return done(who, dbsp_launch_cache_attn(p, cache->d, cache->dtype == DBSP_FP16, (int)cut.grid, static_cast<hipStream_t>(stream)));
 }
 

@@ -12,7 +12,7 @@
 //
 // Items.  An item is a row tile and a range of its key tiles.  Lengths are known on the device only, so every workgroup
 // works out from them how the launch is cut: about kCacheTarget items of equally many tiles, each sequence into equal parts.
-// Parts leave partial results (O, and LSE to base 2, in f32) that dbsp_cache_merge joins: LSE = log sum exp LSE_i,
+// Parts leave partial results (O, and LSE to base 2, in f32) that a second launch joins: LSE = log sum exp LSE_i,
 // O = sum exp(LSE_i - LSE) O_i.  Items of the same keys lie next to each other and on the same die (workgroup number mod 8).
 //
 // A workgroup is four waves of 32 queries each.  Tiles of 64 keys go to the LDS directly (global_load_lds_dwordx4), two in
@@ -285,6 +285,13 @@ void dbsp_cache_attn_kernel(const dbsp_cache_attn_params p) {
         for (int e = 0; e < 16; ++e)
           if (32 * u + 8 * (e / 4) + e % 4 >= left) s[u][e] = -INFINITY;
     }
+    if (p.scores && !pre && valid) {       // few rows: kept for the weights, which then need not read K again
+      float* to = p.scores + (((int64_t)b * p.Hk + hk) * p.own_rows + row) * p.score_pitch + tok + 4 * g;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(to + 32 * u + 8 * i) = f32x4{s[u][4 * i], s[u][4 * i + 1], s[u][4 * i + 2], s[u][4 * i + 3]};
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -361,32 +368,47 @@ void dbsp_cache_attn_kernel(const dbsp_cache_attn_params p) {
   }
 }
 
-// Joins the partial results of a row: D / 4 lanes a row, four values each.
-template <class T, int D>
-__global__ __launch_bounds__(256) void dbsp_cache_merge_kernel(const dbsp_cache_attn_params p) {
-  constexpr int LANES = D / 4, ROWS = 256 / LANES;
-  const int64_t q_row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;      // [b][h][t]
-  if (q_row >= (int64_t)p.B * p.H * p.Nq) return;
-  const int t = (int)(q_row % p.Nq), h = (int)(q_row / p.Nq % p.H), b = (int)(q_row / p.Nq / p.H), x = 4 * (threadIdx.x % LANES);
-  if (t >= q_len_of(p, b)) return;
-  const int hk = h / p.G, g = h % p.G, pre_parts = p.table[0], first = p.table[2 + 2 * b], parts = p.table[3 + 2 * b];
-  if (pre_parts == 0 && parts == 1) return;            // one item had them all
-  const int own_row = t * p.G + g, pre_row = (b * p.Nq + t) * p.G + g;
-  const int rt = own_row / kCacheRows, n = pre_parts + parts;
-  auto at = [&](int i) -> int64_t {
-    if (i < pre_parts) return part_row(p, false, ((int64_t)hk * pre_parts + i) * p.pre_row_tiles + pre_row / kCacheRows) + pre_row % kCacheRows;
-    return part_row(p, true, (int64_t)first * p.Hk * p.own_row_tiles + ((int64_t)hk * parts + i - pre_parts) * p.own_row_tiles + rt) + own_row % kCacheRows;
-  };
+// Where the partial results of a query lie: parts of the pooled prefix, then parts of its own items.
+struct Parts {
+  int pre, own;
+  int64_t pre_row, pre_step, own_row, own_step;        // rows of the first part, and from part to part
+  __device__ __forceinline__ int64_t row(int i) const { return i < pre ? pre_row + i * pre_step : own_row + (i - pre) * own_step; }
+};
+__device__ __forceinline__ Parts parts_of(const dbsp_cache_attn_params& p, int b, int hk, int t, int g) {
+  const int own = t * p.G + g, pre = (b * p.Nq + t) * p.G + g;
+  Parts x;
+  x.pre = p.table[0];
+  x.own = p.table[3 + 2 * b];
+  x.pre_row = part_row(p, false, (int64_t)hk * x.pre * p.pre_row_tiles + pre / kCacheRows) + pre % kCacheRows;
+  x.pre_step = (int64_t)p.pre_row_tiles * kCacheRows;
+  x.own_row = part_row(p, true, ((int64_t)p.table[2 + 2 * b] * p.Hk + (int64_t)hk * x.own) * p.own_row_tiles + own / kCacheRows) + own % kCacheRows;
+  x.own_step = (int64_t)p.own_row_tiles * p.own_rows;
+  return x;
+}
+
+// Behind the attention kernel.  The first p.merge_groups workgroups join partial results, D / 4 lanes a part of a row, four values
+// each: WAYS of them a row, which take its parts in turn (rows are few where parts are many).  The others sum the
+// weights from the scores that the attention kernel has kept, 1024 slots of a (sequence, KV head) each.
+template <class T, int D, int WAYS>
+__device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
+  constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, U = 4;
+  const int unit = threadIdx.x / LANES, way = unit % WAYS, x = 4 * (threadIdx.x % LANES);
+  const int64_t q_row = (int64_t)blockIdx.x * ROWS + unit / WAYS;      // [b][h][t]
+  const bool there = q_row < (int64_t)p.B * p.H * p.Nq;
+  const int t = there ? (int)(q_row % p.Nq) : 0, h = there ? (int)(q_row / p.Nq % p.H) : 0, b = there ? (int)(q_row / p.Nq / p.H) : 0;
+  const Parts parts = parts_of(p, b, h / p.G, t, h % p.G);
+  const int n = parts.pre + parts.own;
+  const bool mine = there && t < q_len_of(p, b) && n > 1;      // (a part alone has been written as it is)
   float m = -FLT_MAX, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  constexpr int U = 4;
-  for (int i0 = 0; i0 < n; i0 += U) {
+  for (int i0 = way; mine && i0 < n; i0 += U * WAYS) {
     float ls[U];
     f32x4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t row = at(min(i0 + u, n - 1));
-      ls[u] = i0 + u < n ? p.part_lse[row] : -INFINITY;
+      const int i = i0 + u * WAYS;
+      const int64_t row = parts.row(min(i, n - 1));
+      ls[u] = i < n ? p.part_lse[row] : -INFINITY;
       v[u] = *reinterpret_cast<const f32x4*>(p.part_o + row * D + x);
     }
     float to = m;
@@ -398,12 +420,35 @@ __global__ __launch_bounds__(256) void dbsp_cache_merge_kernel(const dbsp_cache_
     acc *= f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + u >= n) break;
+      if (i0 + u * WAYS >= n) break;
       const float wgt = __builtin_amdgcn_exp2f(ls[u] - m);
       sum += wgt;
       acc += wgt * v[u];                   // (a part without a key has zeros)
     }
   }
+  if constexpr (WAYS > 1) {
+    static_assert(ROWS == 1, "a row a workgroup");
+    __shared__ f32x4 accs[WAYS][LANES];
+    __shared__ float ms[WAYS], sums[WAYS];
+    accs[way][threadIdx.x % LANES] = acc;
+    if (x == 0) {
+      ms[way] = m;
+      sums[way] = sum;
+    }
+    __syncthreads();
+    if (way != 0) return;
+#pragma unroll
+    for (int y = 1; y < WAYS; ++y) m = fmaxf(m, ms[y]);
+    sum = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int y = 0; y < WAYS; ++y) {
+      const float f = __builtin_amdgcn_exp2f(ms[y] - m);
+      sum += f * sums[y];
+      acc += f * accs[y][threadIdx.x % LANES];
+    }
+  }
+  if (!mine) return;
   const bool none = __builtin_bit_cast(uint32_t, sum) == 0u;
   acc *= none ? 0.f : 1.f / sum;
   *reinterpret_cast<u32x2*>(p.o + b * p.o_sb + h * p.o_sh + t * p.o_st + x) = u32x2{T::pack(acc.x, acc.y), T::pack(acc.z, acc.w)};
@@ -412,6 +457,65 @@ __global__ __launch_bounds__(256) void dbsp_cache_merge_kernel(const dbsp_cache_
     if (p.lse) p.lse[q_row] = lse2 * 0.69314718055994531f;
     if (p.weights) p.row_lse[q_row] = lse2;
   }
+}
+
+constexpr int kSlots = 1024;       // a workgroup's, four a thread
+
+__device__ __forceinline__ void sum_scores(const dbsp_cache_attn_params& p, int group) {
+  __shared__ float row_lse[kScoreRows];
+  const int per_pair = (p.cap + kSlots - 1) / kSlots, pair = group / per_pair, slot0 = group % per_pair * kSlots;
+  const int b = pair / p.Hk, hk = pair % p.Hk, len = len_of(p, b), tid = threadIdx.x, w = tid >> 6, l = tid & 63;
+  if (slot0 >= len) return;
+  const int rows = q_len_of(p, b) * p.G, slot = slot0 + 4 * tid;
+  float* to = p.weights + (int64_t)pair * p.cap + slot;
+  f32x4 old;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) old[i] = p.decay != 0.f && slot + i < len ? p.decay * to[i] : 0.f;
+  // LSE of the group's rows, from their parts: a wave a row
+  for (int r = w; r < rows; r += 4) {
+    const int t = r / p.G, g = r % p.G;
+    float ls = 0.f;
+    if (p.split) {
+      const Parts parts = parts_of(p, b, hk, t, g);
+      const int n = parts.pre + parts.own;
+      float m = -FLT_MAX, sum = 0.f;
+      for (int i = l; i < n; i += 64) {
+        const float x = p.part_lse[parts.row(i)], up = fmaxf(m, x);
+        sum = sum * __builtin_amdgcn_exp2f(m - up) + __builtin_amdgcn_exp2f(x - up);
+        m = up;
+      }
+      float top = m;
+#pragma unroll
+      for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+      sum *= __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+      for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
+      ls = __builtin_bit_cast(uint32_t, sum) == 0u ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+      if (n == 1) ls = p.row_lse[((int64_t)b * p.H + hk * p.G + g) * p.Nq + t];
+    } else {
+      ls = p.row_lse[((int64_t)b * p.H + hk * p.G + g) * p.Nq + t];
+    }
+    if (__builtin_bit_cast(uint32_t, ls) == 0xff800000u) ls = INFINITY;      // a row without a key: probabilities of 0
+    if (l == 0) row_lse[r] = ls;
+  }
+  __syncthreads();
+  if (slot >= len) return;
+  const float* s = p.scores + (int64_t)pair * p.own_rows * p.score_pitch + slot;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < rows; ++r, s += p.score_pitch) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], p.scale_log2, -row_lse[r]));
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (slot + i < len) to[i] = old[i] + acc[i];
+}
+
+template <class T, int D, int WAYS>
+__global__ __launch_bounds__(256) void dbsp_cache_finish_kernel(const dbsp_cache_attn_params p) {
+  if ((int)blockIdx.x < p.merge_groups) merge_rows<T, D, WAYS>(p);
+  else sum_scores(p, blockIdx.x - p.merge_groups);
 }
 
 // The own keys' weights: a workgroup has 128 keys of a (sequence, KV head), 32 a wave with K as an operand in registers, and
@@ -494,15 +598,21 @@ __global__ __launch_bounds__(256) void dbsp_cache_weights_kernel(const dbsp_cach
 }
 
 template <class T, int D>
-hipError_t launch(const dbsp_cache_attn_params& p, int grid, hipStream_t stream) {
+hipError_t launch(dbsp_cache_attn_params p, int grid, hipStream_t stream) {
   dbsp_cache_attn_kernel<T, D><<<grid, 256, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
-  if (e == hipSuccess && p.split) {
-    constexpr int ROWS = 256 / (D / 4);
-    dbsp_cache_merge_kernel<T, D><<<(unsigned)(((int64_t)p.B * p.H * p.Nq + ROWS - 1) / ROWS), 256, 0, stream>>>(p);
+  if (e != hipSuccess) return e;
+  constexpr int UNITS = 256 / (D / 4);
+  const int64_t rows = (int64_t)p.B * p.H * p.Nq, sums = p.scores ? (int64_t)p.B * p.Hk * ((p.cap + kSlots - 1) / kSlots) : 0;
+  const bool all_ways = rows <= kMergeRows;
+  p.merge_groups = !p.split ? 0 : (int)(all_ways ? rows : (rows + UNITS - 1) / UNITS);
+  if (p.merge_groups + sums > 0) {
+    const unsigned groups = (unsigned)(p.merge_groups + sums);
+    if (all_ways) dbsp_cache_finish_kernel<T, D, UNITS><<<groups, 256, 0, stream>>>(p);
+    else dbsp_cache_finish_kernel<T, D, 1><<<groups, 256, 0, stream>>>(p);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && p.weights && p.cap > 0) {
+  if (e == hipSuccess && p.weights && !p.scores) {
     dbsp_cache_weights_kernel<T, D><<<dim3(p.B * p.Hk, (p.cap + 127) / 128), 256, 0, stream>>>(p);
     e = hipGetLastError();
   }

@@ -10,6 +10,9 @@ constexpr int kCacheRows = 128;        // queries of a workgroup: four waves of 
 constexpr int kCacheKeys = 64;         // keys of a tile
 constexpr int kCacheTarget = 1024;     // items that a launch is cut into where there is enough to cut, see cache_attn.hip
 
+constexpr int kCacheWhole = 4;         // tiles that are not cut, and prefixes that are not read for the whole batch at once
+constexpr int kScoreRows = 16;         // rows of a (sequence, KV head) up to which scores are kept for the weights, at d = 128
+constexpr int kMergeRows = 4096;       // rows up to which a workgroup joins the parts of one
 constexpr int kEvictWhole = 32768;     // slots that a workgroup chooses among by itself, and those of a part where there are more
 constexpr int kEvictPart = 8192;
 
@@ -37,6 +40,9 @@ struct dbsp_cache_attn_params {
   float* row_lse;                      // f32 [B,H,Nq]: log2 of the sum of exp, for the weights
   float* part_o;                       // f32 [items][rows][D], prefix items first
   float* part_lse;                     // f32 [items][rows], base 2
+  float* scores;                       // f32 [B,Hk][own_rows][score_pitch] q.k of the own keys (-inf where not seen), or null
+  int64_t score_pitch;
+  int32_t merge_groups;                // set by dbsp_launch_cache_attn
 };
 
 struct dbsp_cache_evict_params {
