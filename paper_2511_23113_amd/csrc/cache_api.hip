@@ -88,8 +88,9 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   p.pre_tiles = (p.P + kCacheKeys - 1) / kCacheKeys;
   p.pooled = p.pre_tiles > kCacheWhole && p.B > 1 && rows < kCacheRows;
   p.pre_row_tiles = p.pooled ? (int32_t)((all_rows + kCacheRows - 1) / kCacheRows) : 0;
-  p.own_row_tiles = (int32_t)((rows + kCacheRows - 1) / kCacheRows);
-  p.own_rows = (int32_t)std::min<int64_t>(rows, kCacheRows);
+  p.own_tile_rows = rows > kCacheRows ? kLongRows : kCacheRows;
+  p.own_row_tiles = (int32_t)((rows + p.own_tile_rows - 1) / p.own_tile_rows);
+  p.own_rows = (int32_t)std::min<int64_t>(rows, p.own_tile_rows);
   const int64_t unit = (int64_t)p.Hk * p.own_row_tiles, pre_unit = (int64_t)p.Hk * p.pre_row_tiles, row_tiles = unit * p.B;
   const int64_t most_tiles = (p.pooled ? 0 : p.pre_tiles) + (p.cap + kCacheKeys - 1) / kCacheKeys;
   p.split = p.pooled || (row_tiles < kCacheTarget && most_tiles > kCacheWhole);

@@ -1,0 +1,201 @@
+// What the kernels of attention over a key/value cache share: types, the layout of tiles in the LDS, copies, and which item a workgroup has.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cfloat>
+#include <climits>
+#include <cstdint>
+
+#include "attn_common.hpp"
+#include "cache_params.hpp"
+
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+struct Bf16 {
+  static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16x2(a, b); }
+};
+struct Fp16 {
+  static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    f32x2 f = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2));      // round to nearest even
+  }
+};
+
+// Of a d-wide K or V tile in the LDS: rows unpadded, 16-byte chunks XOR-swizzled inside each row (K by the row, so that the
+// operand reads of 16 consecutive keys hit distinct banks; V by (row & 3), for the 4 keys of a transposing read).
+template <int D>
+struct Lay {
+  static constexpr int DT = D / 32, KS = D / 16, NCH = D / 8, RPL = 128 / D, ROWB = 2 * D;
+  static constexpr int TILE = kCacheKeys * ROWB;       // bytes of a K (or V) tile
+  static constexpr int RPC = 64 / NCH;                 // rows that one copy instruction of a wave moves
+  static constexpr int COPIES = 16 / RPC;              // a wave copies 16 rows of K and 16 of V
+  static __device__ __forceinline__ int k_swz(int row) { return (row / RPL) % NCH; }
+  static __device__ __forceinline__ int v_swz(int row) { return ((row / RPL) % (NCH / 4)) << 2; }
+};
+
+// 16 bytes a lane from base + voff to the LDS at dst + 16 * lane.  Its own wait counts: see wait_all.
+__device__ __forceinline__ void copy_row16(const unsigned char* base, uint32_t voff, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(dst) : "memory");
+}
+__device__ __forceinline__ void wait_all() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ int len_of(const dbsp_cache_attn_params& p, int b) { return p.lens ? max(0, min(p.lens[b], p.cap)) : 0; }
+__device__ __forceinline__ int q_len_of(const dbsp_cache_attn_params& p, int b) { return p.q_lens ? max(0, min(p.q_lens[b], p.Nq)) : p.Nq; }
+__device__ __forceinline__ int tiles_of(int keys) { return (int)(((unsigned)keys + kCacheKeys - 1) / kCacheKeys); }
+// key tiles of sequence b's row tiles (the last one's, where causality leaves the others fewer)
+__device__ __forceinline__ int own_tiles(const dbsp_cache_attn_params& p, int b) {
+  return (p.pooled ? 0 : p.pre_tiles) + tiles_of(len_of(p, b));
+}
+
+struct Item {
+  int b;                 // sequence, -1: an item of the pooled prefix
+  int hk, rt;            // KV head, row tile
+  int c, n;              // part c of n
+  int64_t slot;          // of its partial result
+};
+
+// Which item this workgroup has; false: none.  All of the workgroup's threads call it.
+template <int NT>
+__device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item& it) {
+  constexpr int WAVES = NT / 64;
+  const int t = threadIdx.x, w = t >> 6, l = t & 63;
+  const int unit = p.Hk * p.own_row_tiles;
+  if (!p.split) {        // a row tile an item
+    const int n = p.B * unit, per = (n + 7) / 8, x = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || x >= n) return false;
+    it.b = x / unit;
+    it.hk = x % unit / p.own_row_tiles;
+    it.rt = p.own_row_tiles - 1 - x % p.own_row_tiles;      // the longest first
+    it.c = 0;
+    it.n = 1;
+    it.slot = -1;
+    return true;
+  }
+  __shared__ int64_t tile_sum[WAVES];
+  __shared__ int part_sum[WAVES], found[3];
+  const int per_thread = (p.B + NT - 1) / NT, b0 = min(t * per_thread, p.B), b1 = min(b0 + per_thread, p.B);
+  int64_t tiles = 0;
+  for (int b = b0; b < b1; ++b) tiles += own_tiles(p, b);
+  for (int s = 32; s > 0; s >>= 1) tiles += __shfl_xor(tiles, s);
+  if (l == 0) tile_sum[w] = tiles;
+  __syncthreads();
+  int64_t own = 0;
+  for (int i = 0; i < WAVES; ++i) own += tile_sum[i];
+  const int64_t total = own * unit + (p.pooled ? (int64_t)p.Hk * p.pre_row_tiles * p.pre_tiles : 0);
+  const int chunk = (int)max((int64_t)1, min((int64_t)(1 << 30), (total + kCacheTarget - 1) / kCacheTarget));
+  auto parts = [&](int n) { return max(1, (n + chunk - 1) / chunk); };
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) mine += parts(own_tiles(p, b));
+  int upto = mine;
+  for (int s = 1; s < 64; s <<= 1) {
+    const int o = __shfl_up(upto, s);
+    if (l >= s) upto += o;
+  }
+  if (l == 63) part_sum[w] = upto;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int i = 0; i < WAVES; ++i) {
+    if (i < w) before += part_sum[i];
+    all += part_sum[i];
+  }
+  const int pre_parts = p.pooled ? parts(p.pre_tiles) : 0, pre_items = p.Hk * p.pre_row_tiles * pre_parts;
+  int first = before + upto - mine;        // parts of the sequences before this thread's
+  if (blockIdx.x == 0) {                   // for the merge
+    if (t == 0) { p.table[0] = pre_parts; p.table[1] = pre_items; }
+    int f = first;
+    for (int b = b0; b < b1; ++b) {
+      const int n = parts(own_tiles(p, b));
+      p.table[2 + 2 * b] = f;
+      p.table[3 + 2 * b] = n;
+      f += n;
+    }
+  }
+  const int n_items = pre_items + unit * all, per = (n_items + 7) / 8, x = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || x >= n_items) return false;
+  if (x < pre_items) {
+    it.b = -1;
+    it.rt = x % p.pre_row_tiles;
+    it.c = x / p.pre_row_tiles % pre_parts;
+    it.hk = x / p.pre_row_tiles / pre_parts;
+    it.n = pre_parts;
+    it.slot = x;
+    return true;
+  }
+  const int y = x - pre_items, part = y / unit;      // parts before it, over all sequences
+  if (part >= first && part < first + mine) {
+    for (int b = b0; b < b1; ++b) {
+      const int n = parts(own_tiles(p, b));
+      if (part < first + n) {
+        found[0] = b;
+        found[1] = first;
+        found[2] = n;
+        break;
+      }
+      first += n;
+    }
+  }
+  __syncthreads();
+  const int z = y - found[1] * unit;
+  it.b = found[0];
+  it.n = found[2];
+  it.rt = p.own_row_tiles - 1 - z % p.own_row_tiles;
+  it.c = z / p.own_row_tiles % it.n;
+  it.hk = z / p.own_row_tiles / it.n;
+  // partial results lie by sequence, head, part and row tile as the merge counts them; one item alone needs none
+  it.slot = (it.n == 1 && !p.pooled) ? -1 : (int64_t)found[1] * unit + (it.hk * it.n + it.c) * p.own_row_tiles + it.rt;
+  return true;
+}
+
+// Where an own (or prefix) item's partial result begins, in rows.
+__device__ __forceinline__ int64_t part_row(const dbsp_cache_attn_params& p, bool own, int64_t slot) {
+  return own ? (int64_t)p.max_pre_items * kCacheRows + slot * p.own_rows : slot * kCacheRows;
+}
+
+// Row r of a row list: token, head of the group, sequence.
+struct Row { int b, t, g; };
+__device__ __forceinline__ Row row_of(const dbsp_cache_attn_params& p, int b, int r) {
+  const int tok = r / p.G, g = r % p.G;
+  if (b >= 0) return {b, tok, g};
+  return {tok / p.Nq, tok % p.Nq, g};
+}
+
+// The result of one row of an item: lanes (r, g) of its wave hold, of tile dt of the head dim, values 8 i + 4 g .. + 3 in o[dt][4 i ..].
+// Behind a division by the sum of its probabilities (inv) it goes to O, or, of a part, to the workspace.
+template <class T, int D>
+__device__ __forceinline__ void store_row(const dbsp_cache_attn_params& p, const Item& it, const f32x16 (&o)[D / 32], const Row& at, int h, int row_in_tile,
+                                          int g, float inv, float lse2) {
+  if (it.slot >= 0) {
+    const int64_t pr = part_row(p, it.b >= 0, it.slot) + row_in_tile;
+    float* to = p.part_o + pr * D + 4 * g;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(to + 32 * dt + 8 * i) = f32x4{o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv, o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv};
+    if (g == 0) p.part_lse[pr] = lse2;
+    return;
+  }
+  uint16_t* to = p.o + at.b * p.o_sb + h * p.o_sh + at.t * p.o_st + 4 * g;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<u32x2*>(to + 32 * dt + 8 * i) = u32x2{T::pack(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv), T::pack(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv)};
+  if (g == 0) {
+    const int64_t q_row = ((int64_t)at.b * p.H + h) * p.Nq + at.t;
+    if (p.lse) p.lse[q_row] = lse2 * 0.69314718055994531f;
+    if (p.weights) p.row_lse[q_row] = lse2;
+  }
+}
+
+}  // namespace

@@ -7,6 +7,7 @@
 #include <cstdint>
 
 constexpr int kCacheRows = 128;        // queries of a workgroup: four waves of 32
+constexpr int kLongWaves = 4, kLongRows = 64 * kLongWaves;      // those of cache_attn_long.hip: waves of 64
 constexpr int kCacheKeys = 64;         // keys of a tile
 constexpr int kCacheTarget = 1024;     // items that a launch is cut into where there is enough to cut, see cache_attn.hip
 
@@ -31,7 +32,8 @@ struct dbsp_cache_attn_params {
   int32_t split;                       // items may be parts of a row tile's keys: partial results, and a merge behind the kernel
   int32_t pre_tiles;                   // tiles of the prefix
   int32_t pre_row_tiles, own_row_tiles;            // row tiles of a KV head: of all sequences together (pooled), of one sequence
-  int32_t own_rows;                    // rows of an own item's partial result: min(kCacheRows, Nq * G)
+  int32_t own_tile_rows;               // rows of an own item: kCacheRows, or kLongRows for the kernel of cache_attn_long.hip
+  int32_t own_rows;                    // and of its partial result: not more than Nq * G
   int32_t max_pre_items;
   float scale_log2;                    // softmax scale * log2(e)
   float decay;
@@ -65,4 +67,5 @@ struct dbsp_cache_evict_params {
 };
 
 hipError_t dbsp_launch_cache_attn(const dbsp_cache_attn_params& p, int d, bool fp16, int grid, hipStream_t stream);
+hipError_t dbsp_launch_cache_attn_long(const dbsp_cache_attn_params& p, int d, bool fp16, int grid, hipStream_t stream);
 hipError_t dbsp_launch_cache_evict(const dbsp_cache_evict_params& p, hipStream_t stream);
