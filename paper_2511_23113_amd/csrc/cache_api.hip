@@ -74,6 +74,30 @@ struct Cut {             // how an attention call is laid out
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
+// Of a launch of n row tiles of `tiles` key tiles each on a chip that holds `slots` workgroups at a time: whole rounds of row tiles
+// as they are, and the last one or two cut into parts that fill their rounds.  What an item costs beside its tiles, in tiles:
+// kStart, and kPart more for a part (its partial result, and its share of the merge).
+constexpr double kStart = 2, kPart = 3;
+dbsp_cache_long_cut cut_long(int64_t n, int64_t tiles, int slots) {
+  const int dies = n < 64 ? 1 : 8;         // few row tiles: their parts go to all dies
+  const int64_t per = (n + dies - 1) / dies, room = slots / dies;
+  dbsp_cache_long_cut best = {(int32_t)n, dies, (int32_t)per, (int32_t)per, 0, 1};
+  double least = (double)((per + room - 1) / room) * (tiles + kStart);
+  for (int64_t whole = per / room * room; whole >= 0 && whole + 2 * room > per; whole -= room) {
+    const int64_t tail = per - whole;
+    for (int64_t k = 2; tail > 0 && 2 * k <= tiles && tail * k <= 6 * room; ++k) {
+      const double cost = (double)(whole / room) * (tiles + kStart) + (double)((tail * k + room - 1) / room) * ((tiles + k - 1) / k + kStart + kPart);
+      if (cost < least) {
+        least = cost;
+        best.whole = (int32_t)whole;
+        best.tail = (int32_t)tail;
+        best.k = (int32_t)k;
+      }
+    }
+  }
+  return best;
+}
+
 int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool with_weights, Cut& cut) {
   const int rc = check_cache(who, c);
   if (rc != DBSP_OK) return rc;
@@ -88,21 +112,25 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   p.pre_tiles = (p.P + kCacheKeys - 1) / kCacheKeys;
   p.pooled = p.pre_tiles > kCacheWhole && p.B > 1 && rows < kCacheRows;
   p.pre_row_tiles = p.pooled ? (int32_t)((all_rows + kCacheRows - 1) / kCacheRows) : 0;
-  p.own_tile_rows = rows > kCacheRows ? kLongRows : kCacheRows;
+  p.many = rows > kCacheRows;
+  p.own_tile_rows = p.many ? kLongRows : kCacheRows;
   p.own_row_tiles = (int32_t)((rows + p.own_tile_rows - 1) / p.own_tile_rows);
   p.own_rows = (int32_t)std::min<int64_t>(rows, p.own_tile_rows);
   const int64_t unit = (int64_t)p.Hk * p.own_row_tiles, pre_unit = (int64_t)p.Hk * p.pre_row_tiles, row_tiles = unit * p.B;
   const int64_t most_tiles = (p.pooled ? 0 : p.pre_tiles) + (p.cap + kCacheKeys - 1) / kCacheKeys;
-  p.split = p.pooled || (row_tiles < kCacheTarget && most_tiles > kCacheWhole);
+  if (row_tiles > kMost) return fail(who, DBSP_ESHAPE, "too many queries");
+  const bool many = p.many;
+  p.split = !many && (p.pooled || (row_tiles < kCacheTarget && most_tiles > kCacheWhole));
+  if (many) p.cut = cut_long(row_tiles, most_tiles, (c->d == 128 ? 1 : 2) * kLongSlots * 4 / kLongWaves);
   // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kCacheTarget of them
   const int64_t pre_items = std::min(pre_unit * p.pre_tiles, kCacheTarget + pre_unit);
-  const int64_t own_items = p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), kCacheTarget + row_tiles) : row_tiles;
-  cut.grid = round_up(p.split ? std::min(pre_items + own_items, kCacheTarget + pre_unit + row_tiles) : row_tiles, 8);
+  const int64_t own_items = many ? (int64_t)p.cut.dies * p.cut.tail * p.cut.k : p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), kCacheTarget + row_tiles) : row_tiles;
+  cut.grid = many ? (int64_t)p.cut.dies * (p.cut.whole + (int64_t)p.cut.tail * p.cut.k) : round_up(p.split ? std::min(pre_items + own_items, kCacheTarget + pre_unit + row_tiles) : row_tiles, 8);
   if (cut.grid > kMost || pre_items > kMost / kCacheRows) return fail(who, DBSP_ESHAPE, "too many queries");
   p.max_pre_items = p.pooled ? (int32_t)pre_items : 0;
   cut.row_lse_at = round_up((2 + 2 * (int64_t)p.B) * 4, 256);
   cut.part_o_at = cut.row_lse_at + (with_weights ? round_up(q_rows * 4, 256) : 0);
-  const int64_t part_rows = p.split ? p.max_pre_items * (int64_t)kCacheRows + own_items * p.own_rows : 0;
+  const int64_t part_rows = p.split || many ? p.max_pre_items * (int64_t)kCacheRows + own_items * p.own_rows : 0;
   cut.part_lse_at = cut.part_o_at + part_rows * c->d * 4;
   cut.scores_at = round_up(cut.part_lse_at + part_rows * 4, 256);
   const bool keep_scores = with_weights && p.cap > 0 && rows * 128 <= kScoreRows * c->d;

@@ -36,7 +36,7 @@ void dbsp_cache_attn_kernel(const dbsp_cache_attn_params p) {
   const uint32_t lds_base = (uint32_t)(uintptr_t)(LDS_PTR(unsigned char))lds;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, r = l & 31, g = l >> 5;
   Item it;
-  if (!find_item<256>(p, it)) return;
+  if (!find_item(p, it)) return;
   const int b = __builtin_amdgcn_readfirstlane(it.b), hk = __builtin_amdgcn_readfirstlane(it.hk), rt = __builtin_amdgcn_readfirstlane(it.rt);
   const bool own = b >= 0;
   const int len = own ? len_of(p, b) : 0, q_len = own ? q_len_of(p, b) : 0;
@@ -203,7 +203,7 @@ __device__ __forceinline__ Parts parts_of(const dbsp_cache_attn_params& p, int b
   x.own = p.table[3 + 2 * b];
   x.pre_row = part_row(p, false, (int64_t)hk * x.pre * p.pre_row_tiles + pre / kCacheRows) + pre % kCacheRows;
   x.pre_step = (int64_t)p.pre_row_tiles * kCacheRows;
-  x.own_row = part_row(p, true, ((int64_t)p.table[2 + 2 * b] * p.Hk + (int64_t)hk * x.own) * p.own_row_tiles + own / p.own_tile_rows) + own % p.own_tile_rows;
+  x.own_row = part_row(p, true, ((int64_t)p.table[2 + 2 * b] * p.Hk + (int64_t)hk * x.own) * p.own_row_tiles + own / kCacheRows) + own % kCacheRows;
   x.own_step = (int64_t)p.own_row_tiles * p.own_rows;
   return x;
 }
@@ -215,10 +215,28 @@ template <class T, int D, int WAYS>
 __device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
   constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, U = 4;
   const int unit = threadIdx.x / LANES, way = unit % WAYS, x = 4 * (threadIdx.x % LANES);
-  const int64_t q_row = (int64_t)blockIdx.x * ROWS + unit / WAYS;      // [b][h][t]
-  const bool there = q_row < (int64_t)p.B * p.H * p.Nq;
-  const int t = there ? (int)(q_row % p.Nq) : 0, h = there ? (int)(q_row / p.Nq % p.H) : 0, b = there ? (int)(q_row / p.Nq / p.H) : 0;
-  const Parts parts = parts_of(p, b, h / p.G, t, h % p.G);
+  const int64_t nth = (int64_t)blockIdx.x * ROWS + unit / WAYS;
+  Parts parts;
+  int b, h, t;
+  bool there;
+  if (p.many) {      // the rows of the tiles that were cut
+    const dbsp_cache_long_cut& cut = p.cut;
+    const int z = (int)(nth / p.own_rows), in = (int)(nth % p.own_rows), x = z / cut.tail * cut.per + cut.whole + z % cut.tail;
+    there = z < cut.dies * cut.tail && x < cut.items;
+    Item it;
+    row_tile(p, there ? x : 0, it);
+    const int row = it.rt * kLongRows + in;
+    b = it.b;
+    t = row / p.G;
+    h = it.hk * p.G + row % p.G;
+    parts = {0, cut.k, 0, 0, (int64_t)z * cut.k * p.own_rows + in, p.own_rows};
+  } else {
+    there = nth < (int64_t)p.B * p.H * p.Nq;      // [b][h][t]
+    t = there ? (int)(nth % p.Nq) : 0;
+    h = there ? (int)(nth / p.Nq % p.H) : 0;
+    b = there ? (int)(nth / p.Nq / p.H) : 0;
+    parts = parts_of(p, b, h / p.G, t, h % p.G);
+  }
   const int n = parts.pre + parts.own;
   const bool mine = there && t < q_len_of(p, b) && n > 1;      // (a part alone has been written as it is)
   float m = -FLT_MAX, sum = 0.f;
@@ -275,6 +293,7 @@ __device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
   acc *= none ? 0.f : 1.f / sum;
   *reinterpret_cast<u32x2*>(p.o + b * p.o_sb + h * p.o_sh + t * p.o_st + x) = u32x2{T::pack(acc.x, acc.y), T::pack(acc.z, acc.w)};
   if (x == 0) {
+    const int64_t q_row = ((int64_t)b * p.H + h) * p.Nq + t;
     const float lse2 = none ? -INFINITY : m + __builtin_amdgcn_logf(sum);
     if (p.lse) p.lse[q_row] = lse2 * 0.69314718055994531f;
     if (p.weights) p.row_lse[q_row] = lse2;
@@ -422,7 +441,7 @@ __global__ __launch_bounds__(256) void dbsp_cache_weights_kernel(const dbsp_cach
 template <class T, int D>
 hipError_t launch(dbsp_cache_attn_params p, int grid, hipStream_t stream) {
   hipError_t e;
-  if (p.own_tile_rows == kLongRows) {
+  if (p.many) {
     e = dbsp_launch_cache_attn_long(p, D, std::is_same_v<T, Fp16>, grid, stream);
   } else {
     dbsp_cache_attn_kernel<T, D><<<grid, 256, 0, stream>>>(p);
@@ -430,9 +449,11 @@ hipError_t launch(dbsp_cache_attn_params p, int grid, hipStream_t stream) {
   }
   if (e != hipSuccess) return e;
   constexpr int UNITS = 256 / (D / 4);
-  const int64_t rows = (int64_t)p.B * p.H * p.Nq, sums = p.scores ? (int64_t)p.B * p.Hk * ((p.cap + kSlots - 1) / kSlots) : 0;
+  const bool cut_long = p.many && p.cut.k > 1;
+  const int64_t rows = cut_long ? (int64_t)p.cut.dies * p.cut.tail * p.own_rows : (int64_t)p.B * p.H * p.Nq;
+  const int64_t sums = p.scores ? (int64_t)p.B * p.Hk * ((p.cap + kSlots - 1) / kSlots) : 0;
   const bool all_ways = rows <= kMergeRows;
-  p.merge_groups = !p.split ? 0 : (int)(all_ways ? rows : (rows + UNITS - 1) / UNITS);
+  p.merge_groups = !p.split && !cut_long ? 0 : (int)(all_ways ? rows : (rows + UNITS - 1) / UNITS);
   if (p.merge_groups + sums > 0) {
     const unsigned groups = (unsigned)(p.merge_groups + sums);
     if (all_ways) dbsp_cache_finish_kernel<T, D, UNITS><<<groups, 256, 0, stream>>>(p);

@@ -64,18 +64,22 @@ struct Item {
   int64_t slot;          // of its partial result
 };
 
+// Row tile x of all, sequence by sequence and head by head, the last rows first: causal ones are the longest there.
+__device__ __forceinline__ void row_tile(const dbsp_cache_attn_params& p, int x, Item& it) {
+  it.rt = p.own_row_tiles - 1 - x % p.own_row_tiles;
+  it.hk = x / p.own_row_tiles % p.Hk;
+  it.b = x / p.own_row_tiles / p.Hk;
+}
+
 // Which item this workgroup has; false: none.  All of the workgroup's threads call it.
-template <int NT>
 __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item& it) {
-  constexpr int WAVES = NT / 64;
+  constexpr int NT = 256, WAVES = NT / 64;
   const int t = threadIdx.x, w = t >> 6, l = t & 63;
   const int unit = p.Hk * p.own_row_tiles;
   if (!p.split) {        // a row tile an item
     const int n = p.B * unit, per = (n + 7) / 8, x = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || x >= n) return false;
-    it.b = x / unit;
-    it.hk = x % unit / p.own_row_tiles;
-    it.rt = p.own_row_tiles - 1 - x % p.own_row_tiles;      // the longest first
+    row_tile(p, x, it);
     it.c = 0;
     it.n = 1;
     it.slot = -1;
@@ -153,6 +157,18 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
   it.hk = z / p.own_row_tiles / it.n;
   // partial results lie by sequence, head, part and row tile as the merge counts them; one item alone needs none
   it.slot = (it.n == 1 && !p.pooled) ? -1 : (int64_t)found[1] * unit + (it.hk * it.n + it.c) * p.own_row_tiles + it.rt;
+  return true;
+}
+
+// The same for the kernel for many queries.  Parts at the same place of their tiles' keys lie next to each other.
+__device__ __forceinline__ bool find_long_item(const dbsp_cache_attn_params& p, Item& it) {
+  const dbsp_cache_long_cut& cut = p.cut;
+  const int die = blockIdx.x % cut.dies, y = blockIdx.x / cut.dies, z = y - cut.whole, x = z < 0 ? y : cut.whole + z % cut.tail;
+  if (die * cut.per + x >= cut.items) return false;
+  row_tile(p, die * cut.per + x, it);
+  it.n = z < 0 ? 1 : cut.k;
+  it.c = z < 0 ? 0 : z / cut.tail;
+  it.slot = it.n == 1 ? -1 : ((int64_t)die * cut.tail + x - cut.whole) * cut.k + it.c;
   return true;
 }
 

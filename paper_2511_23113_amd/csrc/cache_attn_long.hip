@@ -37,7 +37,7 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
   const uint32_t lds_base = (uint32_t)(uintptr_t)(LDS_PTR(unsigned char))lds;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, r = l & 31, g = l >> 5;
   Item it;
-  if (!find_item<64 * NW>(p, it)) return;
+  if (!find_long_item(p, it)) return;
   const int b = __builtin_amdgcn_readfirstlane(it.b), hk = __builtin_amdgcn_readfirstlane(it.hk), rt = __builtin_amdgcn_readfirstlane(it.rt);
   const int len = len_of(p, b), q_len = q_len_of(p, b), row0 = rt * ROWS;
   if (row0 / p.G >= q_len) return;         // no query here: its rows stay as they are

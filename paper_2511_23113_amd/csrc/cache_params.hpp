@@ -8,6 +8,7 @@
 
 constexpr int kCacheRows = 128;        // queries of a workgroup: four waves of 32
 constexpr int kLongWaves = 4, kLongRows = 64 * kLongWaves;      // those of cache_attn_long.hip: waves of 64
+constexpr int kLongSlots = 256;       // of them at a time at d = 128: a compute unit each; at d = 64 twice as many
 constexpr int kCacheKeys = 64;         // keys of a tile
 constexpr int kCacheTarget = 1024;     // items that a launch is cut into where there is enough to cut, see cache_attn.hip
 
@@ -16,6 +17,12 @@ constexpr int kScoreRows = 16;         // rows of a (sequence, KV head) up to wh
 constexpr int kMergeRows = 4096;       // rows up to which a workgroup joins the parts of one
 constexpr int kEvictWhole = 32768;     // slots that a workgroup chooses among by itself, and those of a part where there are more
 constexpr int kEvictPart = 8192;
+
+// How a launch of the kernel for many queries is cut: its row tiles, `per` for each of `dies` dies (workgroup number mod 8), of which
+// the first `whole` are one item each and the `tail` others `k` parts, so that the last round of workgroups ends together.
+struct dbsp_cache_long_cut {
+  int32_t items, dies, per, whole, tail, k;
+};
 
 struct dbsp_cache_attn_params {
   const uint16_t *q, *pk, *pv, *k, *v;
@@ -28,13 +35,15 @@ struct dbsp_cache_attn_params {
   int32_t pk_st, pv_st, k_st, v_st;                // token strides in bytes
   int32_t B, H, Hk, G, Nq, P, cap;
   int32_t causal;
+  int32_t many;                        // the kernel of cache_attn_long.hip
   int32_t pooled;                      // the prefix is read by the rows of all sequences together, own keys apart
-  int32_t split;                       // items may be parts of a row tile's keys: partial results, and a merge behind the kernel
+  int32_t split;                       // items may be parts of a row tile's keys: partial results, and a merge behind the kernel (kernel for few queries)
   int32_t pre_tiles;                   // tiles of the prefix
   int32_t pre_row_tiles, own_row_tiles;            // row tiles of a KV head: of all sequences together (pooled), of one sequence
   int32_t own_tile_rows;               // rows of an own item: kCacheRows, or kLongRows for the kernel of cache_attn_long.hip
   int32_t own_rows;                    // and of its partial result: not more than Nq * G
   int32_t max_pre_items;
+  dbsp_cache_long_cut cut;             // with `many` only
   float scale_log2;                    // softmax scale * log2(e)
   float decay;
   // workspace
