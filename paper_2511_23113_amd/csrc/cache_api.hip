@@ -69,7 +69,7 @@ int check_cache(const char* who, const dbsp_cache* c) {
 
 struct Cut {             // how an attention call is laid out
   dbsp_cache_attn_params p;
-  int64_t grid, row_lse_at, part_o_at, part_lse_at, scores_at, bytes;
+  int64_t grid, row_lse_at, part_o_at, part_lse_at, scores_at, part_w_at, bytes;
 };
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -135,7 +135,11 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   cut.scores_at = round_up(cut.part_lse_at + part_rows * 4, 256);
   const bool keep_scores = with_weights && p.cap > 0 && rows * 128 <= kScoreRows * c->d;
   p.score_pitch = keep_scores ? round_up(p.cap, kCacheKeys) : 0;
-  cut.bytes = round_up(cut.scores_at + (int64_t)p.B * p.Hk * rows * p.score_pitch * 4, 256);
+  cut.part_w_at = round_up(cut.scores_at + (int64_t)p.B * p.Hk * rows * p.score_pitch * 4, 256);
+  // rows are cut, down to 512 a part, until there are workgroups for two rounds of the chip
+  const int64_t groups = (int64_t)p.B * p.Hk * ((p.cap + kWeightKeys - 1) / kWeightKeys);
+  p.row_parts = with_weights && p.cap > 0 && !keep_scores ? (int32_t)std::clamp<int64_t>(std::min(4 * kLongSlots / groups, rows / 512), 1, 64) : 1;
+  cut.bytes = round_up(cut.part_w_at + (p.row_parts > 1 ? (int64_t)p.row_parts * p.B * p.Hk * p.cap * 4 : 0), 256);
   return DBSP_OK;
 }
 
@@ -215,6 +219,7 @@ int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch,
   p.part_o = reinterpret_cast<float*>(ws + cut.part_o_at);
   p.part_lse = reinterpret_cast<float*>(ws + cut.part_lse_at);
   p.scores = p.score_pitch > 0 ? reinterpret_cast<float*>(ws + cut.scores_at) : nullptr;
+  p.part_w = reinterpret_cast<float*>(ws + cut.part_w_at);
   return done(who, dbsp_launch_cache_attn(p, cache->d, cache->dtype == DBSP_FP16, (int)cut.grid, static_cast<hipStream_t>(stream)));
 }
 

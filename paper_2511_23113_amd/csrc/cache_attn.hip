@@ -359,85 +359,6 @@ __global__ __launch_bounds__(256) void dbsp_cache_finish_kernel(const dbsp_cache
   else sum_scores(p, blockIdx.x - p.merge_groups);
 }
 
-// The own keys' weights: a workgroup has 128 keys of a (sequence, KV head), 32 a wave with K as an operand in registers, and
-// goes over the sequence's rows, 64 at a time by way of the LDS.
-template <class T, int D>
-__global__ __launch_bounds__(256) void dbsp_cache_weights_kernel(const dbsp_cache_attn_params p) {
-  using L = Lay<D>;
-  constexpr int RT = 64, PER = RT * L::NCH / 256;      // 16-byte chunks of a row tile that a thread moves
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[RT * L::ROWB];
-  __shared__ float row_lse[RT];
-  __shared__ int row_limit[RT];
-  const uint32_t lds_base = (uint32_t)(uintptr_t)(LDS_PTR(unsigned char))lds;
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, r = l & 31, g = l >> 5;
-  const int b = blockIdx.x / p.Hk, hk = blockIdx.x % p.Hk;
-  const int len = len_of(p, b), q_len = q_len_of(p, b), key0 = blockIdx.y * 128;
-  if (key0 >= len) return;
-  const int rows = q_len * p.G;
-  // causal: the first query that sees key0
-  const int base = len - q_len + 1, t_first = p.causal ? max(0, key0 + 1 - base) : 0;
-  const int mykey0 = key0 + 32 * w;
-  u32x4 k[L::KS];
-  {
-    const unsigned char* src = reinterpret_cast<const unsigned char*>(p.k + b * p.k_sb + hk * p.k_sh) + (int64_t)min(mykey0 + r, len - 1) * p.k_st;
-#pragma unroll
-    for (int ks = 0; ks < L::KS; ++ks) k[ks] = *reinterpret_cast<const u32x4*>(src + 32 * ks + 16 * g);
-  }
-  float acc[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-  const float c = p.scale_log2;
-  for (int r0 = t_first * p.G / RT * RT; r0 < rows; r0 += RT) {
-    __syncthreads();
-#pragma unroll
-    for (int y = 0; y < PER; ++y) {
-      const int i = (y * 256 + tid) / L::NCH, ch = tid % L::NCH;
-      const Row at = row_of(p, b, r0 + i);
-      u32x4 v = {0u, 0u, 0u, 0u};          // (rows that are not there: no NaN may come of them)
-      if (r0 + i < rows) v = *reinterpret_cast<const u32x4*>(p.q + b * p.q_sb + (hk * p.G + at.g) * p.q_sh + at.t * p.q_st + 8 * ch);
-      *(LDS_PTR(u32x4))(uintptr_t)(lds_base + i * L::ROWB + ((ch ^ L::k_swz(i)) << 4)) = v;
-    }
-    if (tid < RT) {
-      const Row at = row_of(p, b, r0 + tid);
-      float ls = INFINITY;                 // a row without a key, or none: probabilities of 0
-      if (r0 + tid < rows) {
-        ls = p.row_lse[((int64_t)b * p.H + hk * p.G + at.g) * p.Nq + at.t];
-        if (__builtin_bit_cast(uint32_t, ls) == 0xff800000u) ls = INFINITY;
-      }
-      row_lse[tid] = ls;
-      row_limit[tid] = p.causal ? base + at.t : len;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < RT / 32; ++u) {
-      f32x16 s;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < L::KS; ++ks)
-        s = T::mfma(k[ks], *(LDS_PTR(u32x4))(uintptr_t)(lds_base + (32 * u + r) * L::ROWB + (((2 * ks + g) ^ L::k_swz(r)) << 4)), s);
-      const float ls = row_lse[32 * u + r];
-      const int left = row_limit[32 * u + r] - mykey0 - 4 * g;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -ls));
-        acc[e] += 8 * (e / 4) + e % 4 < left ? x : 0.f;
-      }
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 16; ++e)
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) acc[e] += __shfl_xor(acc[e], s);
-  float* to = p.weights + (int64_t)blockIdx.x * p.cap;
-  // lane e of each half stores its key e
-  float mine = 0.f;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) mine = r == e ? acc[e] : mine;
-  const int key = mykey0 + 8 * (r / 4) + 4 * g + r % 4;
-  if (r < 16 && key < len) to[key] = (p.decay == 0.f ? 0.f : p.decay * to[key]) + mine;
-}
-
 template <class T, int D>
 hipError_t launch(dbsp_cache_attn_params p, int grid, hipStream_t stream) {
   hipError_t e;
@@ -460,10 +381,7 @@ hipError_t launch(dbsp_cache_attn_params p, int grid, hipStream_t stream) {
     else dbsp_cache_finish_kernel<T, D, 1><<<groups, 256, 0, stream>>>(p);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && p.weights && !p.scores) {
-    dbsp_cache_weights_kernel<T, D><<<dim3(p.B * p.Hk, (p.cap + 127) / 128), 256, 0, stream>>>(p);
-    e = hipGetLastError();
-  }
+  if (e == hipSuccess && p.weights && !p.scores) e = dbsp_launch_cache_weights(p, D, std::is_same_v<T, Fp16>, stream);
   return e;
 }
 

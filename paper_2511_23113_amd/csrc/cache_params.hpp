@@ -14,6 +14,7 @@ constexpr int kCacheTarget = 1024;     // items that a launch is cut into where 
 
 constexpr int kCacheWhole = 4;         // tiles that are not cut, and prefixes that are not read for the whole batch at once
 constexpr int kScoreRows = 16;         // rows of a (sequence, KV head) up to which scores are kept for the weights, at d = 128
+constexpr int kWeightKeys = 256;       // own keys of a workgroup that forms their scores anew
 constexpr int kMergeRows = 4096;       // rows up to which a workgroup joins the parts of one
 constexpr int kEvictWhole = 32768;     // slots that a workgroup chooses among by itself, and those of a part where there are more
 constexpr int kEvictPart = 8192;
@@ -53,6 +54,8 @@ struct dbsp_cache_attn_params {
   float* part_lse;                     // f32 [items][rows], base 2
   float* scores;                       // f32 [B,Hk][own_rows][score_pitch] q.k of the own keys (-inf where not seen), or null
   int64_t score_pitch;
+  int32_t row_parts;                   // parts into which the rows are cut for the weights of own keys, and f32 [row_parts][B,Hk,cap]
+  float* part_w;                       // for their sums where there are more than one
   int32_t merge_groups;                // set by dbsp_launch_cache_attn
 };
 
@@ -77,4 +80,5 @@ struct dbsp_cache_evict_params {
 
 hipError_t dbsp_launch_cache_attn(const dbsp_cache_attn_params& p, int d, bool fp16, int grid, hipStream_t stream);
 hipError_t dbsp_launch_cache_attn_long(const dbsp_cache_attn_params& p, int d, bool fp16, int grid, hipStream_t stream);
+hipError_t dbsp_launch_cache_weights(const dbsp_cache_attn_params& p, int d, bool fp16, hipStream_t stream);
 hipError_t dbsp_launch_cache_evict(const dbsp_cache_evict_params& p, hipStream_t stream);

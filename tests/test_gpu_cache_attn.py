@@ -122,6 +122,8 @@ CASES = {
     "prompt": (2, 2, 1, 150, 64, 0, 150, [150, 97], [150, 97], True, "bf16", 1.0),
     "prompt_no_prefix_fp16": (1, 3, 3, 257, 128, 0, 300, [257], None, True, "fp16", 0.0),
     "prompt_after_others": (1, 2, 1, 200, 128, 77, 600, [431], None, True, "bf16", 1.0),
+    "prompt_weights_in_parts": (1, 4, 2, 620, 64, 0, 700, [689], None, True, "bf16", 0.5),
+    "frame_weights_in_parts": (1, 3, 1, 500, 128, 30, 700, [601], [433], False, "fp16", 1.0),
     "many_sequences": (300, 2, 1, 1, 64, 40, 20, [i % 21 for i in range(300)], None, True, "bf16", 1.0),
     "long_prefix": (2, 4, 2, 1, 64, 5000, 100, [100, 57], None, True, "bf16", 1.0),
     "long_own": (1, 2, 1, 2, 128, 0, 7000, [6999], None, True, "fp16", 1.0),
