@@ -270,7 +270,7 @@ typedef struct dbsp_cache {
  *      weights[b, hk, j] = decay * weights[b, hk, j] + sum over the heads h of hk and t < q_lens[b] of exp(s - LSE)
  *      (0: what was there is not read; 1: the sum over all calls), in f32; weights from lens[b] on are left as they were.
  * workspace: device, 256-byte aligned, of at least the size that dbsp_cache_attn_workspace gives for the same cache, H, Nq and
- *      whether decay >= 0; written by the call, holds nothing between calls.  Calls under way at the same time need one each.
+ *      whether decay >= 0 (NULL where that is 0); written by the call, holds nothing between calls.  Calls under way at the same time need one each.
  * stream: a hipStream_t (NULL = default stream).  The call only enqueues kernels, under capture too; lens and q_lens are read on
  * the device, so that a graph's replays follow what they hold then.
  * Errors: DBSP_EINVAL, DBSP_ESHAPE (H is no multiple of Hk, sizes too large), DBSP_EHIP.

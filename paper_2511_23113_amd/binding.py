@@ -7,6 +7,7 @@ hipcc, and any failure to build or load raises -- there is no CPU fallback.
 
 from __future__ import annotations
 
+import copy
 import ctypes as C
 import os
 
@@ -342,6 +343,7 @@ class KVCache:
 
     def __init__(self, k=None, v=None, lens=None, prefix_k=None, prefix_v=None, weights=None, positions=None):
         torch = _torch_module()
+        load_library()
         some = k if k is not None else prefix_k
         if some is None or (k is None) != (v is None) or (prefix_k is None) != (prefix_v is None) or (k is None) != (lens is None):
             raise ValueError("a cache has k, v and lens, or prefix_k and prefix_v, or all of them")
@@ -375,38 +377,45 @@ class KVCache:
                 raise ValueError(f"{name} must be a contiguous {dtype} tensor of {'[B]' if name == 'lens' else '[B, Hk, capacity]'} on the cache's GPU")
             setattr(desc, name, x.data_ptr())
         self.k, self.v, self.lens, self.prefix_k, self.prefix_v, self.weights, self.positions = k, v, lens, prefix_k, prefix_v, weights, positions
-        self.B, self.Hk, self.d, self.capacity, self.n_prefix = desc.B, desc.Hk, d, desc.capacity, desc.n_prefix
-        self._desc, self._bytes = desc, {}
+        self.B, self.Hk, self.d, self.capacity, self.n_prefix = desc.B if k is not None else None, desc.Hk, d, desc.capacity, desc.n_prefix
+        self._desc, self._at, self._bytes, self._index = desc, C.byref(desc), {}, self.device.index
 
-    def _need(self, key, ask) -> int:
-        """Workspace bytes of a call, by its sizes."""
-        n = self._bytes.get(key)
-        if n is None:
-            out = C.c_int64()
-            _check(ask(C.byref(out)))
-            n = self._bytes[key] = out.value
-        return n
+    def _for(self, B):
+        """The same prefix for B sequences."""
+        other = copy.copy(self)
+        other._desc = CacheDesc.from_buffer_copy(self._desc)
+        other._desc.B = other.B = B
+        other._at, other._bytes = C.byref(other._desc), {}
+        return other
 
     def _on(self, stream):
         """The raw stream, and whether tensors made on torch's current one are used on another."""
         torch = _torch
-        if self.device.index != torch.cuda.current_device():
+        if self._index != torch._C._cuda_getDevice():
             raise ValueError("the cache lives on another device than the current one")
-        now = torch._C._cuda_getCurrentRawStream(self.device.index)
+        now = torch._C._cuda_getCurrentRawStream(self._index)
         if stream is None:
             return now, False
         raw = stream if isinstance(stream, int) else stream.cuda_stream
         return raw, raw != now
 
-    def _workspace(self, workspace, need, raw, elsewhere):
+    def _workspace(self, workspace, key, ask, raw, elsewhere):
+        """The caller's workspace, or one of the size that a call with these sizes (key) needs; its address and size."""
         torch = _torch
         if workspace is None:
+            need = self._bytes.get(key)
+            if need is None:
+                out = C.c_int64()
+                _check(ask(self._at, *key, C.byref(out)))
+                need = self._bytes[key] = out.value
+            if need == 0:
+                return None, None, 0
             workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
             if elsewhere:
                 workspace.record_stream(torch.cuda.ExternalStream(raw, device=self.device))
         elif workspace.dtype != torch.uint8 or workspace.device != self.device or not workspace.is_contiguous():
             raise ValueError("the workspace must be a contiguous uint8 tensor on the cache's GPU")
-        return workspace
+        return workspace, workspace.data_ptr(), workspace.numel()
 
 
 def cache_attn_fwd(cache: KVCache, q, q_lens=None, causal: bool = True, decay=None, o=None, lse=None, softmax_scale: float = 0.0,
@@ -417,19 +426,18 @@ def cache_attn_fwd(cache: KVCache, q, q_lens=None, causal: bool = True, decay=No
     weights hold, to which this call's attention is added.  Enqueues on `stream` (default: torch's current stream) and
     returns (o, lse)."""
     torch = _torch
-    if q.dim() != 4 or q.dtype != cache.dtype or q.device != cache.device or q.shape[-1] != cache.d or q.stride(-1) != 1:
+    shape, q_s = q.shape, q.stride()
+    if len(shape) != 4 or q.dtype != cache.dtype or q.device != cache.device or shape[3] != cache.d or q_s[3] != 1:
         raise ValueError("q must be [B, H, Nq, d] of the cache's type and head dim on its GPU, with a dense last dimension")
-    B, H, Nq, _ = q.shape
-    desc = cache._desc
-    if cache.k is None:
-        desc = CacheDesc.from_buffer_copy(desc)      # a prefix alone serves any number of sequences
-        desc.B = B
+    B, H, Nq, _ = shape
+    if cache.B is None:
+        cache = cache._for(B)                        # a prefix alone serves any number of sequences
     elif B != cache.B:
         raise ValueError("q and the cache differ in the number of sequences")
     raw, elsewhere = cache._on(stream)
     if o is None:
-        o = torch.empty((B, H, Nq, cache.d), dtype=q.dtype, device=q.device)
-    elif o.shape != q.shape or o.dtype != q.dtype or o.device != q.device or o.stride(-1) != 1:
+        o = torch.empty(shape, dtype=q.dtype, device=q.device)
+    elif o.shape != shape or o.dtype != q.dtype or o.device != q.device or o.stride(3) != 1:
         raise ValueError("o must be as q")
     if lse is None:
         if want_lse:
@@ -444,12 +452,11 @@ def cache_attn_fwd(cache: KVCache, q, q_lens=None, causal: bool = True, decay=No
         raise ValueError("decay must not be negative")
     elif cache.weights is None:
         raise ValueError("the cache has no weights")
-    lib, at = load_library(), C.byref(desc)
-    workspace = cache._workspace(workspace, cache._need((B, H, Nq, decay >= 0), lambda n: lib.dbsp_cache_attn_workspace(at, H, Nq, decay >= 0, n)), raw, elsewhere)
-    q_s, o_s = q.stride(), o.stride()
-    rc = lib.dbsp_cache_attn_fwd(at, q.data_ptr(), q_s[0], q_s[1], q_s[2], o.data_ptr(), o_s[0], o_s[1], o_s[2], None if lse is None else lse.data_ptr(),
-                                 None if q_lens is None else q_lens.data_ptr(), H, Nq, causal, softmax_scale, decay, workspace.data_ptr(),
-                                 workspace.numel(), raw)
+    lib = _lib
+    workspace, at, size = cache._workspace(workspace, (H, Nq, decay >= 0), lib.dbsp_cache_attn_workspace, raw, elsewhere)
+    o_s = o.stride()
+    rc = lib.dbsp_cache_attn_fwd(cache._at, q.data_ptr(), q_s[0], q_s[1], q_s[2], o.data_ptr(), o_s[0], o_s[1], o_s[2], None if lse is None else lse.data_ptr(),
+                                 None if q_lens is None else q_lens.data_ptr(), H, Nq, causal, softmax_scale, decay, at, size, raw)
     if rc:
         _check(rc)
     return o, lse
@@ -459,15 +466,14 @@ def cache_evict(cache: KVCache, budget: int, sinks: int = 0, keep_from=None, str
     """Cuts the sequences with more than `budget` used slots back to the `budget` keys of the largest weights, in place, each KV
     head by itself (see dbsp.h: dbsp_cache_evict).  Keys at positions below `sinks`, and from keep_from[b] on (int32 [B] on the
     GPU), rank above all others.  Updates k, v, weights, positions and lens; enqueues on `stream`."""
+    if cache.k is None:
+        raise ValueError("the cache has no keys of its own")
     torch = _torch
     raw, elsewhere = cache._on(stream)
     if keep_from is not None and (keep_from.shape != (cache.B,) or keep_from.dtype != torch.int32 or keep_from.device != cache.device or not keep_from.is_contiguous()):
         raise ValueError("keep_from must be a contiguous int32 tensor of [B] on the cache's GPU")
-    if cache.k is None:
-        raise ValueError("the cache has no keys of its own")
-    lib, at = load_library(), C.byref(cache._desc)
-    workspace = cache._workspace(workspace, cache._need(budget, lambda n: lib.dbsp_cache_evict_workspace(at, budget, n)), raw, elsewhere)
-    rc = lib.dbsp_cache_evict(at, budget, sinks, None if keep_from is None else keep_from.data_ptr(), workspace.data_ptr(), workspace.numel(), raw)
+    workspace, at, size = cache._workspace(workspace, (budget,), _lib.dbsp_cache_evict_workspace, raw, elsewhere)
+    rc = _lib.dbsp_cache_evict(cache._at, budget, sinks, None if keep_from is None else keep_from.data_ptr(), at, size, raw)
     if rc:
         _check(rc)
 

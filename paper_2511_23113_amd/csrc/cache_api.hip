@@ -140,6 +140,7 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   const int64_t groups = (int64_t)p.B * p.Hk * ((p.cap + kWeightKeys - 1) / kWeightKeys);
   p.row_parts = with_weights && p.cap > 0 && !keep_scores ? (int32_t)std::clamp<int64_t>(std::min(4 * kLongSlots / groups, rows / 512), 1, 64) : 1;
   cut.bytes = round_up(cut.part_w_at + (p.row_parts > 1 ? (int64_t)p.row_parts * p.B * p.Hk * p.cap * 4 : 0), 256);
+  if (!p.split && p.cut.k <= 1 && !with_weights) cut.bytes = 0;      // one launch, and nothing between workgroups
   return DBSP_OK;
 }
 
@@ -186,7 +187,7 @@ int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch,
   Cut cut;
   const int rc = lay_out(who, cache, H, Nq, with_weights, cut);
   if (rc != DBSP_OK) return rc;
-  if (!q || !o || !workspace) return fail(who, DBSP_EINVAL, "null pointer");
+  if (!q || !o || (!workspace && cut.bytes > 0)) return fail(who, DBSP_EINVAL, "null pointer");
   const int64_t size[3] = {cache->B, H, Nq}, q_stride[3] = {q_batch, q_head, q_token}, o_stride[3] = {o_batch, o_head, o_token};
   if (!strides_ok(q_stride, 3) || !strides_ok(o_stride, 3) || !aligned(q, 16) || !aligned(o, 16))
     return fail(who, DBSP_EINVAL, "q and o must be 16-byte aligned, their strides multiples of 8 and a token's at most 2^24");

@@ -28,6 +28,185 @@
 
 namespace {
 
+// Where an item's rows and keys are: sequence (-1: the pooled prefix), KV head, first row and rows of the sequence, used slots, new
+// tokens, tiles of the prefix in front of the own ones, and the item's tiles.
+struct Span { int b, hk, row0, rows, len, q_len, pre_tiles, t0, t1; };
+
+// Row tiles of at most 16 NR rows, the form for single tokens: bound by the stream of K and V.  The keys of a tile are dealt to the
+// waves, 16 each, with 16 x 16 MFMAs: lane (n, g) of 16 x 4 has row n and keys 4 g .. 4 g + 3, and the packed probabilities
+// are the second product's operand again.  A wave reads what it has copied itself, so no barrier couples the waves; each has
+// statistics of its own, against which it forms its probabilities as they stand (the max is raised where one passes 64), and
+// the four are joined through the LDS at the end.
+template <class T, int D, int NR>
+__device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const Item& it, const Span& s, unsigned char* lds) {
+  using L = Lay<D>;
+  constexpr int KS = D / 32, DT = D / 16, CH = D / 4;
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(LDS_PTR(unsigned char))lds;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 15, g = l >> 4;
+  const bool own = s.b >= 0;
+  const int base = s.len - s.q_len + 1;
+  int limit[NR], all_see = INT_MAX;
+  bool valid[NR];
+  u32x4 q[NR][KS];
+#pragma unroll
+  for (int y = 0; y < NR; ++y) {
+    const int row = s.row0 + 16 * y + n;
+    const Row at = row_of(p, s.b, min(row, s.rows - 1));
+    valid[y] = row < s.rows && at.t < (own ? s.q_len : q_len_of(p, at.b));
+    limit[y] = p.causal ? max(0, min(s.len, base + at.t)) : s.len;
+    all_see = min(all_see, valid[y] ? limit[y] : INT_MAX);
+    const uint16_t* src = p.q + at.b * p.q_sb + (s.hk * p.G + at.g) * p.q_sh + at.t * p.q_st;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q[y][ks] = *reinterpret_cast<const u32x4*>(src + 32 * ks + 8 * g);
+  }
+  for (int x = 8; x > 0; x >>= 1) all_see = min(all_see, __shfl_xor(all_see, x));
+  all_see = __builtin_amdgcn_readfirstlane(all_see);
+
+  const int row_in = l / L::NCH, pch = l % L::NCH;
+  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+    const bool pre = t < s.pre_tiles;
+    const int tok = (pre ? t : t - s.pre_tiles) * kCacheKeys, there = (pre ? p.P : s.len) - tok;
+    const uint32_t kst = pre ? p.pk_st : p.k_st, vst = pre ? p.pv_st : p.v_st;
+    const unsigned char* kb = reinterpret_cast<const unsigned char*>(pre ? p.pk + s.hk * p.pk_sh : p.k + s.b * p.k_sb + s.hk * p.k_sh) + (int64_t)tok * kst;
+    const unsigned char* vb = reinterpret_cast<const unsigned char*>(pre ? p.pv + s.hk * p.pv_sh : p.v + s.b * p.v_sb + s.hk * p.v_sh) + (int64_t)tok * vst;
+    const uint32_t dst = lds_base + buf * 2 * L::TILE + 16 * w * L::ROWB;
+#pragma unroll
+    for (int x = 0; x < L::COPIES; ++x) {
+      const int in = x * L::RPC + row_in, from = min(16 * w + in, there - 1);
+      copy_row16(kb, from * kst + ((pch ^ L::k_swz(in)) << 4), dst + x * 1024);
+      copy_row16(vb, from * vst + ((pch ^ L::v_swz(in)) << 4), dst + L::TILE + x * 1024);
+    }
+  };
+  // operand reads: K rows n with 16-byte chunk 4 ks + g; of V^T, lane 4 j + a of 16 has the address of four values of key j
+  const uint32_t mine = lds_base + 16 * w * L::ROWB;
+  uint32_t k_rd[KS], v_rd[DT];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) k_rd[ks] = mine + n * L::ROWB + (((4 * ks + g) ^ L::k_swz(n)) << 4);
+  {
+    const int key = 4 * g + (n >> 2), a4 = n & 3;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v_rd[dt] = mine + L::TILE + key * L::ROWB + (((2 * dt + (a4 >> 1)) ^ L::v_swz(key)) << 4) + (a4 & 1) * 8;
+  }
+  f32x4 o[NR][DT];
+  float mc[NR], sum[NR];
+#pragma unroll
+  for (int y = 0; y < NR; ++y) {
+    mc[y] = -FLT_MAX;
+    sum[y] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[y][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float c = p.scale_log2;
+  float* scores = p.scores && own ? p.scores + ((int64_t)s.b * p.Hk + s.hk) * p.own_rows * p.score_pitch : nullptr;
+
+  if (s.t0 < s.t1) copy_tile(s.t0, 0);
+  for (int t = s.t0; t < s.t1; ++t) {
+    const int buf = (t - s.t0) & 1;
+    if (t + 1 < s.t1) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // what was read there has arrived
+      copy_tile(t + 1, buf ^ 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * L::COPIES) : "memory");      // this tile has landed, the next one is under way
+    } else {
+      wait_all();
+    }
+    const uint32_t off = buf * 2 * L::TILE;
+    const bool pre = t < s.pre_tiles;
+    const int tok = (pre ? t : t - s.pre_tiles) * kCacheKeys, key = tok + 16 * w + 4 * g;
+    u32x4 kf[KS];
+    u32x2 vf[DT], pb[NR];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kf[ks] = *(LDS_PTR(u32x4))(uintptr_t)(k_rd[ks] + off);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) vf[dt] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(v_rd[dt] + off)));
+#pragma unroll
+    for (int y = 0; y < NR; ++y) {
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) x = T::mfma32(kf[ks], q[y][ks], x);
+      if (tok + kCacheKeys > (pre ? p.P : all_see)) {
+        const int left = (pre ? p.P : limit[y]) - key;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i >= left) x[i] = -INFINITY;
+      }
+      if (scores && !pre && valid[y]) *reinterpret_cast<f32x4*>(scores + (int64_t)(s.row0 + 16 * y + n) * p.score_pitch + key) = x;
+      float pr[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -mc[y]));
+      const float top4 = fmaxf(fmaxf(pr[0], pr[1]), fmaxf(pr[2], pr[3]));
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(top4 > 64.f) != 0, 0)) {
+        float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float to = fmaxf(mc[y], top * c), f = __builtin_amdgcn_exp2f(mc[y] - to);
+        mc[y] = to;
+        sum[y] *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[y][dt] *= f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -to));
+      }
+      sum[y] += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+      pb[y] = u32x2{T::pack(pr[0], pr[1]), T::pack(pr[2], pr[3])};
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int y = 0; y < NR; ++y) o[y][dt] = T::mfma16(vf[dt], pb[y], o[y][dt]);
+  }
+
+  // the waves' results: [wave][row][16-byte chunk of the head dim, by row swizzled]
+  __shared__ float mcs[4][16 * NR], sums[4][16 * NR];
+  __syncthreads();                         // everybody has read its last tile
+  f32x4* const os = reinterpret_cast<f32x4*>(lds);
+#pragma unroll
+  for (int y = 0; y < NR; ++y) {
+    sum[y] += __shfl_xor(sum[y], 16);
+    sum[y] += __shfl_xor(sum[y], 32);
+    if (g == 0) {
+      mcs[w][16 * y + n] = mc[y];
+      sums[w][16 * y + n] = sum[y];
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) os[(w * 16 * NR + 16 * y + n) * CH + ((4 * dt + g) ^ n)] = o[y][dt];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int z = 0; z < 16 * NR * CH / 256; ++z) {
+    const int i = z * 256 + threadIdx.x, in = i / CH, ch = i % CH, row = s.row0 + in;
+    if (row >= s.rows) continue;
+    const Row at = row_of(p, s.b, row);
+    if (at.t >= (own ? s.q_len : q_len_of(p, at.b))) continue;
+    float m = mcs[0][in];
+#pragma unroll
+    for (int x = 1; x < 4; ++x) m = fmaxf(m, mcs[x][in]);
+    float all = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float f = __builtin_amdgcn_exp2f(mcs[x][in] - m);
+      all += f * sums[x][in];
+      acc += f * os[(x * 16 * NR + in) * CH + (ch ^ (in & 15))];
+    }
+    const bool none = __builtin_bit_cast(uint32_t, all) == 0u;
+    acc *= none ? 0.f : 1.f / all;
+    const float lse2 = none ? -INFINITY : m + __builtin_amdgcn_logf(all);
+    const int h = s.hk * p.G + at.g;
+    if (it.slot >= 0) {
+      const int64_t pr = part_row(p, own, it.slot) + in;
+      *reinterpret_cast<f32x4*>(p.part_o + pr * D + 4 * ch) = acc;
+      if (ch == 0) p.part_lse[pr] = lse2;
+    } else {
+      *reinterpret_cast<u32x2*>(p.o + at.b * p.o_sb + h * p.o_sh + at.t * p.o_st + 4 * ch) = u32x2{T::pack(acc.x, acc.y), T::pack(acc.z, acc.w)};
+      if (ch == 0) {
+        const int64_t q_row = ((int64_t)at.b * p.H + h) * p.Nq + at.t;
+        if (p.lse) p.lse[q_row] = lse2 * 0.69314718055994531f;
+        if (p.weights) p.row_lse[q_row] = lse2;
+      }
+    }
+  }
+}
+
 template <class T, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 void dbsp_cache_attn_kernel(const dbsp_cache_attn_params p) {
@@ -52,6 +231,10 @@ void dbsp_cache_attn_kernel(const dbsp_cache_attn_params p) {
   const int n_all = own ? own_tiles(p, b) : p.pre_tiles, per = (n_all + it.n - 1) / it.n;
   const int n_here = pre_tiles + tiles_of(seen);
   const int t0 = __builtin_amdgcn_readfirstlane(min(it.c * per, n_here)), t1 = __builtin_amdgcn_readfirstlane(min((it.c + 1) * per, n_here));
+
+  const Span span{b, hk, row0, rows, len, q_len, pre_tiles, t0, t1};
+  if (min(rows - row0, kCacheRows) <= 16) return few_rows<T, D, 1>(p, it, span, lds);
+  if (min(rows - row0, kCacheRows) <= 32) return few_rows<T, D, 2>(p, it, span, lds);
 
   // this lane's query
   const int row = row0 + 32 * w + r;

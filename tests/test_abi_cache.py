@@ -101,9 +101,10 @@ def test_workspaces_grow_with_the_call_and_stay_moderate():
     def need(d, H, Nq, weights=0):
         assert lib.dbsp_cache_attn_workspace(C.byref(d), H, Nq, weights, C.byref(n)) == B.DBSP_OK
         return n.value
-    small = need(desc(), 4, 1)
-    assert 0 < small < 1 << 20 and small % 256 == 0
-    assert need(desc(), 4, 1, 1) > small
+    assert need(desc(), 4, 1) == 0         # one launch
+    small = need(desc(n_prefix=1000), 4, 1)
+    assert 0 < small < 1 << 22 and small % 256 == 0
+    assert need(desc(n_prefix=1000), 4, 1, 1) > small
     # of long prompts only the last rounds' row tiles are cut
     assert need(desc(B=4, Hk=40, capacity=9000), 40, 9000) < 1 << 28
     assert need(desc(n_prefix=1 << 20), 4, 1) < 1 << 30
