@@ -125,7 +125,9 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kCacheTarget of them
   const int64_t pre_items = std::min(pre_unit * p.pre_tiles, kCacheTarget + pre_unit);
   const int64_t own_items = many ? (int64_t)p.cut.dies * p.cut.tail * p.cut.k : p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), kCacheTarget + row_tiles) : row_tiles;
-  cut.grid = many ? (int64_t)p.cut.dies * (p.cut.whole + (int64_t)p.cut.tail * p.cut.k) : round_up(p.split ? std::min(pre_items + own_items, kCacheTarget + pre_unit + row_tiles) : row_tiles, 8);
+  if (many) cut.grid = (int64_t)p.cut.dies * (p.cut.whole + (int64_t)p.cut.tail * p.cut.k);
+  else if (p.split) cut.grid = round_up(std::min(pre_items + own_items, kCacheTarget + pre_unit + row_tiles), 8) + 16;      // (dies' shares of two lists, rounded up)
+  else cut.grid = round_up(row_tiles, 8);
   if (cut.grid > kMost || pre_items > kMost / kCacheRows) return fail(who, DBSP_ESHAPE, "too many queries");
   p.max_pre_items = p.pooled ? (int32_t)pre_items : 0;
   cut.row_lse_at = round_up((2 + 2 * (int64_t)p.B) * 4, 256);

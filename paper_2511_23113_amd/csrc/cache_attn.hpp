@@ -140,9 +140,14 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
       f += n;
     }
   }
-  const int n_items = pre_items + unit * all, per = (n_items + 7) / 8, x = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || x >= n_items) return false;
-  if (x < pre_items) {
+  // every die has its share of the prefix's items, then of the own ones: the first are bound by the matrix pipe where their rows are
+  // many, the others by memory, and neither is left to a few dies
+  const int die = blockIdx.x & 7, i = blockIdx.x >> 3;
+  auto share = [](int64_t n, int d) { return (int)(n * d / 8); };
+  const int own_items = unit * all, p0 = share(pre_items, die), np = share(pre_items, die + 1) - p0, o0 = share(own_items, die);
+  if (i >= np + share(own_items, die + 1) - o0) return false;
+  if (i < np) {
+    const int x = p0 + i;
     it.b = -1;
     it.rt = x % p.pre_row_tiles;
     it.c = x / p.pre_row_tiles % pre_parts;
@@ -151,7 +156,7 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
     it.slot = x;
     return true;
   }
-  const int y = x - pre_items, part = y / unit;      // parts before it, over all sequences
+  const int y = o0 + i - np, part = y / unit;      // parts before it, over all sequences
   if (part >= first && part < first + mine) {
     for (int b = b0; b < b1; ++b) {
       const int n = parts(own_tiles(p, b));
