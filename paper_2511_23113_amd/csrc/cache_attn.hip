@@ -396,7 +396,7 @@ __device__ __forceinline__ Parts parts_of(const dbsp_cache_attn_params& p, int b
 // weights from the scores that the attention kernel has kept, 1024 slots of a (sequence, KV head) each.
 template <class T, int D, int WAYS>
 __device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
-  constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, U = 4;
+  constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, U = WAYS > 1 ? 8 : 4;
   const int unit = threadIdx.x / LANES, way = unit % WAYS, x = 4 * (threadIdx.x % LANES);
   const int64_t nth = (int64_t)blockIdx.x * ROWS + unit / WAYS;
   Parts parts;
@@ -488,48 +488,56 @@ constexpr int kSlots = 1024;       // a workgroup's, four a thread
 __device__ __forceinline__ void sum_scores(const dbsp_cache_attn_params& p, int group) {
   __shared__ float row_lse[kScoreRows];
   const int per_pair = (p.cap + kSlots - 1) / kSlots, pair = group / per_pair, slot0 = group % per_pair * kSlots;
-  const int b = pair / p.Hk, hk = pair % p.Hk, len = len_of(p, b), tid = threadIdx.x, w = tid >> 6, l = tid & 63;
+  const int b = pair / p.Hk, hk = pair % p.Hk, len = len_of(p, b), tid = threadIdx.x;
   if (slot0 >= len) return;
   const int rows = q_len_of(p, b) * p.G, slot = slot0 + 4 * tid;
   float* to = p.weights + (int64_t)pair * p.cap + slot;
   f32x4 old;
 #pragma unroll
   for (int i = 0; i < 4; ++i) old[i] = p.decay != 0.f && slot + i < len ? p.decay * to[i] : 0.f;
-  // LSE of the group's rows, from their parts: a wave a row
-  for (int r = w; r < rows; r += 4) {
+  // LSE of the group's rows, from their parts: 16 lanes a row
+  const int lane = tid & 15;
+  for (int r = tid >> 4; r < rows; r += 16) {
     const int t = r / p.G, g = r % p.G;
     float ls = 0.f;
-    if (p.split) {
-      const Parts parts = parts_of(p, b, hk, t, g);
-      const int n = parts.pre + parts.own;
+    Parts parts{0, 1, 0, 0, 0, 0};
+    if (p.split) parts = parts_of(p, b, hk, t, g);
+    const int n = parts.pre + parts.own;
+    if (n > 1) {
       float m = -FLT_MAX, sum = 0.f;
-      for (int i = l; i < n; i += 64) {
+      for (int i = lane; i < n; i += 16) {
         const float x = p.part_lse[parts.row(i)], up = fmaxf(m, x);
         sum = sum * __builtin_amdgcn_exp2f(m - up) + __builtin_amdgcn_exp2f(x - up);
         m = up;
       }
       float top = m;
 #pragma unroll
-      for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+      for (int s = 8; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
       sum *= __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
-      for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
+      for (int s = 8; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
       ls = __builtin_bit_cast(uint32_t, sum) == 0u ? -INFINITY : top + __builtin_amdgcn_logf(sum);
-      if (n == 1) ls = p.row_lse[((int64_t)b * p.H + hk * p.G + g) * p.Nq + t];
     } else {
       ls = p.row_lse[((int64_t)b * p.H + hk * p.G + g) * p.Nq + t];
     }
     if (__builtin_bit_cast(uint32_t, ls) == 0xff800000u) ls = INFINITY;      // a row without a key: probabilities of 0
-    if (l == 0) row_lse[r] = ls;
+    if (lane == 0) row_lse[r] = ls;
   }
   __syncthreads();
   if (slot >= len) return;
   const float* s = p.scores + (int64_t)pair * p.own_rows * p.score_pitch + slot;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int r = 0; r < rows; ++r, s += p.score_pitch) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(s);
+  constexpr int U = 4;
+  for (int r = 0; r < rows; r += U, s += U * p.score_pitch) {
+    f32x4 x[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], p.scale_log2, -row_lse[r]));
+    for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const f32x4*>(s + (r + u < rows ? u : 0) * p.score_pitch);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float ls = r + u < rows ? row_lse[r + u] : INFINITY;      // (a row again: probabilities of 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][i], p.scale_log2, -ls));
+    }
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
