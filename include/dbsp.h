@@ -269,8 +269,8 @@ typedef struct dbsp_cache {
  * decay: below 0 leaves the cache's weights alone; else, for every own key in use,
  *      weights[b, hk, j] = decay * weights[b, hk, j] + sum over the heads h of hk and t < q_lens[b] of exp(s - LSE)
  *      (0: what was there is not read; 1: the sum over all calls), in f32; weights from lens[b] on are left as they were.
- * workspace: device, 256-byte aligned, of at least the size that dbsp_cache_attn_workspace gives for the same cache, H, Nq and
- *      whether decay >= 0 (NULL where that is 0); written by the call, holds nothing between calls.  Calls under way at the same time need one each.
+ * workspace: device, 256-byte aligned, of at least the size that dbsp_cache_attn_workspace gives for the same cache, H, Nq,
+ *      causal and whether decay >= 0 (NULL where that is 0); written by the call, holds nothing between calls.  Calls under way at the same time need one each.
  * stream: a hipStream_t (NULL = default stream).  The call only enqueues kernels, under capture too; lens and q_lens are read on
  * the device, so that a graph's replays follow what they hold then.
  * Errors: DBSP_EINVAL, DBSP_ESHAPE (H is no multiple of Hk, sizes too large), DBSP_EHIP.
@@ -278,7 +278,7 @@ typedef struct dbsp_cache {
 int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token, void* o,
                         int64_t o_batch, int64_t o_head, int64_t o_token, float* lse, const int32_t* q_lens, int32_t H, int32_t Nq,
                         int32_t causal, float softmax_scale, float decay, void* workspace, int64_t workspace_bytes, void* stream);
-int dbsp_cache_attn_workspace(const dbsp_cache* cache, int32_t H, int32_t Nq, int32_t with_weights, int64_t* bytes);
+int dbsp_cache_attn_workspace(const dbsp_cache* cache, int32_t H, int32_t Nq, int32_t causal, int32_t with_weights, int64_t* bytes);
 
 /*
  * dbsp_cache_evict -- cuts every sequence with more than `budget` used slots back to `budget`, each KV head by itself: the keys

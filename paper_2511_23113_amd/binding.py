@@ -107,7 +107,7 @@ def load_library(path: str | None = None):
     cache, f32 = C.POINTER(CacheDesc), C.c_float
     lib.dbsp_cache_attn_fwd.argtypes = [cache, vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, i32, i32, i32, f32, f32, vp, i64, vp]
     lib.dbsp_cache_attn_fwd.restype = C.c_int
-    lib.dbsp_cache_attn_workspace.argtypes = [cache, i32, i32, i32, i64p]
+    lib.dbsp_cache_attn_workspace.argtypes = [cache, i32, i32, i32, i32, i64p]
     lib.dbsp_cache_attn_workspace.restype = C.c_int
     lib.dbsp_cache_evict.argtypes = [cache, i32, i32, vp, vp, i64, vp]
     lib.dbsp_cache_evict.restype = C.c_int
@@ -453,7 +453,7 @@ def cache_attn_fwd(cache: KVCache, q, q_lens=None, causal: bool = True, decay=No
     elif cache.weights is None:
         raise ValueError("the cache has no weights")
     lib = _lib
-    workspace, at, size = cache._workspace(workspace, (H, Nq, decay >= 0), lib.dbsp_cache_attn_workspace, raw, elsewhere)
+    workspace, at, size = cache._workspace(workspace, (H, Nq, causal, decay >= 0), lib.dbsp_cache_attn_workspace, raw, elsewhere)
     o_s = o.stride()
     rc = lib.dbsp_cache_attn_fwd(cache._at, q.data_ptr(), q_s[0], q_s[1], q_s[2], o.data_ptr(), o_s[0], o_s[1], o_s[2], None if lse is None else lse.data_ptr(),
                                  None if q_lens is None else q_lens.data_ptr(), H, Nq, causal, softmax_scale, decay, at, size, raw)

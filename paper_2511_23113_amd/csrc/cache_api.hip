@@ -74,31 +74,40 @@ struct Cut {             // how an attention call is laid out
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Of a launch of n row tiles of `tiles` key tiles each on a chip that holds `slots` workgroups at a time: whole rounds of row tiles
-// as they are, and the last one or two cut into parts that fill their rounds.  What an item costs beside its tiles, in tiles:
-// kStart, and kPart more for a part (its partial result, and its share of the merge).
-constexpr double kStart = 2, kPart = 3;
-dbsp_cache_long_cut cut_long(int64_t n, int64_t tiles, int slots) {
+// Of a launch of n row tiles on a chip that holds `slots` workgroups at a time.  They have `tiles` key tiles each: whole rounds of row
+// tiles go as they are, and the last one or two are cut into parts that fill their rounds.  Or causality leaves the first
+// ones `span` fewer: then the longest go first, and all are cut if the longest alone would outlast the others' share.
+// What an item costs beside its tiles, in tiles: kStart, and kPart more for a part (its result goes to memory and back).
+constexpr double kStart = 2, kPart = 8;
+dbsp_cache_long_cut cut_long(int64_t n, int64_t tiles, int64_t span, int slots) {
   const int dies = n < 64 ? 1 : 8;         // few row tiles: their parts go to all dies
   const int64_t per = (n + dies - 1) / dies, room = slots / dies;
-  dbsp_cache_long_cut best = {(int32_t)n, dies, (int32_t)per, (int32_t)per, 0, 1};
-  double least = (double)((per + room - 1) / room) * (tiles + kStart);
-  for (int64_t whole = per / room * room; whole >= 0 && whole + 2 * room > per; whole -= room) {
-    const int64_t tail = per - whole;
-    for (int64_t k = 2; tail > 0 && 2 * k <= tiles && tail * k <= 6 * room; ++k) {
-      const double cost = (double)(whole / room) * (tiles + kStart) + (double)((tail * k + room - 1) / room) * ((tiles + k - 1) / k + kStart + kPart);
-      if (cost < least) {
-        least = cost;
-        best.whole = (int32_t)whole;
-        best.tail = (int32_t)tail;
-        best.k = (int32_t)k;
-      }
+  const bool longest_first = 4 * span > tiles;
+  dbsp_cache_long_cut best = {(int32_t)n, dies, (int32_t)per, (int32_t)per, 0, 1, longest_first};
+  auto take = [&](double cost, double& least, int64_t whole, int64_t k) {
+    if (cost >= least) return;
+    least = cost;
+    best.whole = (int32_t)(k > 1 ? whole : per);
+    best.tail = (int32_t)(k > 1 ? per - whole : 0);
+    best.k = (int32_t)k;
+  };
+  double least = 1e300;
+  if (longest_first) {
+    const double work = (double)per * (tiles - 0.5 * span), longest = (double)tiles;
+    for (int64_t k = 1; k == 1 || (2 * k <= tiles && per * k <= 6 * room); ++k) {
+      const double more = kStart + (k > 1 ? kPart : 0);
+      take(std::max((work + per * k * more) / room, longest / k + more) + 0.15 * longest / k, least, 0, k);
     }
+    return best;
   }
+  least = (double)((per + room - 1) / room) * (tiles + kStart);
+  for (int64_t whole = per / room * room; whole >= 0 && whole + 2 * room > per; whole -= room)
+    for (int64_t k = 2; per > whole && 2 * k <= tiles && (per - whole) * k <= 6 * room; ++k)
+      take((double)(whole / room) * (tiles + kStart) + (double)(((per - whole) * k + room - 1) / room) * ((tiles + k - 1) / k + kStart + kPart), least, whole, k);
   return best;
 }
 
-int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool with_weights, Cut& cut) {
+int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool causal, bool with_weights, Cut& cut) {
   const int rc = check_cache(who, c);
   if (rc != DBSP_OK) return rc;
   if (H <= 0 || Nq <= 0) return fail(who, DBSP_EINVAL, "H and Nq must be positive");
@@ -121,7 +130,8 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool wi
   if (row_tiles > kMost) return fail(who, DBSP_ESHAPE, "too many queries");
   const bool many = p.many;
   p.split = !many && (p.pooled || (row_tiles < kCacheTarget && most_tiles > kCacheWhole));
-  if (many) p.cut = cut_long(row_tiles, most_tiles, (c->d == 128 ? 1 : 2) * kLongSlots * 4 / kLongWaves);
+  const int64_t span = causal ? std::min(Nq, c->capacity) / kCacheKeys : 0;
+  if (many) p.cut = cut_long(row_tiles, most_tiles, span, (c->d == 128 ? 1 : 2) * kLongSlots * 4 / kLongWaves);
   // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kCacheTarget of them
   const int64_t pre_items = std::min(pre_unit * p.pre_tiles, kCacheTarget + pre_unit);
   const int64_t own_items = many ? (int64_t)p.cut.dies * p.cut.tail * p.cut.k : p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), kCacheTarget + row_tiles) : row_tiles;
@@ -170,11 +180,11 @@ int lay_out_evict(const char* who, const dbsp_cache* c, int32_t budget, Moves& m
 
 extern "C" {
 
-int dbsp_cache_attn_workspace(const dbsp_cache* cache, int32_t H, int32_t Nq, int32_t with_weights, int64_t* bytes) {
+int dbsp_cache_attn_workspace(const dbsp_cache* cache, int32_t H, int32_t Nq, int32_t causal, int32_t with_weights, int64_t* bytes) {
   const char* who = "dbsp_cache_attn_workspace";
   if (!bytes) return fail(who, DBSP_EINVAL, "null pointer");
   Cut cut;
-  const int rc = lay_out(who, cache, H, Nq, with_weights != 0, cut);
+  const int rc = lay_out(who, cache, H, Nq, causal != 0, with_weights != 0, cut);
   *bytes = rc == DBSP_OK ? cut.bytes : 0;
   return rc;
 }
@@ -187,7 +197,7 @@ int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch,
   if (!(softmax_scale == softmax_scale) || softmax_scale > 1e30f) return fail(who, DBSP_EINVAL, "softmax_scale must be finite");
   const bool with_weights = decay >= 0.f;
   Cut cut;
-  const int rc = lay_out(who, cache, H, Nq, with_weights, cut);
+  const int rc = lay_out(who, cache, H, Nq, causal != 0, with_weights, cut);
   if (rc != DBSP_OK) return rc;
   if (!q || !o || (!workspace && cut.bytes > 0)) return fail(who, DBSP_EINVAL, "null pointer");
   const int64_t size[3] = {cache->B, H, Nq}, q_stride[3] = {q_batch, q_head, q_token}, o_stride[3] = {o_batch, o_head, o_token};

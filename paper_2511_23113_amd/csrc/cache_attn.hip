@@ -404,10 +404,10 @@ __device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
   bool there;
   if (p.many) {      // the rows of the tiles that were cut
     const dbsp_cache_long_cut& cut = p.cut;
-    const int z = (int)(nth / p.own_rows), in = (int)(nth % p.own_rows), x = z / cut.tail * cut.per + cut.whole + z % cut.tail;
-    there = z < cut.dies * cut.tail && x < cut.items;
+    const int z = (int)(nth / p.own_rows), in = (int)(nth % p.own_rows);
     Item it;
-    row_tile(p, there ? x : 0, it);
+    there = z < cut.dies * cut.tail && long_row_tile(p, z / cut.tail, cut.whole + z % cut.tail, it);
+    if (!there) it = {0, 0, 0, 0, 0, 0};
     const int row = it.rt * kLongRows + in;
     b = it.b;
     t = row / p.G;

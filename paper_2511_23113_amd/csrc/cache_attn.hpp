@@ -79,11 +79,28 @@ struct Item {
   int64_t slot;          // of its partial result
 };
 
-// Row tile x of all, sequence by sequence and head by head, the last rows first: causal ones are the longest there.
+// Row tile x of all, sequence by sequence and head by head, the last rows first.
 __device__ __forceinline__ void row_tile(const dbsp_cache_attn_params& p, int x, Item& it) {
   it.rt = p.own_row_tiles - 1 - x % p.own_row_tiles;
   it.hk = x / p.own_row_tiles % p.Hk;
   it.b = x / p.own_row_tiles / p.Hk;
+}
+// Row tile x of a die, of a launch of the kernel for many queries; false: it has no such.  Either a run of the tiles in the order
+// above, so that those of the same keys run at the same time, or, where causality makes the tiles of different lengths, the
+// longest ones first, the (sequence, head) pairs dealt to the dies in turn.
+__device__ __forceinline__ bool long_row_tile(const dbsp_cache_attn_params& p, int die, int x, Item& it) {
+  const dbsp_cache_long_cut& cut = p.cut;
+  const int n = cut.longest_first ? x * cut.dies + die : die * cut.per + x;
+  if (n >= cut.items) return false;
+  if (cut.longest_first) {
+    const int pairs = p.B * p.Hk;
+    it.rt = p.own_row_tiles - 1 - n / pairs;
+    it.hk = n % pairs % p.Hk;
+    it.b = n % pairs / p.Hk;
+  } else {
+    row_tile(p, n, it);
+  }
+  return true;
 }
 
 // Which item this workgroup has; false: none.  All of the workgroup's threads call it.
@@ -185,8 +202,7 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
 __device__ __forceinline__ bool find_long_item(const dbsp_cache_attn_params& p, Item& it) {
   const dbsp_cache_long_cut& cut = p.cut;
   const int die = blockIdx.x % cut.dies, y = blockIdx.x / cut.dies, z = y - cut.whole, x = z < 0 ? y : cut.whole + z % cut.tail;
-  if (die * cut.per + x >= cut.items) return false;
-  row_tile(p, die * cut.per + x, it);
+  if (!long_row_tile(p, die, x, it)) return false;
   it.n = z < 0 ? 1 : cut.k;
   it.c = z < 0 ? 0 : z / cut.tail;
   it.slot = it.n == 1 ? -1 : ((int64_t)die * cut.tail + x - cut.whole) * cut.k + it.c;

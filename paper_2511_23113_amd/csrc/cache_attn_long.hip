@@ -33,6 +33,8 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
   constexpr int ROWS = 64 * NW, SHARE = 64 / NW, COPIES = SHARE / L::RPC;
   constexpr int SUB = 2 * L::KS;           // sub-slots of a step
   constexpr int KP = 3, VP = 2;            // places
+  constexpr int kBias = 3072;
+  static_assert(COPIES <= 4, "a group's copies share a destination");
   __shared__ __attribute__((aligned(1024))) unsigned char lds[(KP + VP) * L::TILE];
   const uint32_t lds_base = (uint32_t)(uintptr_t)(LDS_PTR(unsigned char))lds;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, r = l & 31, g = l >> 5;
@@ -65,6 +67,13 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
 #pragma unroll
     for (int ks = 0; ks < L::KS; ++ks) q[y][ks] = *reinterpret_cast<const u32x4*>(src + 16 * ks + 8 * g);
   }
+  // (d = 128: MFMAs read Q from accumulation registers)
+#pragma unroll
+  for (int y = 0; y < 2; ++y)
+#pragma unroll
+    for (int ks = 0; ks < L::KS; ++ks) {
+      if constexpr (D == 128) asm volatile("" : "+a"(q[y][ks]));
+    }
   for (int s = 16; s > 0; s >>= 1) {
     all_see = min(all_see, __shfl_xor(all_see, s));
     any_sees = max(any_sees, __shfl_xor(any_sees, s));
@@ -77,7 +86,7 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
   // Copies: this wave's share of a tile.  Where a tile lies and how its rows are clamped changes at the ends of prefix and own keys only
   const int row_in = l / L::NCH, pch = l % L::NCH;
   struct Source {
-    const unsigned char* at;               // of the tile's first row of this wave
+    const unsigned char* at;               // of the tile, less kBias
     int there;                             // rows of the tile that hold keys, as far as the offsets go by it
     uint32_t off[COPIES];
   } ksrc{nullptr, -1, {}}, vsrc{nullptr, -1, {}};
@@ -88,24 +97,28 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
     const int tok = (pre ? t : t - pre_tiles) * kCacheKeys, there = min((pre ? p.P : len) - tok, kCacheKeys) + (pre ? 2 * kCacheKeys : 0);
     const uint32_t st = IS_K ? (pre ? p.pk_st : p.k_st) : (pre ? p.pv_st : p.v_st);
     const uint16_t* from = IS_K ? (pre ? p.pk + hk * p.pk_sh : p.k + b * p.k_sb + hk * p.k_sh) : (pre ? p.pv + hk * p.pv_sh : p.v + b * p.v_sb + hk * p.v_sh);
-    src.at = reinterpret_cast<const unsigned char*>(from) + (int64_t)tok * st;
+    src.at = reinterpret_cast<const unsigned char*>(from) + (int64_t)tok * st - kBias;
     if (there != src.there) {
       src.there = there;
       const int last = (pre ? there - 2 * kCacheKeys : there) - 1;
 #pragma unroll
       for (int x = 0; x < COPIES; ++x) {
         const int in = x * L::RPC + row_in;
-        src.off[x] = min(w * SHARE + in, last) * st + ((pch ^ (IS_K ? L::k_swz(in) : L::v_swz(in))) << 4);
+        src.off[x] = min(w * SHARE + in, last) * st + ((pch ^ (IS_K ? L::k_swz(in) : L::v_swz(in))) << 4) + kBias - x * 1024;
       }
     }
   };
   constexpr std::integral_constant<bool, true> K_{};
   constexpr std::integral_constant<bool, false> V_{};
   const uint32_t share = lds_base + w * SHARE * L::ROWB;
-  auto copy = [&](const Source& src, uint32_t place, int x) __attribute__((always_inline)) { copy_row16(src.at, src.off[x], share + place * L::TILE + x * 1024); };
+  // a group's destination, and its copies: the instruction's offset, x KiB, counts on both sides, and kBias keeps the source's other
+  // offset from below 0
+  auto copy_to = [&](uint32_t place) __attribute__((always_inline)) { set_copy_dst(share + place * L::TILE); };
+  auto copy = [&](const Source& src, int x) __attribute__((always_inline)) { copy16_nth(x, src.at, src.off[x]); };
   auto copy_all = [&](const Source& src, uint32_t place) __attribute__((always_inline)) {
+    copy_to(place);
 #pragma unroll
-    for (int x = 0; x < COPIES; ++x) copy(src, place, x);
+    for (int x = 0; x < COPIES; ++x) copy(src, x);
   };
 
   // operand reads, at the place of this tile
@@ -120,11 +133,11 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
   }
   u32x4 kf[L::KS], vf[L::KS];              // operands: of V by 16-key step * DT + d-tile
   auto read_k = [&](int ks, int half) __attribute__((always_inline)) { kf[ks] = *(LDS_PTR(u32x4))(uintptr_t)(k_rd[ks] + half * 32 * L::ROWB); };
-  auto read_v = [&](int x, int half) __attribute__((always_inline)) {
-    const uint32_t a = v_rd[x % L::DT] + (32 * half + 16 * (x / L::DT)) * L::ROWB;
-    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(a)));
-    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(a + 8 * L::ROWB)));
-    vf[x] = u32x4{lo.x, lo.y, hi.x, hi.y};
+  auto read_v = [&](int x, int part, int half) __attribute__((always_inline)) {      // part 0, 1: keys 0 .. 7, 8 .. 15 of its 16
+    const uint32_t a = v_rd[x % L::DT] + (32 * half + 16 * (x / L::DT) + 8 * part) * L::ROWB;
+    const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(a)));
+    vf[x][2 * part] = v.x;
+    vf[x][2 * part + 1] = v.y;
   };
 
   f32x16 o[2][L::DT], s[2];                // by query tile
@@ -147,21 +160,20 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
       if (8 * (e / 4) + e % 4 >= left) s[y][e] = -INFINITY;
   };
   auto needs_mask = [&](int t) { return t < pre_tiles ? (t + 1) * kCacheKeys > p.P : (t - pre_tiles + 1) * kCacheKeys > all_see; };
-  auto exp_at = [](int j) constexpr { return 1 + j * (SUB - 3) / 16; };
+  auto exp_at = [](int j) constexpr { return 1 + j * (SUB - 4) / 16; };
 
   // Step of query tile Y in half HALF of a tile: copies from `src` to its place where there are any.
   auto step = [&](auto y_tag, auto half_tag, const Source* src, uint32_t place) __attribute__((always_inline)) {
     constexpr int Y = decltype(y_tag)::value, HALF = decltype(half_tag)::value, N = 1 - Y;
     float xs[16], ps[16], l0 = 0.f, l1 = 0.f;
     bool far = false;
+    if constexpr (HALF == 0) copy_to(place);
     for_each<SUB>([&](auto z_tag) __attribute__((always_inline)) {
       constexpr int z = decltype(z_tag)::value, x = z / 2;
       if constexpr (z % 2 == 0) {
         s[N] = T::mfma(kf[x], q[N][x], x == 0 ? zero : s[N]);
-        if constexpr (Y == 0) read_k(x, 1 - HALF);      // of the next 32 keys: k_rd is at the next tile in the second half
       } else {
         o[N][x % L::DT] = T::mfma(vf[x], pr[N][x / L::DT], o[N][x % L::DT]);
-        if constexpr (Y == 0) read_v(x, HALF);
       }
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
@@ -172,11 +184,22 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
           else if (j == 1) l1 = ps[1];
           else if (j & 1) l1 += ps[j];
           else l0 += ps[j];
-          if (j & 1) pr[Y][j / 8][j % 8 / 2] = T::pack(ps[j - 1], ps[j]);
+          if (j & 1) {
+            uint32_t both = T::pack(ps[j - 1], ps[j]);
+            asm volatile("" : "+v"(both));      // here, not behind the branch at the step's end
+            pr[Y][j / 8][j % 8 / 2] = both;
+          }
         }
       }
-      if constexpr (HALF == 0 && z % 2 == 1 && x < COPIES) copy(*src, place, x);
-      if constexpr (z == SUB - 1) {
+      // operand x is used a last time in sub-slots 2 x and 2 x + 1 of the first step, and next at the same place of the second: its
+      // three reads are dealt evenly over both (K of the next 32 keys: k_rd is at the next tile in the second half)
+      constexpr int rd = Y * SUB + z - 1, rx = rd / 3;
+      if constexpr (rd >= 0 && rx < L::KS) {
+        if constexpr (rd % 3 == 0) read_k(rx, 1 - HALF);
+        else read_v(rx, rd % 3 - 1, HALF);
+      }
+      if constexpr (HALF == 0 && z % 2 == 0 && x > 0 && x <= COPIES) copy(*src, x - 1);
+      if constexpr (z == SUB - 2) {        // (a sub-slot ahead of the branch)
         l0 += l1;
         far = __builtin_amdgcn_ballot_w64(l0 > SPEC_SUM_LIMIT) != 0;
       }
@@ -240,7 +263,7 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
     if (t < mine) {
       const bool pre = t < pre_tiles, pre_n = t + 1 < pre_tiles;
       const int key = (pre ? t : t - pre_tiles) * kCacheKeys, key_n = (pre_n ? t + 1 : t + 1 - pre_tiles) * kCacheKeys;
-      const bool m = needs_mask(t), m_n = needs_mask(t + 1);
+      const int m = __builtin_amdgcn_readfirstlane(needs_mask(t)), m_n = __builtin_amdgcn_readfirstlane(needs_mask(t + 1));
       step(C0, C0, &vsrc, KP + v_next);
       if (m) mask(1, pre, key);
       step(C1, C0, &ksrc, k_to);
@@ -249,9 +272,9 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
       for (int ks = 0; ks < L::KS; ++ks) k_rd[ks] += (k_next - kp) * L::TILE;
       step(C0, C1, nullptr, 0);
       if (m) mask(1, pre, key + 32);
+      step(C1, C1, nullptr, 0);
 #pragma unroll
       for (int dt = 0; dt < L::DT; ++dt) v_rd[dt] += (v_next - vp) * L::TILE;
-      step(C1, C1, nullptr, 0);
       if (m_n) mask(0, pre_n, key_n);
     } else {
       copy_all(vsrc, KP + v_next);

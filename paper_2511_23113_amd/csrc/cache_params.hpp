@@ -22,7 +22,7 @@ constexpr int kEvictPart = 8192;
 // How a launch of the kernel for many queries is cut: its row tiles, `per` for each of `dies` dies (workgroup number mod 8), of which
 // the first `whole` are one item each and the `tail` others `k` parts, so that the last round of workgroups ends together.
 struct dbsp_cache_long_cut {
-  int32_t items, dies, per, whole, tail, k;
+  int32_t items, dies, per, whole, tail, k, longest_first;
 };
 
 struct dbsp_cache_attn_params {

@@ -50,7 +50,7 @@ def test_bad_caches_are_refused_by_every_entry_point(change, word):
     for rc, msg in (attn(desc(**change)), evict(desc(**change))):
         assert rc == B.DBSP_EINVAL and word in msg
     n = C.c_int64(7)
-    assert B.load_library().dbsp_cache_attn_workspace(C.byref(desc(**change)), 4, 1, 1, C.byref(n)) == B.DBSP_EINVAL and n.value == 0
+    assert B.load_library().dbsp_cache_attn_workspace(C.byref(desc(**change)), 4, 1, 1, 1, C.byref(n)) == B.DBSP_EINVAL and n.value == 0
 
 
 BAD_CALLS = [
@@ -77,7 +77,7 @@ def test_attention_shapes_and_missing_weights():
     rc, msg = attn(desc(weights=None))
     assert rc == B.DBSP_EINVAL and "no weights" in msg
     lib = B.load_library()
-    assert lib.dbsp_cache_attn_workspace(C.byref(desc()), 4, 1, 1, None) == B.DBSP_EINVAL
+    assert lib.dbsp_cache_attn_workspace(C.byref(desc()), 4, 1, 1, 1, None) == B.DBSP_EINVAL
 
 
 def test_bad_evictions():
@@ -98,15 +98,16 @@ def test_bad_evictions():
 def test_workspaces_grow_with_the_call_and_stay_moderate():
     lib, n = B.load_library(), C.c_int64()
 
-    def need(d, H, Nq, weights=0):
-        assert lib.dbsp_cache_attn_workspace(C.byref(d), H, Nq, weights, C.byref(n)) == B.DBSP_OK
+    def need(d, H, Nq, weights=0, causal=1):
+        assert lib.dbsp_cache_attn_workspace(C.byref(d), H, Nq, causal, weights, C.byref(n)) == B.DBSP_OK
         return n.value
     assert need(desc(), 4, 1) == 0         # one launch
     small = need(desc(n_prefix=1000), 4, 1)
     assert 0 < small < 1 << 22 and small % 256 == 0
     assert need(desc(n_prefix=1000), 4, 1, 1) > small
     # of long prompts only the last rounds' row tiles are cut
-    assert need(desc(B=4, Hk=40, capacity=9000), 40, 9000) < 1 << 28
+    assert need(desc(B=4, Hk=40, capacity=9000), 40, 9000) == 0
+    assert need(desc(B=4, Hk=40, capacity=9000), 40, 9000, causal=0) < 1 << 28
     assert need(desc(n_prefix=1 << 20), 4, 1) < 1 << 30
     assert lib.dbsp_cache_evict_workspace(C.byref(desc()), 48, C.byref(n)) == B.DBSP_OK and n.value == 256 + 2 * 256
 
