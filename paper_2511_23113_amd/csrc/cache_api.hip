@@ -132,6 +132,7 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool ca
   p.split = !many && (p.pooled || (row_tiles < kCacheTarget && most_tiles > kCacheWhole));
   const int64_t span = causal ? std::min(Nq, c->capacity) / kCacheKeys : 0;
   if (many) p.cut = cut_long(row_tiles, most_tiles, span, (c->d == 128 ? 1 : 2) * kLongSlots * 4 / kLongWaves);
+  p.row_shift = many && p.cut.longest_first && p.own_row_tiles > 1 ? (int32_t)(p.own_row_tiles * (int64_t)kLongRows - rows) : 0;
   // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kCacheTarget of them
   const int64_t pre_items = std::min(pre_unit * p.pre_tiles, kCacheTarget + pre_unit);
   const int64_t own_items = many ? (int64_t)p.cut.dies * p.cut.tail * p.cut.k : p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), kCacheTarget + row_tiles) : row_tiles;

@@ -408,7 +408,8 @@ __device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
     Item it;
     there = z < cut.dies * cut.tail && long_row_tile(p, z / cut.tail, cut.whole + z % cut.tail, it);
     if (!there) it = {0, 0, 0, 0, 0, 0};
-    const int row = it.rt * kLongRows + in;
+    const int row = max(0, it.rt * kLongRows - p.row_shift + in);
+    there = there && it.rt * kLongRows + in >= p.row_shift;
     b = it.b;
     t = row / p.G;
     h = it.hk * p.G + row % p.G;

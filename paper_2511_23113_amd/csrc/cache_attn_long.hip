@@ -41,8 +41,8 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
   Item it;
   if (!find_long_item(p, it)) return;
   const int b = __builtin_amdgcn_readfirstlane(it.b), hk = __builtin_amdgcn_readfirstlane(it.hk), rt = __builtin_amdgcn_readfirstlane(it.rt);
-  const int len = len_of(p, b), q_len = q_len_of(p, b), row0 = rt * ROWS;
-  if (row0 / p.G >= q_len) return;         // no query here: its rows stay as they are
+  const int len = len_of(p, b), q_len = q_len_of(p, b), row0 = rt * ROWS - p.row_shift;      // (rows below 0 are none)
+  if (max(row0, 0) / p.G >= q_len) return; // no query here: its rows stay as they are
   const int base = len - q_len + 1;        // causal: query t sees the first base + t own keys
   const int seen = p.causal ? max(0, min(len, base + min(q_len - 1, (row0 + ROWS - 1) / p.G))) : len;
   const int pre_tiles = p.pre_tiles, n_all = own_tiles(p, b), per = (n_all + it.n - 1) / it.n, n_here = pre_tiles + tiles_of(seen);
@@ -57,8 +57,8 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
     const int row = row0 + 64 * w + 32 * y + r;
-    at[y] = row_of(p, b, min(row, rows - 1));
-    valid[y] = row < rows && at[y].t < q_len;
+    at[y] = row_of(p, b, max(0, min(row, rows - 1)));
+    valid[y] = row >= 0 && row < rows && at[y].t < q_len;
     h[y] = hk * p.G + at[y].g;
     limit[y] = p.causal ? max(0, min(len, base + at[y].t)) : len;
     all_see = min(all_see, valid[y] ? limit[y] : INT_MAX);

@@ -43,6 +43,7 @@ struct dbsp_cache_attn_params {
   int32_t pre_row_tiles, own_row_tiles;            // row tiles of a KV head: of all sequences together (pooled), of one sequence
   int32_t own_tile_rows;               // rows of an own item: kCacheRows, or kLongRows for the kernel of cache_attn_long.hip
   int32_t own_rows;                    // and of its partial result: not more than Nq * G
+  int32_t row_shift;                   // with longest_first: so many rows of the first row tile are none, as it has the fewest keys
   int32_t max_pre_items;
   dbsp_cache_long_cut cut;             // with `many` only
   float scale_log2;                    // softmax scale * log2(e)

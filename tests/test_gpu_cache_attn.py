@@ -121,6 +121,8 @@ CASES = {
     "frame": (2, 4, 2, 70, 128, 130, 210, [210, 140], None, False, "bf16", 1.0),
     "prompt": (2, 2, 1, 150, 64, 0, 150, [150, 97], [150, 97], True, "bf16", 1.0),
     "prompt_no_prefix_fp16": (1, 3, 3, 257, 128, 0, 300, [257], None, True, "fp16", 0.0),
+    "prompt_rows_from_the_end": (2, 10, 2, 130, 128, 20, 140, [140, 130], [130, 77], True, "fp16", 1.0),
+    "prompt_in_parts": (1, 2, 2, 700, 64, 0, 700, [700], None, True, "bf16", None),
     "prompt_after_others": (1, 2, 1, 200, 128, 77, 600, [431], None, True, "bf16", 1.0),
     "prompt_weights_in_parts": (1, 4, 2, 620, 64, 0, 700, [689], None, True, "bf16", 0.5),
     "frame_weights_in_parts": (1, 3, 1, 500, 128, 30, 700, [601], [433], False, "fp16", 1.0),
