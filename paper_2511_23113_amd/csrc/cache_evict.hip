@@ -126,6 +126,12 @@ __device__ __forceinline__ void list_moves(const uint32_t (&x)[R], int first, in
     const bool stays = kept >> j & 1, in = i < n;
     const uint64_t hm = __builtin_amdgcn_ballot_w64(in && i < budget && !stays), fm = __builtin_amdgcn_ballot_w64(in && i >= budget && stays);
     if (l == 0) table[j * WAVES + w] = __popcll(hm) | __popcll(fm) << 16;
+    if (first + (j + 1) * NT >= n) {       // none behind
+#pragma unroll
+      for (int y = j + 1; y < R; ++y)
+        if (l == 0) table[y * WAVES + w] = 0;
+      break;
+    }
   }
   scan_table<NT, R>(table);
 #pragma unroll
@@ -149,16 +155,7 @@ __device__ __forceinline__ void count_digits(const uint32_t (&x)[R], int here, u
   for (int j = 0; j < R; ++j) {
     if (j * kNT >= here) break;
     const bool in = x[j] != 0u && (PASS == 0 || (x[j] ^ limit) >> kShift[PASS ? PASS - 1 : 0] == 0u);
-    const uint32_t digit = x[j] >> kShift[PASS] & (PASS == 2 ? 1023 : 2047);
-    const uint64_t m = __builtin_amdgcn_ballot_w64(in);
-    if (m == 0) continue;
-    // a wave whose images all have one digit adds once (equal weights would take turns at one counter)
-    const uint32_t one = __builtin_amdgcn_readlane(digit, __builtin_ctzll(m));
-    if (__builtin_amdgcn_ballot_w64(in && digit != one) == 0) {
-      if ((threadIdx.x & 63) == 0) atomicAdd(&hist[one], (uint32_t)__popcll(m));
-    } else if (in) {
-      atomicAdd(&hist[digit], 1u);
-    }
+    if (in) atomicAdd(&hist[x[j] >> kShift[PASS] & (PASS == 2 ? 1023 : 2047)], 1u);
   }
 }
 
@@ -167,8 +164,9 @@ struct two { uint32_t hi, lo; };
 __device__ __forceinline__ two my_digits(const uint32_t* counts) { return {counts[kDigits - 1 - 2 * threadIdx.x], counts[kDigits - 2 - 2 * threadIdx.x]}; }
 
 // Of the images whose upper bits are those of `limit`: the digit below them at which `left` of them, from the largest on, are
-// reached.  limit and left are brought up to date; returns how many have the chosen digit.
-__device__ __forceinline__ uint32_t pick_digit(two counts, int shift, uint32_t& limit, uint32_t& left) {
+// reached.  limit and left are brought up to date; returns how many have the chosen digit.  (PASS: its own places in the LDS)
+template <int PASS>
+__device__ __forceinline__ uint32_t pick_digit(two counts, uint32_t& limit, uint32_t& left) {
   __shared__ uint32_t wave_sum[kNT / 64], got[3];
   const int t = threadIdx.x, w = t >> 6, l = t & 63;
   const uint32_t hi = counts.hi, lo = counts.lo;
@@ -189,11 +187,9 @@ __device__ __forceinline__ uint32_t pick_digit(two counts, int shift, uint32_t& 
     got[2] = first ? hi : lo;
   }
   __syncthreads();
-  limit |= got[0] << shift;
+  limit |= got[0] << kShift[PASS];
   left = got[1];
-  const uint32_t equal = got[2];
-  __syncthreads();
-  return equal;
+  return got[2];
 }
 
 template <int R>
@@ -215,16 +211,16 @@ __global__ __launch_bounds__(kNT) void dbsp_cache_choose_kernel(const dbsp_cache
   uint32_t limit = 0, left = (uint32_t)budget;
   count_digits<0, R>(x, n, limit, hist);
   __syncthreads();
-  uint32_t equal = pick_digit(my_digits(hist), kShift[0], limit, left);
+  uint32_t equal = pick_digit<0>(my_digits(hist), limit, left);
   if (equal != left) {
     count_digits<1, R>(x, n, limit, hist + kDigits);
     __syncthreads();
-    equal = pick_digit(my_digits(hist + kDigits), kShift[1], limit, left);
+    equal = pick_digit<1>(my_digits(hist + kDigits), limit, left);
   }
   if (equal != left) {
     count_digits<2, R>(x, n, limit, hist + 2 * kDigits);
     __syncthreads();
-    equal = pick_digit(my_digits(hist + 2 * kDigits), kShift[2], limit, left);
+    equal = pick_digit<2>(my_digits(hist + 2 * kDigits), limit, left);
   }
   int32_t *holes = p.holes + (int64_t)pair * p.max_moves, *fillers = p.fillers + (int64_t)pair * p.max_moves;
   float* weights = p.weights + (int64_t)pair * p.cap;
@@ -272,8 +268,9 @@ __global__ __launch_bounds__(kNT) void dbsp_cache_part_kernel(const dbsp_cache_e
 #pragma unroll
   for (int y = 0; y < PASS && PASS < 4; ++y) counts[y] = my_digits(digits + y * kDigits);
   load_images<kNT, kR>(p, pair, first, n, x);
-#pragma unroll
-  for (int y = 0; y < PASS && PASS < 4; ++y) equal = pick_digit(counts[y], kShift[y], limit, left);
+  if constexpr (PASS > 0 && PASS < 4) equal = pick_digit<0>(counts[0], limit, left);
+  if constexpr (PASS > 1 && PASS < 4) equal = pick_digit<1>(counts[1], limit, left);
+  if constexpr (PASS > 2 && PASS < 4) equal = pick_digit<2>(counts[2], limit, left);
   if (PASS == 3 && part == 0 && t == 0) {
     chosen[0] = limit;
     chosen[1] = left;
