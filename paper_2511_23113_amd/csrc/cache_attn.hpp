@@ -103,6 +103,17 @@ __device__ __forceinline__ bool long_row_tile(const dbsp_cache_attn_params& p, i
   return true;
 }
 
+// Sum over the wave's lanes up to and with this one: within rows of 16 lanes, then from the ends of rows on.
+__device__ __forceinline__ int scan_wave(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast:15, into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // row_bcast:31, into rows 2 and 3
+  return x;
+}
+
 // Which item this workgroup has; false: none.  All of the workgroup's threads call it.
 __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item& it) {
   constexpr int NT = 256, WAVES = NT / 64;
@@ -117,37 +128,43 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
     it.slot = -1;
     return true;
   }
+  // Parts of every sequence, and where they begin: a sequence (or a run of them) a thread.  Up to 64 of them each wave works it
+  // out for itself, without a barrier.
+  const bool by_wave = p.B <= 64;
+  const int x = by_wave ? l : t, per_thread = by_wave ? 1 : (p.B + NT - 1) / NT, b0 = min(x * per_thread, p.B), b1 = min(b0 + per_thread, p.B);
   __shared__ int64_t tile_sum[WAVES];
   __shared__ int part_sum[WAVES], found[3];
-  const int per_thread = (p.B + NT - 1) / NT, b0 = min(t * per_thread, p.B), b1 = min(b0 + per_thread, p.B);
-  int64_t tiles = 0;
-  for (int b = b0; b < b1; ++b) tiles += own_tiles(p, b);
-  for (int s = 32; s > 0; s >>= 1) tiles += __shfl_xor(tiles, s);
-  if (l == 0) tile_sum[w] = tiles;
-  __syncthreads();
   int64_t own = 0;
-  for (int i = 0; i < WAVES; ++i) own += tile_sum[i];
+  for (int b = b0; b < b1; ++b) own += own_tiles(p, b);
+  if (by_wave) {
+    own = __builtin_amdgcn_readlane(scan_wave((int)own), 63);
+  } else {
+    for (int s = 32; s > 0; s >>= 1) own += __shfl_xor(own, s);
+    if (l == 0) tile_sum[w] = own;
+    __syncthreads();
+    own = 0;
+    for (int i = 0; i < WAVES; ++i) own += tile_sum[i];
+  }
   const int64_t total = own * unit + (p.pooled ? (int64_t)p.Hk * p.pre_row_tiles * p.pre_tiles : 0);
   // (of short key lists up to four tiles an item as long as there are 256 of them: every part costs the merge)
   const int chunk = (int)max(max((int64_t)1, min((int64_t)4, total / 256)), min((int64_t)(1 << 30), (total + kCacheTarget - 1) / kCacheTarget));
   auto parts = [&](int n) { return max(1, (n + chunk - 1) / chunk); };
   int mine = 0;
   for (int b = b0; b < b1; ++b) mine += parts(own_tiles(p, b));
-  int upto = mine;
-  for (int s = 1; s < 64; s <<= 1) {
-    const int o = __shfl_up(upto, s);
-    if (l >= s) upto += o;
-  }
-  if (l == 63) part_sum[w] = upto;
-  __syncthreads();
-  int before = 0, all = 0;
-  for (int i = 0; i < WAVES; ++i) {
-    if (i < w) before += part_sum[i];
-    all += part_sum[i];
+  const int upto = scan_wave(mine);
+  int before = 0, all = __builtin_amdgcn_readlane(upto, 63);
+  if (!by_wave) {
+    if (l == 63) part_sum[w] = upto;
+    __syncthreads();
+    all = 0;
+    for (int i = 0; i < WAVES; ++i) {
+      if (i < w) before += part_sum[i];
+      all += part_sum[i];
+    }
   }
   const int pre_parts = p.pooled ? parts(p.pre_tiles) : 0, pre_items = p.Hk * p.pre_row_tiles * pre_parts;
   int first = before + upto - mine;        // parts of the sequences before this thread's
-  if (blockIdx.x == 0) {                   // for the merge
+  if (blockIdx.x == 0 && (w == 0 || !by_wave)) {      // for the merge
     if (t == 0) { p.table[0] = pre_parts; p.table[1] = pre_items; }
     int f = first;
     for (int b = b0; b < b1; ++b) {
@@ -164,37 +181,47 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
   const int own_items = unit * all, p0 = share(pre_items, die), np = share(pre_items, die + 1) - p0, o0 = share(own_items, die);
   if (i >= np + share(own_items, die + 1) - o0) return false;
   if (i < np) {
-    const int x = p0 + i;
+    const int z = p0 + i;
     it.b = -1;
-    it.rt = x % p.pre_row_tiles;
-    it.c = x / p.pre_row_tiles % pre_parts;
-    it.hk = x / p.pre_row_tiles / pre_parts;
+    it.rt = z % p.pre_row_tiles;
+    it.c = z / p.pre_row_tiles % pre_parts;
+    it.hk = z / p.pre_row_tiles / pre_parts;
     it.n = pre_parts;
-    it.slot = x;
+    it.slot = z;
     return true;
   }
   const int y = o0 + i - np, part = y / unit;      // parts before it, over all sequences
-  if (part >= first && part < first + mine) {
-    for (int b = b0; b < b1; ++b) {
-      const int n = parts(own_tiles(p, b));
-      if (part < first + n) {
-        found[0] = b;
-        found[1] = first;
-        found[2] = n;
-        break;
+  int n = mine;
+  if (by_wave) {
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(part >= first && part < first + mine));
+    it.b = at;
+    first = __builtin_amdgcn_readlane(first, at);
+    n = __builtin_amdgcn_readlane(mine, at);
+  } else {
+    if (part >= first && part < first + mine) {
+      for (int b = b0; b < b1; ++b) {
+        n = parts(own_tiles(p, b));
+        if (part < first + n) {
+          found[0] = b;
+          found[1] = first;
+          found[2] = n;
+          break;
+        }
+        first += n;
       }
-      first += n;
     }
+    __syncthreads();
+    it.b = found[0];
+    first = found[1];
+    n = found[2];
   }
-  __syncthreads();
-  const int z = y - found[1] * unit;
-  it.b = found[0];
-  it.n = found[2];
+  const int z = y - first * unit;
+  it.n = n;
   it.rt = p.own_row_tiles - 1 - z % p.own_row_tiles;
   it.c = z / p.own_row_tiles % it.n;
   it.hk = z / p.own_row_tiles / it.n;
   // partial results lie by sequence, head, part and row tile as the merge counts them; one item alone needs none
-  it.slot = (it.n == 1 && !p.pooled) ? -1 : (int64_t)found[1] * unit + (it.hk * it.n + it.c) * p.own_row_tiles + it.rt;
+  it.slot = (it.n == 1 && !p.pooled) ? -1 : (int64_t)first * unit + (it.hk * it.n + it.c) * p.own_row_tiles + it.rt;
   return true;
 }
 
