@@ -35,7 +35,7 @@ struct Span { int b, hk, row0, rows, len, q_len, pre_tiles, t0, t1; };
 // Row tiles of at most 16 NR rows, the form for single tokens: bound by the stream of K and V.  The keys of a tile are dealt to the
 // waves, 16 each, with 16 x 16 MFMAs: lane (n, g) of 16 x 4 has row n and keys 4 g .. 4 g + 3, and the packed probabilities
 // are the second product's operand again.  A wave reads what it has copied itself, so no barrier couples the waves; each has
-// statistics of its own, against which it forms its probabilities as they stand (the max is raised where one passes 64), and
+// statistics of its own, against which it forms its probabilities as they stand (the max is raised where one passes kRaiseAt), and
 // the four are joined through the LDS at the end.
 template <class T, int D, int NR>
 __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const Item& it, const Span& s, unsigned char* lds) {
@@ -134,7 +134,7 @@ __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const 
 #pragma unroll
       for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -mc[y]));
       const float top4 = fmaxf(fmaxf(pr[0], pr[1]), fmaxf(pr[2], pr[3]));
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(top4 > 64.f) != 0, 0)) {
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(top4 > kRaiseAt) != 0, 0)) {
         float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));

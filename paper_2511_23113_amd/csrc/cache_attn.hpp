@@ -12,6 +12,10 @@
 
 namespace {
 
+// Probabilities are formed against a running max as it stands, and may pass 1 by this (a single one, or a lane's sum of 16) before it
+// is raised: f32 sums hold that as they hold 1, and so do fp16's 65504 and its 2^-14 at the other end.
+constexpr float kRaiseAt = 1024.f;
+
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 

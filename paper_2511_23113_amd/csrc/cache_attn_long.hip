@@ -87,9 +87,11 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
   const int row_in = l / L::NCH, pch = l % L::NCH;
   struct Source {
     const unsigned char* at;               // of the tile, less kBias
+    int64_t step;                          // from tile to tile
+    int until;                             // tiles in front of this one are whole, and of the same list of keys
     int there;                             // rows of the tile that hold keys, as far as the offsets go by it
     uint32_t off[COPIES];
-  } ksrc{nullptr, -1, {}}, vsrc{nullptr, -1, {}};
+  } ksrc{nullptr, 0, 0, -1, {}}, vsrc{nullptr, 0, 0, -1, {}};
   auto aim = [&](Source& src, int t, auto is_k_tag) __attribute__((always_inline)) {
     constexpr bool IS_K = decltype(is_k_tag)::value;
     t = min(t, t1 - 1);
@@ -98,6 +100,8 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
     const uint32_t st = IS_K ? (pre ? p.pk_st : p.k_st) : (pre ? p.pv_st : p.v_st);
     const uint16_t* from = IS_K ? (pre ? p.pk + hk * p.pk_sh : p.k + b * p.k_sb + hk * p.k_sh) : (pre ? p.pv + hk * p.pv_sh : p.v + b * p.v_sb + hk * p.v_sh);
     src.at = reinterpret_cast<const unsigned char*>(from) + (int64_t)tok * st - kBias;
+    src.step = (int64_t)kCacheKeys * st;
+    src.until = min(pre ? p.P / kCacheKeys : pre_tiles + len / kCacheKeys, t1);
     if (there != src.there) {
       src.there = there;
       const int last = (pre ? there - 2 * kCacheKeys : there) - 1;
@@ -110,6 +114,10 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
   };
   constexpr std::integral_constant<bool, true> K_{};
   constexpr std::integral_constant<bool, false> V_{};
+  auto aim_next = [&](Source& src, int t, auto is_k_tag) __attribute__((always_inline)) {      // from tile t - 1
+    if (t < src.until) src.at += src.step;
+    else aim(src, t, is_k_tag);
+  };
   const uint32_t share = lds_base + w * SHARE * L::ROWB;
   // a group's destination, and its copies: the instruction's offset, x KiB, counts on both sides, and kBias keeps the source's other
   // offset from below 0
@@ -198,10 +206,10 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
         if constexpr (rd % 3 == 0) read_k(rx, 1 - HALF);
         else read_v(rx, rd % 3 - 1, HALF);
       }
-      if constexpr (HALF == 0 && z % 2 == 0 && x > 0 && x <= COPIES) copy(*src, x - 1);
+      if constexpr (HALF == 0 && z % (SUB / 4) == SUB / 8 && z * 4 / SUB < COPIES) copy(*src, z * 4 / SUB);
       if constexpr (z == SUB - 2) {        // (a sub-slot ahead of the branch)
         l0 += l1;
-        far = __builtin_amdgcn_ballot_w64(l0 > SPEC_SUM_LIMIT) != 0;
+        far = __builtin_amdgcn_ballot_w64(l0 > kRaiseAt) != 0;
       }
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -253,17 +261,19 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
     }
   }
   uint32_t kp = 0, vp = 0;                 // places of this tile
+  int m_n = t0 < t1 ? needs_mask(t0) : 0;
   for (int t = t0; t < t1; ++t) {
     wait_all();                            // this wave's copies have landed, and its reads of what the next ones overwrite are done
     __builtin_amdgcn_s_barrier();          // everybody's
     asm volatile("" ::: "memory");
     const uint32_t k_next = kp == KP - 1 ? 0 : kp + 1, k_to = k_next == KP - 1 ? 0 : k_next + 1, v_next = vp ^ 1;
-    aim(vsrc, t + 1, V_);
-    aim(ksrc, t + 2, K_);
+    aim_next(vsrc, t + 1, V_);
+    aim_next(ksrc, t + 2, K_);
     if (t < mine) {
       const bool pre = t < pre_tiles, pre_n = t + 1 < pre_tiles;
       const int key = (pre ? t : t - pre_tiles) * kCacheKeys, key_n = (pre_n ? t + 1 : t + 1 - pre_tiles) * kCacheKeys;
-      const int m = __builtin_amdgcn_readfirstlane(needs_mask(t)), m_n = __builtin_amdgcn_readfirstlane(needs_mask(t + 1));
+      const int m = m_n;
+      m_n = __builtin_amdgcn_readfirstlane(needs_mask(t + 1));
       step(C0, C0, &vsrc, KP + v_next);
       if (m) mask(1, pre, key);
       step(C1, C0, &ksrc, k_to);
