@@ -244,7 +244,8 @@ typedef struct dbsp_cache {
   const void *prefix_k, *prefix_v; /* device, [Hk, n_prefix, d]; not looked at if n_prefix == 0 */
   void *k, *v;                /* device, [B, Hk, capacity, d]; not looked at if capacity == 0 */
   /* strides in elements, of the head (and before it the batch) and the token dimension; d has stride 1.  Multiples of 8, at least
-   * 0, a token's at most 2^24; the pointers are 16-byte aligned.  Eviction writes k and v: no two of their elements may share a place */
+   * 0, a token's at most 2^24 (that of a dimension of one is not looked at); the pointers are 16-byte aligned.  Eviction writes k and
+   * v: no two of their elements may share a place */
   int64_t prefix_k_stride[2], prefix_v_stride[2], k_stride[3], v_stride[3];
   int32_t* lens;              /* device, int32 [B]: used slots; taken as 0 below 0 and as capacity above it.  NULL only if capacity == 0 */
   float* weights;             /* device, f32 [B, Hk, capacity] contiguous; NULL where no call uses them */
@@ -259,13 +260,13 @@ typedef struct dbsp_cache {
  * The prefix's keys are read once for the whole batch where a sequence's queries alone would not fill a tile.
  *
  * q:   device, [B, H, Nq, d] with strides in elements (batch, head, token; multiples of 8, d has stride 1), 16-byte aligned.
- * o:   device, as q, written; its own strides, no two elements in one place.
+ * o:   device, as q, written; its own strides, no two elements in one place.  It and lse overlap no input.
  * lse: device, f32 [B, H, Nq] contiguous, written; may be NULL.
  * q_lens: device, int32 [B]: new tokens of each sequence, taken as 0 below 0 and as Nq above it; NULL: Nq each.  Rows t >= q_lens[b]
  *      of o and lse are left as they were, whatever q holds there.
  * A query without a key gets O = 0, LSE = -inf.  K and V must be finite in every used slot and in the prefix (a key that a query
  * does not see has probability zero, which an infinite value does not survive); slots from lens[b] on are never read.
- * softmax_scale <= 0 selects 1 / sqrt(d).  f32 accumulation; results do not depend on anything but the arguments.
+ * softmax_scale <= 0 selects 1 / sqrt(d), else it lies between 1e-30 and 1e30.  f32 accumulation; the same call gives the same bits.
  * decay: below 0 leaves the cache's weights alone; else, for every own key in use,
  *      weights[b, hk, j] = decay * weights[b, hk, j] + sum over the heads h of hk and t < q_lens[b] of exp(s - LSE)
  *      (0: what was there is not read; 1: the sum over all calls), in f32; weights from lens[b] on are left as they were.

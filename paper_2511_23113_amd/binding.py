@@ -339,7 +339,7 @@ class KVCache:
     k, v: [B, Hk, capacity, d], bf16 or fp16 on one GPU, d in (64, 128) dense, other strides multiples of 8 elements; the first
     lens[b] (int32 [B] there) slots of sequence b are used.  prefix_k, prefix_v: [Hk, P, d], shared by all sequences.  Either
     pair may be missing.  weights: f32 [B, Hk, capacity], positions: int32 [B, Hk, capacity], both contiguous.  The object keeps the
-    tensors, which the caller goes on writing; it copies nothing."""
+    tensors, which the caller goes on writing; it copies nothing, and other tensors make another object."""
 
     def __init__(self, k=None, v=None, lens=None, prefix_k=None, prefix_v=None, weights=None, positions=None):
         torch = _torch_module()
@@ -359,7 +359,7 @@ class KVCache:
             setattr(desc, name, x.data_ptr())
             stride = getattr(desc, name + "_stride")
             for i in range(dims - 1):
-                stride[i] = x.stride(i) if x.shape[i] > 1 else 0
+                stride[i] = x.stride(i)
         if k is not None:
             if k.shape != v.shape:
                 raise ValueError("k and v differ in shape")

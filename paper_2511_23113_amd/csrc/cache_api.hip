@@ -22,12 +22,13 @@ int done(const char* who, hipError_t e) {
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-// Strides (the token's last) are ones that the kernels can go by.
-bool strides_ok(const int64_t* s, int n) {
+// Strides (the token's last) are ones that the kernels can go by; that of a dimension of one says nothing.
+bool strides_ok(const int64_t* size, const int64_t* s, int n) {
   for (int i = 0; i < n; ++i)
-    if (s[i] < 0 || s[i] % 8 != 0 || s[i] > (int64_t)1 << 40) return false;
-  return s[n - 1] <= (int64_t)1 << 24;
+    if (size[i] > 1 && (s[i] < 0 || s[i] % 8 != 0 || s[i] > (int64_t)1 << (i == n - 1 ? 24 : 40))) return false;
+  return true;
 }
+int64_t step(int64_t size, int64_t stride) { return size > 1 ? stride : 0; }
 
 // No two elements of a tensor with these sizes and strides (its last dimension dense, d long) share a place: in the order of their
 // strides each dimension steps over all that the ones before it reach.
@@ -54,12 +55,14 @@ int check_cache(const char* who, const dbsp_cache* c) {
   if (c->n_prefix > kMost || c->capacity > 65535 * 128 || (int64_t)c->B * c->Hk > kMost) return fail(who, DBSP_ESHAPE, "the cache is too large");
   if (c->n_prefix > 0) {
     if (!c->prefix_k || !c->prefix_v) return fail(who, DBSP_EINVAL, "null pointer (prefix)");
-    if (!strides_ok(c->prefix_k_stride, 2) || !strides_ok(c->prefix_v_stride, 2) || !aligned(c->prefix_k, 16) || !aligned(c->prefix_v, 16))
+    const int64_t size[2] = {c->Hk, c->n_prefix};
+    if (!strides_ok(size, c->prefix_k_stride, 2) || !strides_ok(size, c->prefix_v_stride, 2) || !aligned(c->prefix_k, 16) || !aligned(c->prefix_v, 16))
       return fail(who, DBSP_EINVAL, "the prefix must be 16-byte aligned, its strides multiples of 8 and a token's at most 2^24");
   }
   if (c->capacity > 0) {
     if (!c->k || !c->v || !c->lens) return fail(who, DBSP_EINVAL, "null pointer (k, v or lens)");
-    if (!strides_ok(c->k_stride, 3) || !strides_ok(c->v_stride, 3) || !aligned(c->k, 16) || !aligned(c->v, 16))
+    const int64_t size[3] = {c->B, c->Hk, c->capacity};
+    if (!strides_ok(size, c->k_stride, 3) || !strides_ok(size, c->v_stride, 3) || !aligned(c->k, 16) || !aligned(c->v, 16))
       return fail(who, DBSP_EINVAL, "k and v must be 16-byte aligned, their strides multiples of 8 and a token's at most 2^24");
     if (!aligned(c->lens, 4) || !aligned(c->weights, 4) || !aligned(c->positions, 4))
       return fail(who, DBSP_EINVAL, "lens, weights and positions must be 4-byte aligned");
@@ -117,7 +120,7 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool ca
   p = {};
   p.B = c->B; p.H = H; p.Hk = c->Hk; p.G = H / c->Hk; p.Nq = Nq; p.P = c->n_prefix; p.cap = c->capacity;
   const int64_t rows = (int64_t)Nq * p.G, all_rows = rows * p.B, q_rows = (int64_t)p.B * Nq * H;
-  if (rows > kMost || all_rows > kMost || q_rows / 8 > kMost) return fail(who, DBSP_ESHAPE, "too many queries");
+  if (rows > kMost || all_rows > kMost || q_rows > INT_MAX) return fail(who, DBSP_ESHAPE, "too many queries");
   p.pre_tiles = (p.P + kCacheKeys - 1) / kCacheKeys;
   p.pooled = p.pre_tiles > kCacheWhole && p.B > 1 && rows < kCacheRows;
   p.pre_row_tiles = p.pooled ? (int32_t)((all_rows + kCacheRows - 1) / kCacheRows) : 0;
@@ -195,14 +198,15 @@ int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch,
                         int32_t causal, float softmax_scale, float decay, void* workspace, int64_t workspace_bytes, void* stream) {
   const char* who = "dbsp_cache_attn_fwd";
   if (!(decay == decay) || decay > 3.0e38f) return fail(who, DBSP_EINVAL, "decay must be finite");
-  if (!(softmax_scale == softmax_scale) || softmax_scale > 1e30f) return fail(who, DBSP_EINVAL, "softmax_scale must be finite");
+  if (!(softmax_scale == softmax_scale) || softmax_scale > 1e30f || (softmax_scale > 0.f && softmax_scale < 1e-30f))
+    return fail(who, DBSP_EINVAL, "softmax_scale must be 0 or between 1e-30 and 1e30");
   const bool with_weights = decay >= 0.f;
   Cut cut;
   const int rc = lay_out(who, cache, H, Nq, causal != 0, with_weights, cut);
   if (rc != DBSP_OK) return rc;
   if (!q || !o || (!workspace && cut.bytes > 0)) return fail(who, DBSP_EINVAL, "null pointer");
   const int64_t size[3] = {cache->B, H, Nq}, q_stride[3] = {q_batch, q_head, q_token}, o_stride[3] = {o_batch, o_head, o_token};
-  if (!strides_ok(q_stride, 3) || !strides_ok(o_stride, 3) || !aligned(q, 16) || !aligned(o, 16))
+  if (!strides_ok(size, q_stride, 3) || !strides_ok(size, o_stride, 3) || !aligned(q, 16) || !aligned(o, 16))
     return fail(who, DBSP_EINVAL, "q and o must be 16-byte aligned, their strides multiples of 8 and a token's at most 2^24");
   if (!distinct(size, o_stride, cache->d)) return fail(who, DBSP_EINVAL, "elements of o overlap");
   if (!aligned(lse, 4) || !aligned(q_lens, 4)) return fail(who, DBSP_EINVAL, "lse and q_lens must be 4-byte aligned");
@@ -217,13 +221,13 @@ int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch,
   p.weights = with_weights && p.cap > 0 ? cache->weights : nullptr;
   p.lens = p.cap > 0 ? cache->lens : nullptr;
   p.q_lens = q_lens;
-  p.q_sb = q_batch; p.q_sh = q_head; p.q_st = q_token;
-  p.o_sb = o_batch; p.o_sh = o_head; p.o_st = o_token;
-  p.pk_sh = cache->prefix_k_stride[0]; p.pv_sh = cache->prefix_v_stride[0];
-  p.k_sb = cache->k_stride[0]; p.k_sh = cache->k_stride[1];
-  p.v_sb = cache->v_stride[0]; p.v_sh = cache->v_stride[1];
-  p.pk_st = (int32_t)(p.P > 0 ? cache->prefix_k_stride[1] * 2 : 0); p.pv_st = (int32_t)(p.P > 0 ? cache->prefix_v_stride[1] * 2 : 0);
-  p.k_st = (int32_t)(p.cap > 0 ? cache->k_stride[2] * 2 : 0); p.v_st = (int32_t)(p.cap > 0 ? cache->v_stride[2] * 2 : 0);
+  p.q_sb = step(p.B, q_batch); p.q_sh = step(H, q_head); p.q_st = step(Nq, q_token);
+  p.o_sb = step(p.B, o_batch); p.o_sh = step(H, o_head); p.o_st = step(Nq, o_token);
+  p.pk_sh = step(p.Hk, cache->prefix_k_stride[0]); p.pv_sh = step(p.Hk, cache->prefix_v_stride[0]);
+  p.k_sb = step(p.B, cache->k_stride[0]); p.k_sh = step(p.Hk, cache->k_stride[1]);
+  p.v_sb = step(p.B, cache->v_stride[0]); p.v_sh = step(p.Hk, cache->v_stride[1]);
+  p.pk_st = (int32_t)(step(p.P, cache->prefix_k_stride[1]) * 2); p.pv_st = (int32_t)(step(p.P, cache->prefix_v_stride[1]) * 2);
+  p.k_st = (int32_t)(step(p.cap, cache->k_stride[2]) * 2); p.v_st = (int32_t)(step(p.cap, cache->v_stride[2]) * 2);
   p.causal = causal != 0;
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->d)) * 1.4426950408889634f;
   p.decay = decay;
@@ -266,8 +270,8 @@ int dbsp_cache_evict(const dbsp_cache* cache, int32_t budget, int32_t sinks, con
   dbsp_cache_evict_params p = {};
   p.k = static_cast<unsigned char*>(cache->k); p.v = static_cast<unsigned char*>(cache->v);
   p.weights = cache->weights; p.positions = cache->positions; p.lens = cache->lens; p.keep_from = keep_from;
-  p.k_sb = cache->k_stride[0] * 2; p.k_sh = cache->k_stride[1] * 2; p.k_st = cache->k_stride[2] * 2;
-  p.v_sb = cache->v_stride[0] * 2; p.v_sh = cache->v_stride[1] * 2; p.v_st = cache->v_stride[2] * 2;
+  p.k_sb = step(size[0], cache->k_stride[0]) * 2; p.k_sh = step(size[1], cache->k_stride[1]) * 2; p.k_st = step(size[2], cache->k_stride[2]) * 2;
+  p.v_sb = step(size[0], cache->v_stride[0]) * 2; p.v_sh = step(size[1], cache->v_stride[1]) * 2; p.v_st = step(size[2], cache->v_stride[2]) * 2;
   p.B = cache->B; p.Hk = cache->Hk; p.cap = cache->capacity; p.row_bytes = cache->d * 2;
   p.budget = budget; p.sinks = sinks; p.max_moves = (int32_t)m.most; p.n_parts = (int32_t)m.parts;
   unsigned char* ws = static_cast<unsigned char*>(workspace);

@@ -55,8 +55,8 @@ def test_bad_caches_are_refused_by_every_entry_point(change, word):
 
 BAD_CALLS = [
     (dict(q=None), "null"), (dict(o=None), "null"), (dict(ws=None), "null"), (dict(H=0), "positive"), (dict(Nq=0), "positive"), (dict(q=FAKE + 8), "aligned"),
-    (dict(qs=(256, 64, 4)), "multiples of 8"), (dict(os_=(256, 0, 64)), "overlap"), (dict(os_=(64, 64, 64)), "overlap"), (dict(lse=FAKE + 1), "4-byte"),
-    (dict(q_lens=FAKE + 1), "4-byte"), (dict(scale=float("nan")), "softmax_scale"), (dict(scale=float("inf")), "softmax_scale"), (dict(decay=float("nan")), "decay"),
+    (dict(qs=(256, 4, 64)), "multiples of 8"), (dict(os_=(256, 0, 64)), "overlap"), (dict(os_=(64, 64, 64)), "overlap"), (dict(lse=FAKE + 1), "4-byte"),
+    (dict(q_lens=FAKE + 1), "4-byte"), (dict(scale=float("nan")), "softmax_scale"), (dict(scale=float("inf")), "softmax_scale"), (dict(scale=1e-35), "softmax_scale"), (dict(decay=float("nan")), "decay"),
     (dict(decay=float("inf")), "decay"), (dict(ws=FAKE + 16), "256-byte"), (dict(n=100), "holds 100 bytes"),
 ]
 

@@ -127,6 +127,12 @@ CASES = {
     "prompt_weights_in_parts": (1, 4, 2, 620, 64, 0, 700, [689], None, True, "bf16", 0.5),
     "frame_weights_in_parts": (1, 3, 1, 500, 128, 30, 700, [601], [433], False, "fp16", 1.0),
     "many_sequences": (300, 2, 1, 1, 64, 40, 20, [i % 21 for i in range(300)], None, True, "bf16", 1.0),
+    "many_sequences_in_parts": (100, 2, 1, 1, 64, 400, 300, [(7 * i) % 301 for i in range(100)], None, True, "fp16", 0.5),
+    "many_rows_in_parts": (40, 8, 2, 16, 64, 300, 60, [16 + i for i in range(40)], [i % 17 for i in range(40)], True, "bf16", 1.0),
+    "one_kv_head_of_40": (3, 40, 1, 1, 128, 500, 300, [300, 0, 65], None, True, "bf16", 1.0),
+    "one_kv_head_of_200": (2, 200, 1, 1, 64, 70, 300, [300, 129], None, True, "fp16", 1.0),
+    "rows_100": (3, 20, 2, 10, 128, 400, 200, [200, 10, 77], [10, 3, 0], True, "bf16", 0.0),
+    "frame_in_parts": (1, 2, 2, 300, 128, 2000, 700, [611], None, False, "bf16", 1.0),
     "long_prefix": (2, 4, 2, 1, 64, 5000, 100, [100, 57], None, True, "bf16", 1.0),
     "long_own": (1, 2, 1, 2, 128, 0, 7000, [6999], None, True, "fp16", 1.0),
     "one_head_many_parts": (1, 1, 1, 1, 64, 20000, 1000, [999], None, True, "bf16", 0.3),
@@ -186,6 +192,31 @@ def test_offsets_past_32_bits():
     near, far = (dbsp.cache_attn_fwd(dbsp.KVCache(prefix_k=a[0], prefix_v=b[0]), q) for a, b in ((k, v), (far_k, far_v)))
     assert torch.equal(near[0], far[0])
     check(q, k, v, None, None, [n], None, True, "bf16")
+
+
+def test_one_prefix_serves_batches_of_any_size():
+    import torch
+    import paper_2511_23113_amd as dbsp
+    cache = None
+    for B, Nq, q_lens in ((1, 3, [2]), (5, 3, [3, 0, 1, 2, 3]), (2, 300, [300, 170])):
+        q, _, _, pk, pv = make(B, 4, 2, Nq, 64, 400, 0, "bf16", 13)
+        if cache is None:
+            keep = pk, pv
+            cache = dbsp.KVCache(prefix_k=pk, prefix_v=pv)
+        o, lse = torch.full_like(q, 7.0), torch.full((B, 4, Nq), 7.0, device="cuda")
+        dbsp.cache_attn_fwd(cache, q, q_lens=torch.tensor(q_lens, dtype=torch.int32, device="cuda"), o=o, lse=lse)
+        compare(q, None, None, *keep, None, q_lens, True, "bf16", host(o), host(lse), None, None, None, 0.0)
+
+
+def test_strides_of_dimensions_of_one_say_nothing():
+    import torch
+    import paper_2511_23113_amd as dbsp
+    q, k, v, pk, pv = make(1, 1, 1, 1, 64, 1, 1, "bf16", 14)
+    lens = torch.ones(1, dtype=torch.int32, device="cuda")
+    want = dbsp.cache_attn_fwd(dbsp.KVCache(k, v, lens, pk, pv), q)
+    odd = [torch.as_strided(x, x.shape, (3,) * (x.dim() - 1) + (1,)) for x in (q, k, v, pk, pv)]
+    got = dbsp.cache_attn_fwd(dbsp.KVCache(*odd[1:3], lens, *odd[3:]), odd[0])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 def test_a_prefix_is_as_good_as_own_keys():
