@@ -122,7 +122,8 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool ca
   const int64_t rows = (int64_t)Nq * p.G, all_rows = rows * p.B, q_rows = (int64_t)p.B * Nq * H;
   if (rows > kMost || all_rows > kMost || q_rows > INT_MAX) return fail(who, DBSP_ESHAPE, "too many queries");
   p.pre_tiles = (p.P + kCacheKeys - 1) / kCacheKeys;
-  p.pooled = p.pre_tiles > kCacheWhole && p.B > 1 && rows < kCacheRows;
+  const int64_t tiles = p.pre_tiles + (int64_t)(p.cap + kCacheKeys - 1) / kCacheKeys;
+  p.pooled = tiles > kCacheWhole && p.pre_tiles > kPooledFrom && p.B > 1 && rows < kCacheRows;
   p.pre_row_tiles = p.pooled ? (int32_t)((all_rows + kCacheRows - 1) / kCacheRows) : 0;
   p.many = rows > kCacheRows;
   p.own_tile_rows = p.many ? kLongRows : kCacheRows;

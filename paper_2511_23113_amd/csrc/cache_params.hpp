@@ -12,7 +12,8 @@ constexpr int kLongSlots = 256;       // of them at a time at d = 128: a compute
 constexpr int kCacheKeys = 64;         // keys of a tile
 constexpr int kCacheTarget = 1024;     // items that a launch is cut into where there is enough to cut, see cache_attn.hip
 
-constexpr int kCacheWhole = 4;         // tiles that are not cut, and prefixes that are not read for the whole batch at once
+constexpr int kCacheWhole = 10;        // tiles that are not cut, and
+constexpr int kPooledFrom = 4;         // prefixes that are not read for the whole batch at once
 constexpr int kScoreRows = 48;         // rows of a (sequence, KV head) up to which scores are kept for the weights, at d = 128; half as many at d = 64
 constexpr int kWeightKeys = 256;       // own keys of a workgroup that forms their scores anew
 constexpr int kMergeRows = 4096;       // rows up to which a workgroup joins the parts of one
