@@ -80,7 +80,10 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // Of a launch of n row tiles on a chip that holds `slots` workgroups at a time.  They have `tiles` key tiles each: whole rounds of row
 // tiles go as they are, and the last one or two are cut into parts that fill their rounds.  Or causality leaves the first
 // ones `span` fewer: then the longest go first, and all are cut if the longest alone would outlast the others' share.
-// What an item costs beside its tiles, in tiles: kStart, and kPart more for a part (its result goes to memory and back).
+// us, in a run / longest first: 48 heads, 4101 causal queries at d = 64 187 / 168 (160 with the part tile in front, row_shift), 16 heads
+// of 8192 339 / 263; 40 heads, 1560 queries behind 12,870 keys 1250 uncut but for 1024 items, 1101 so.
+// What an item costs beside its tiles, in tiles: kStart, and kPart more for a part (its result goes to memory and back; 4 and 16
+// choose the same cuts but for half a per cent).
 constexpr double kStart = 2, kPart = 8;
 dbsp_cache_long_cut cut_long(int64_t n, int64_t tiles, int64_t span, int slots) {
   const int dies = n < 64 ? 1 : 8;         // few row tiles: their parts go to all dies

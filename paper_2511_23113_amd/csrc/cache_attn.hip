@@ -15,11 +15,16 @@
 // Parts leave partial results (O, and LSE to base 2, in f32) that a second launch joins: LSE = log sum exp LSE_i,
 // O = sum exp(LSE_i - LSE) O_i.  Items of the same keys lie next to each other and on the same die (workgroup number mod 8).
 //
-// A workgroup is four waves of 32 queries each.  Tiles of 64 keys go to the LDS directly (global_load_lds_dwordx4), two in
-// turn, one barrier a tile.  Products are formed transposed, S^T = K Q^T and O^T = V^T P^T, with 32x32x16 MFMAs: lane r holds
-// query r; the packed probabilities are the second product's operand as they lie, and V^T comes from transposing LDS reads
-// (the layouts are those of attn_fwd.hip).  Probabilities are rounded to the inputs' type for that product, as they
-// must be for the matrix pipe: half a step of it relative to each; sums are of the f32 values.
+// A workgroup is four waves.  Tiles of 64 keys go to the LDS directly (global_load_lds_dwordx4), two in turn.  Products are formed
+// transposed, S^T = K Q^T and O^T = V^T P^T: a lane holds a query, the packed probabilities are the second product's operand as they
+// lie, and V^T comes from transposing LDS reads (the layouts are those of attn_fwd.hip).  Up to 32 rows are given to all waves, which
+// share the keys (few_rows); more are dealt to them, 32 each (the kernel).  Probabilities are rounded to the inputs' type for the second
+// product, as they must be for the matrix pipe: half a step of it relative to each; sums are of the f32 values.
+//
+// Bound by reading K and V once.  32 sequences of 32 heads on 8 KV heads over 4400 own keys each (577 MB): 120 us, 4.8 TB/s, where a large copy
+// reaches 5.0; 8 KV heads over 123,000 keys (506 MB) 95 us, 5.3 TB/s; without any of its arithmetic the kernel takes 3 to 8 % less.
+// 64 sequences of 40 heads on 8 behind 16,384 shared keys, 605 MB in all: 131 us, 4.6 TB/s; there the prefix's rows fill 3 tiles of 128 a KV
+// head, bound by the matrix pipe, and run beside own keys on every die: 152 us with the prefix on the first dies alone.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -32,7 +37,8 @@ namespace {
 // tokens, tiles of the prefix in front of the own ones, and the item's tiles.
 struct Span { int b, hk, row0, rows, len, q_len, pre_tiles, t0, t1; };
 
-// Row tiles of at most 16 NR rows, the form for single tokens: bound by the stream of K and V.  The keys of a tile are dealt to the
+// Row tiles of at most 16 NR rows, the form for single tokens: bound by the stream of K and V (with 32 rows a wave, three of the four
+// waves idle, single rows over 4400 keys took 134 us where they take 120).  The keys of a tile are dealt to the
 // waves, 16 each, with 16 x 16 MFMAs: lane (n, g) of 16 x 4 has row n and keys 4 g .. 4 g + 3, and the packed probabilities
 // are the second product's operand again.  A wave reads what it has copied itself, so no barrier couples the waves; each has
 // statistics of its own, against which it forms its probabilities as they stand (the max is raised where one passes kRaiseAt), and
@@ -393,7 +399,8 @@ __device__ __forceinline__ Parts parts_of(const dbsp_cache_attn_params& p, int b
 
 // Behind the attention kernel.  The first p.merge_groups workgroups join partial results, D / 4 lanes a part of a row, four values
 // each: WAYS of them a row, which take its parts in turn (rows are few where parts are many).  The others sum the
-// weights from the scores that the attention kernel has kept, 1024 slots of a (sequence, KV head) each.
+// weights from the scores that the attention kernel has kept, 1024 slots of a (sequence, KV head) each.  Bound by latencies: 6 us behind
+// 384 rows of 9 parts and as many (sequence, head) pairs of 1500 keys, 9 us behind 96 rows of 205 parts.
 template <class T, int D, int WAYS>
 __device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
   constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, U = WAYS > 1 ? 8 : 4;

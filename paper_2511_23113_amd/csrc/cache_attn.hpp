@@ -13,7 +13,7 @@
 namespace {
 
 // Probabilities are formed against a running max as it stands, and may pass 1 by this (a single one, or a lane's sum of 16) before it
-// is raised: f32 sums hold that as they hold 1, and so do fp16's 65504 and its 2^-14 at the other end.
+// is raised: f32 sums hold that as they hold 1, and so do fp16's 65504 and its 2^-14 at the other end.  (64: 2 % slower)
 constexpr float kRaiseAt = 1024.f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -150,7 +150,8 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
     for (int i = 0; i < WAVES; ++i) own += tile_sum[i];
   }
   const int64_t total = own * unit + (p.pooled ? (int64_t)p.Hk * p.pre_row_tiles * p.pre_tiles : 0);
-  // (of short key lists up to four tiles an item as long as there are 256 of them: every part costs the merge)
+  // (of short key lists up to four tiles an item as long as there are 256 of them, as every part costs the merge: 8 heads over 7600
+  // keys 23.3 us with one tile an item, 17.9 with two, 16.3 with four)
   const int chunk = (int)max(max((int64_t)1, min((int64_t)4, total / 256)), min((int64_t)(1 << 30), (total + kCacheTarget - 1) / kCacheTarget));
   auto parts = [&](int n) { return max(1, (n + chunk - 1) / chunk); };
   int mine = 0;

@@ -5,15 +5,16 @@
 // budget moves into the hole that an evicted one leaves in front of it, both in ascending order.  Sources (slots >= budget) and
 // destinations (slots < budget) are disjoint, so rows move in place, in parallel, and only those that have to.
 //
-// Choosing goes by the weights' order-preserving 32-bit images, of which the budget-th largest is the limit.
-//   * Up to 32,768 slots a workgroup has a (sequence, head), all its images in registers, read once.  The limit is built from the
-//     top, two bits at a time, by counting the images that reach each of three candidates (ballots; one exchange of the waves'
-//     counts a step), until a candidate leaves exactly the budget.  That takes as long whatever the weights are; counts by
-//     digit in the LDS, 8 bits a pass, took 46 us of 16,500 slots where these take FIXME, as weights of like size meet in a few
-//     of the counters.
-//   * Longer ones are cut into workgroups of 8192 slots: three launches count digits of 11, 11 and 10 bits, a fourth what
-//     each part keeps, a fifth lists holes and fillers.  Whole numbers are added, so their order of arrival does not matter.
-// A last launch moves the rows of K and V.
+// Choosing goes by the weights' order-preserving 32-bit images, of which the budget-th largest is the limit: counts by digits of 11, 11
+// and 10 bits from the top, the second and third only among images that agree with the limit so far.  Whole numbers are added, so
+// their order of arrival does not matter.
+//   * Up to 32,768 slots a workgroup has a (sequence, head), its images in registers, read once, and the counts in the LDS; it
+//     stops at the digit at which all images that have it stay.  256 heads of 2064 slots: 9 us, of which the exchanges of a workgroup of 16
+//     waves are most; 96 of 11,500 slots: 21 us, by instructions (46 with four digits of 8 bits, read anew for each; two bits
+//     a step by ballots took 18 and 37).
+//   * Longer ones are cut into workgroups of 8192 slots: three launches count, a fourth counts what each part keeps, a fifth
+//     lists holes and fillers, 5 to 9 us each.  8 heads of 131,100 slots: 69 us with the moves, 431 by a workgroup a head.
+// A last launch moves the rows, bound by memory: 96 heads, 1700 rows of 512 bytes each and back (167 MB) 38 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

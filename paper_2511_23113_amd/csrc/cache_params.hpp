@@ -6,19 +6,35 @@
 
 #include <cstdint>
 
-constexpr int kCacheRows = 128;        // queries of a workgroup: four waves of 32
-constexpr int kLongWaves = 4, kLongRows = 64 * kLongWaves;      // those of cache_attn_long.hip: waves of 64
-constexpr int kLongSlots = 256;       // of them at a time at d = 128: a compute unit each; at d = 64 twice as many
 constexpr int kCacheKeys = 64;         // keys of a tile
-constexpr int kCacheTarget = 1024;     // items that a launch is cut into where there is enough to cut, see cache_attn.hip
-
-constexpr int kCacheWhole = 10;        // tiles that are not cut, and
-constexpr int kPooledFrom = 4;         // prefixes that are not read for the whole batch at once
-constexpr int kScoreRows = 48;         // rows of a (sequence, KV head) up to which scores are kept for the weights, at d = 128; half as many at d = 64
-constexpr int kWeightKeys = 256;       // own keys of a workgroup that forms their scores anew
-constexpr int kMergeRows = 4096;       // rows up to which a workgroup joins the parts of one
-constexpr int kEvictWhole = 32768;     // slots that a workgroup chooses among by itself, and those of a part where there are more
-constexpr int kEvictPart = 8192;
+constexpr int kCacheRows = 128;        // rows of a workgroup of the kernel for few queries: four waves of 32
+// Of the kernel for many queries: waves of 64 rows (two of them a workgroup: frames of 1560 queries 1.5 % slower, though they
+// leave 6 % of the rows of their tiles empty and not 13, causal prompts 1.6 % faster).  It takes over where a (sequence, KV head) has more
+// than kCacheRows rows.  us, by the kernel for few / for many: 128 such of 300 rows 39.6 / 22.5, 160 of 150 rows over 1000
+// keys 58 / 39, 8 of 1000 rows 25.4 / 29.9 (too few for either).
+constexpr int kLongWaves = 4, kLongRows = 64 * kLongWaves;
+constexpr int kLongSlots = 256;        // of its workgroups at a time at d = 128: a compute unit each; at d = 64 twice as many
+// Items that a launch is cut into where there is enough to cut: two rounds of the chip at d = 128, one at d = 64.  us with 512 / 1024 /
+// 2048 / 4096: 384 (sequence, head) pairs of 1500 own keys behind 4096 shared ones 89 / 85 / 88 / 96, 4 heads' prefix of 131,072 84 /
+// 84 / 98 / 123, 256 pairs of 4400 keys 143 / 135 / 130 / 145, 240 pairs of 21 rows 32 / 31 / 35 / 45.
+constexpr int kCacheTarget = 1024;
+// Tiles that are not cut: a launch less, and the merge.  us with 4 / 8 / 16: 256 pairs of 8 tiles 18.3 / 12.4 / 12.4, 8 pairs of 8 tiles
+// 11.4 / 9.7 / 9.7, of 16 tiles 10.5 / 10.5 / 14.0.
+constexpr int kCacheWhole = 10;
+// Prefix tiles that every sequence reads for itself.  us with 2 / 4 / 8: 256 pairs of 5 tiles behind 6 prefix tiles 46 / 46 / 50, 1024 of
+// 24 tiles behind 4 148 / 143 / 143, behind 8 149 / 149 / 151.
+constexpr int kPooledFrom = 4;
+// Rows of a (sequence, KV head) up to which scores are kept for the weights, at d = 128 (half as many at d = 64): they are written and read,
+// 8 bytes a row and key, where forming them anew reads 2 d bytes a key, from memory or a cache.  us, anew / kept: 128 pairs of
+// 1500 keys at d = 128 16 rows 60 / 46, 32 rows 69 / 59, 64 rows 74 / 81; at d = 64 16 rows 41 / 30, 32 rows 46 / 40; 512 pairs of
+// 6000 keys at d = 64 16 rows 349 / 294, 32 rows 347 / 392.
+constexpr int kScoreRows = 48;
+constexpr int kWeightKeys = 256;       // own keys of a workgroup that forms their scores anew: 64 a wave
+// Rows up to which a workgroup joins the parts of one, else of 8 or 16.  us with 1024 / 4096 / 8192: 5040 rows of 7 parts at d = 64
+// 27.1 / 27.1 / 34.3; 96 rows of 205 parts took 53 us of a launch by the eight, and take 9.
+constexpr int kMergeRows = 4096;
+constexpr int kEvictWhole = 32768;     // slots that a workgroup chooses among by itself: what its registers hold; and those of a
+constexpr int kEvictPart = 8192;       // part where there are more
 
 // How a launch of the kernel for many queries is cut: its row tiles, `per` for each of `dies` dies (workgroup number mod 8), of which
 // the first `whole` are one item each and the `tail` others `k` parts, so that the last round of workgroups ends together.

@@ -7,7 +7,10 @@
 // time in three places (64 keys a wave, as each operand of Q then feeds two MFMAs).  As in cache_attn_long.hip a step is a sequence
 // of fenced sub-slots: an MFMA of the next step's S^T = K Q^T, two exponentials of this one's, an operand read.  Lane r has
 // row r of a step and sums 32 keys; the lanes are added once, at the end.  Where there are fewer workgroups than the chip
-// holds the rows are cut into p.row_parts, whose sums a small launch adds.
+// holds the rows are cut into p.row_parts, whose sums a small launch adds (2 KV heads of 4 query heads each, 4096 causal queries: 387 us
+// attention included without, 120 so).
+// Measured: 80 (sequence, head) pairs of 4680 keys and 1560 queries (150 GFLOP) 195 us, 770 TFLOP/s; with 32 keys a wave and Q by way of
+// registers 320.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
