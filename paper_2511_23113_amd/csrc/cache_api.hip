@@ -97,19 +97,26 @@ dbsp_cache_long_cut cut_long(int64_t n, int64_t tiles, int64_t span, int slots) 
     best.tail = (int32_t)(k > 1 ? per - whole : 0);
     best.k = (int32_t)k;
   };
+  // the parts that fill 1 .. 6 rounds with n row tiles (fewer parts of as many rounds only leave places empty)
+  auto fills = [&](int64_t n, int64_t round) { return std::min(round * room / std::max<int64_t>(n, 1), tiles / 2); };
   double least = 1e300;
   if (longest_first) {
     const double work = (double)per * (tiles - 0.5 * span), longest = (double)tiles;
-    for (int64_t k = 1; k == 1 || (2 * k <= tiles && per * k <= 6 * room); ++k) {
+    auto cost = [&](int64_t k) {
       const double more = kStart + (k > 1 ? kPart : 0);
-      take(std::max((work + per * k * more) / room, longest / k + more) + 0.15 * longest / k, least, 0, k);
-    }
+      return std::max((work + per * k * more) / room, longest / k + more) + 0.15 * longest / k;
+    };
+    take(cost(1), least, 0, 1);
+    for (int64_t k = 2; k <= 4 && k <= tiles / 2; ++k) take(cost(k), least, 0, k);
+    for (int64_t round = 1; round <= 6; ++round)
+      if (const int64_t k = fills(per, round); k > 4) take(cost(k), least, 0, k);
     return best;
   }
   least = (double)((per + room - 1) / room) * (tiles + kStart);
   for (int64_t whole = per / room * room; whole >= 0 && whole + 2 * room > per; whole -= room)
-    for (int64_t k = 2; per > whole && 2 * k <= tiles && (per - whole) * k <= 6 * room; ++k)
-      take((double)(whole / room) * (tiles + kStart) + (double)(((per - whole) * k + room - 1) / room) * ((tiles + k - 1) / k + kStart + kPart), least, whole, k);
+    for (int64_t round = 1; round <= 6 && per > whole; ++round)
+      if (const int64_t k = fills(per - whole, round); k > 1)
+        take((double)(whole / room) * (tiles + kStart) + (double)round * ((tiles + k - 1) / k + kStart + kPart), least, whole, k);
   return best;
 }
 

@@ -288,6 +288,43 @@ def test_a_captured_call_follows_the_lengths_of_each_replay():
         assert torch.equal(o, o2) and torch.equal(lse, lse2) and torch.equal(cache.weights, other.weights)
 
 
+def test_two_captured_calls_may_share_a_workspace_that_they_use_in_turn():
+    import torch
+    import paper_2511_23113_amd as dbsp
+    states = [_state(s) for s in (51, 52)]
+    caches = [dbsp.KVCache(k, v, lens, pk, pv, weights=w) for q, k, v, lens, pk, pv, w in states]
+    ws = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    outs = [(torch.empty_like(s[0]), torch.empty(5, 6, 3, device="cuda")) for s in states]
+    graphs = []
+    for c, s, (o, lse) in zip(caches, states, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            dbsp.cache_attn_fwd(c, s[0], decay=0.0, o=o, lse=lse, workspace=ws)
+    want = [(*dbsp.cache_attn_fwd(c, s[0], decay=0.0), c.weights.clone()) for c, s in zip(caches, states)]
+    for step in range(6):
+        i = (0, 1, 1, 0, 1, 0)[step]
+        outs[i][0].zero_()
+        caches[i].weights.zero_()
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        got, used = (*outs[i], caches[i].weights), torch.arange(800, device="cuda") < states[i][3][:, None, None]
+        assert torch.equal(got[0], want[i][0]) and torch.equal(got[1], want[i][1]) and torch.equal(got[2] * used, want[i][2] * used)
+
+
+def test_no_slots_and_no_prefix():
+    import torch
+    import paper_2511_23113_amd as dbsp
+    q, k, v, pk, pv = make(2, 2, 2, 3, 64, 5, 7, "bf16", 15)
+    empty, none = torch.empty(2, 2, 0, 64, dtype=q.dtype, device="cuda"), torch.empty(2, 0, 64, dtype=q.dtype, device="cuda")
+    lens = torch.tensor([4, 7], dtype=torch.int32, device="cuda")
+    for cache, other in ((dbsp.KVCache(empty, empty, lens * 0, pk, pv), dbsp.KVCache(prefix_k=pk, prefix_v=pv)),
+                         (dbsp.KVCache(k, v, lens, none, none), dbsp.KVCache(k, v, lens))):
+        a, b = dbsp.cache_attn_fwd(cache, q), dbsp.cache_attn_fwd(other, q)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    o, lse = dbsp.cache_attn_fwd(dbsp.KVCache(empty, empty, lens * 0, none, none), q)
+    assert (o == 0).all() and (lse == -float("inf")).all()
+
+
 def test_two_streams_at_once_and_a_stream_by_argument():
     import torch
     import paper_2511_23113_amd as dbsp
