@@ -147,11 +147,18 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool ca
   const int64_t span = causal ? std::min(Nq, c->capacity) / kCacheKeys : 0;
   if (many) p.cut = cut_long(row_tiles, most_tiles, span, (c->d == 128 ? 1 : 2) * kLongSlots * 4 / kLongWaves);
   p.row_shift = many && p.cut.longest_first && p.own_row_tiles > 1 ? (int32_t)(p.own_row_tiles * (int64_t)kLongRows - rows) : 0;
-  // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kCacheTarget of them
-  const int64_t pre_items = std::min(pre_unit * p.pre_tiles, kCacheTarget + pre_unit);
-  const int64_t own_items = many ? (int64_t)p.cut.dies * p.cut.tail * p.cut.k : p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), kCacheTarget + row_tiles) : row_tiles;
+  // Rows leave as many partial results: of more than 32 a (sequence, KV head) parts are fewer, 256 items at d = 128 and 512 at d = 64
+  // (us with 1024: 8 heads of 128 rows over 57,000 keys 80 / 59, 128 pairs of 100 rows 92 / 76, 256 of 33 rows 87 / 74, 128 of 48
+  // rows 56 / 59, at d = 64 16 heads of 64 rows over 57,000 keys 56 / 54), and those of a prefix whose rows fill tiles where the own
+  // rows do not have twice the keys of an own one (64 sequences of 5 rows behind 16,384 keys 131 / 122, 40 of 25 rows 67 / 63; four
+  // times 171 and 73).
+  p.target = rows <= 32 ? kCacheTarget : kCacheTarget * 32 / c->d;
+  p.pre_longer = rows <= 32 && all_rows > 32 ? 2 : 1;
+  // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / target of them
+  const int64_t pre_items = std::min(pre_unit * p.pre_tiles, p.target + pre_unit);
+  const int64_t own_items = many ? (int64_t)p.cut.dies * p.cut.tail * p.cut.k : p.split ? std::min(row_tiles * std::max<int64_t>(most_tiles, 1), p.target + row_tiles) : row_tiles;
   if (many) cut.grid = (int64_t)p.cut.dies * (p.cut.whole + (int64_t)p.cut.tail * p.cut.k);
-  else if (p.split) cut.grid = round_up(std::min(pre_items + own_items, kCacheTarget + pre_unit + row_tiles), 8) + 16;      // (dies' shares of two lists, rounded up)
+  else if (p.split) cut.grid = round_up(std::min(pre_items + own_items, p.target + pre_unit + row_tiles), 8) + 16;      // (dies' shares of two lists, rounded up)
   else cut.grid = round_up(row_tiles, 8);
   if (cut.grid > kMost || pre_items > kMost / kCacheRows) return fail(who, DBSP_ESHAPE, "too many queries");
   p.max_pre_items = p.pooled ? (int32_t)pre_items : 0;

@@ -11,7 +11,7 @@
 // and the own keys by each sequence's rows apart; else a row tile goes over the prefix and then over its own keys.
 //
 // Items.  An item is a row tile and a range of its key tiles.  Lengths are known on the device only, so every workgroup
-// works out from them how the launch is cut: about kCacheTarget items of equally many tiles, each sequence into equal parts.
+// works out from them how the launch is cut: about p.target items of equally many tiles, each sequence into equal parts.
 // Parts leave partial results (O, and LSE to base 2, in f32) that a second launch joins: LSE = log sum exp LSE_i,
 // O = sum exp(LSE_i - LSE) O_i.  Items of the same keys lie next to each other and on the same die (workgroup number mod 8).
 //
@@ -23,8 +23,8 @@
 //
 // Bound by reading K and V once.  32 sequences of 32 heads on 8 KV heads over 4400 own keys each (577 MB): 120 us, 4.8 TB/s, where a large copy
 // reaches 5.0; 8 KV heads over 123,000 keys (506 MB) 95 us, 5.3 TB/s; without any of its arithmetic the kernel takes 3 to 8 % less.
-// 64 sequences of 40 heads on 8 behind 16,384 shared keys, 605 MB in all: 131 us, 4.6 TB/s; there the prefix's rows fill 3 tiles of 128 a KV
-// head, bound by the matrix pipe, and run beside own keys on every die: 152 us with the prefix on the first dies alone.
+// 64 sequences of 40 heads on 8 behind 16,384 shared keys, 605 MB in all: 122 us, 5.0 TB/s; there the prefix's rows fill 3 tiles of 128 a KV
+// head, bound by the matrix pipe, and run beside own keys on every die (20 us more with the prefix on the first dies alone).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

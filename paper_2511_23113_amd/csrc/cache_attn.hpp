@@ -152,7 +152,7 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
   const int64_t total = own * unit + (p.pooled ? (int64_t)p.Hk * p.pre_row_tiles * p.pre_tiles : 0);
   // (of short key lists up to four tiles an item as long as there are 256 of them, as every part costs the merge: 8 heads over 7600
   // keys 23.3 us with one tile an item, 17.9 with two, 16.3 with four)
-  const int chunk = (int)max(max((int64_t)1, min((int64_t)4, total / 256)), min((int64_t)(1 << 30), (total + kCacheTarget - 1) / kCacheTarget));
+  const int chunk = (int)max(max((int64_t)1, min((int64_t)4, total / 256)), min((int64_t)(1 << 30), (total + p.target - 1) / p.target));
   auto parts = [&](int n) { return max(1, (n + chunk - 1) / chunk); };
   int mine = 0;
   for (int b = b0; b < b1; ++b) mine += parts(own_tiles(p, b));
@@ -167,7 +167,7 @@ __device__ __forceinline__ bool find_item(const dbsp_cache_attn_params& p, Item&
       all += part_sum[i];
     }
   }
-  const int pre_parts = p.pooled ? parts(p.pre_tiles) : 0, pre_items = p.Hk * p.pre_row_tiles * pre_parts;
+  const int pre_parts = p.pooled ? max(1, (p.pre_tiles + chunk * p.pre_longer - 1) / (chunk * p.pre_longer)) : 0, pre_items = p.Hk * p.pre_row_tiles * pre_parts;
   int first = before + upto - mine;        // parts of the sequences before this thread's
   if (blockIdx.x == 0 && (w == 0 || !by_wave)) {      // for the merge
     if (t == 0) { p.table[0] = pre_parts; p.table[1] = pre_items; }

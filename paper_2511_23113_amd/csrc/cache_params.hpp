@@ -56,6 +56,8 @@ struct dbsp_cache_attn_params {
   int32_t many;                        // the kernel of cache_attn_long.hip
   int32_t pooled;                      // the prefix is read by the rows of all sequences together, own keys apart
   int32_t split;                       // items may be parts of a row tile's keys: partial results, and a merge behind the kernel (kernel for few queries)
+  int32_t target;                      // items that the launch is cut into where there is enough to cut
+  int32_t pre_longer;                  // times the tiles of an own item that one of the pooled prefix has
   int32_t pre_tiles;                   // tiles of the prefix
   int32_t pre_row_tiles, own_row_tiles;            // row tiles of a KV head: of all sequences together (pooled), of one sequence
   int32_t own_tile_rows;               // rows of an own item: kCacheRows, or kLongRows for the kernel of cache_attn_long.hip
