@@ -14,7 +14,8 @@
 //     a step by ballots took 18 and 37).
 //   * Longer ones are cut into workgroups of 8192 slots: three launches count, a fourth counts what each part keeps, a fifth
 //     lists holes and fillers, 5 to 9 us each.  8 heads of 131,100 slots: 69 us with the moves, 431 by a workgroup a head.
-// A last launch moves the rows, bound by memory: 96 heads, 1700 rows of 512 bytes each and back (167 MB) 38 us, 4.4 TB/s.
+// A last launch moves the rows, 64 moves of a workgroup in flight at once, bound by memory: 96 heads, 1700 rows of K and V each (167 MB
+// read and written) 38 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -26,7 +27,10 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMovesPerGroup = 64;
-constexpr int kNT = 1024;              // threads that choose
+// Threads that choose: 256 up to 1024 slots, kMidThreads up to 4096, kNT from there on.  us with 1024 / 512 / 256: 2048 (sequence, head) pairs of
+// 750 slots 87 / - / 65, of 3000 slots 179 / 160 / 164, 256 of 2064 15.5 / 15.5 / 19, 16 of 3800 14.3 / 15.1 / 19.6.
+constexpr int kNT = 1024;
+constexpr int kMidThreads = 512;
 
 // Larger weight, larger image; what must stay comes last.
 __device__ __forceinline__ uint32_t image(float w, bool stays) {
@@ -150,42 +154,58 @@ __device__ __forceinline__ void list_moves(const uint32_t (&x)[R], int first, in
 
 // Counts digit PASS of the `here` images that agree with `limit` above it: hist, 2048 zeros before.
 constexpr int kDigits = 2048, kShift[3] = {21, 10, 0};
-template <int PASS, int R>
+template <int PASS, int NT, int R>
 __device__ __forceinline__ void count_digits(const uint32_t (&x)[R], int here, uint32_t limit, uint32_t* hist) {
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    if (j * kNT >= here) break;
+    if (j * NT >= here) break;
     const bool in = x[j] != 0u && (PASS == 0 || (x[j] ^ limit) >> kShift[PASS ? PASS - 1 : 0] == 0u);
     if (in) atomicAdd(&hist[x[j] >> kShift[PASS] & (PASS == 2 ? 1023 : 2047)], 1u);
   }
 }
 
-// Two of a digit's 2048 counts: thread 0 has those of the largest digits.
-struct two { uint32_t hi, lo; };
-__device__ __forceinline__ two my_digits(const uint32_t* counts) { return {counts[kDigits - 1 - 2 * threadIdx.x], counts[kDigits - 2 - 2 * threadIdx.x]}; }
+// A thread's share of a digit's 2048 counts: thread 0 has those of the largest digits, the largest first.
+template <int NT>
+struct Share { uint32_t c[kDigits / NT]; };
+template <int NT>
+__device__ __forceinline__ Share<NT> my_digits(const uint32_t* counts) {
+  constexpr int PER = kDigits / NT;
+  Share<NT> s;
+#pragma unroll
+  for (int y = 0; y < PER; ++y) s.c[y] = counts[kDigits - 1 - PER * (int)threadIdx.x - y];
+  return s;
+}
 
 // Of the images whose upper bits are those of `limit`: the digit below them at which `left` of them, from the largest on, are
 // reached.  limit and left are brought up to date; returns how many have the chosen digit.  (PASS: its own places in the LDS)
-template <int PASS>
-__device__ __forceinline__ uint32_t pick_digit(two counts, uint32_t& limit, uint32_t& left) {
-  __shared__ uint32_t wave_sum[kNT / 64], got[3];
+template <int PASS, int NT>
+__device__ __forceinline__ uint32_t pick_digit(const Share<NT>& s, uint32_t& limit, uint32_t& left) {
+  constexpr int PER = kDigits / NT;
+  __shared__ uint32_t wave_sum[NT / 64], got[3];
   const int t = threadIdx.x, w = t >> 6, l = t & 63;
-  const uint32_t hi = counts.hi, lo = counts.lo;
-  uint32_t upto = hi + lo;
-  for (int s = 1; s < 64; s <<= 1) {
-    const uint32_t o = __shfl_up(upto, s);
-    if (l >= s) upto += o;
+  uint32_t mine = 0;
+#pragma unroll
+  for (int y = 0; y < PER; ++y) mine += s.c[y];
+  uint32_t upto = mine;
+  for (int x = 1; x < 64; x <<= 1) {
+    const uint32_t o = __shfl_up(upto, x);
+    if (l >= x) upto += o;
   }
   if (l == 63) wave_sum[w] = upto;
   __syncthreads();
-  uint32_t before = upto - hi - lo;
+  uint32_t before = upto - mine;
 #pragma unroll
-  for (int y = 0; y < kNT / 64; ++y) before += y < w ? wave_sum[y] : 0u;
-  if (before < left && left <= before + hi + lo) {
-    const bool first = left <= before + hi;
-    got[0] = kDigits - 1 - 2 * t - (first ? 0 : 1);
-    got[1] = left - before - (first ? 0 : hi);
-    got[2] = first ? hi : lo;
+  for (int y = 0; y < NT / 64; ++y) before += y < w ? wave_sum[y] : 0u;
+  if (before < left && left <= before + mine) {
+#pragma unroll
+    for (int y = 0; y < PER; ++y) {
+      if (before < left && left <= before + s.c[y]) {
+        got[0] = kDigits - 1 - PER * t - y;
+        got[1] = left - before;
+        got[2] = s.c[y];
+      }
+      before += s.c[y];
+    }
   }
   __syncthreads();
   limit |= got[0] << kShift[PASS];
@@ -193,11 +213,11 @@ __device__ __forceinline__ uint32_t pick_digit(two counts, uint32_t& limit, uint
   return got[2];
 }
 
-template <int R>
-__global__ __launch_bounds__(kNT) void dbsp_cache_choose_kernel(const dbsp_cache_evict_params p) {
-  static_assert(R <= 32 && kNT * R <= kEvictWhole, "16 bits a count, a bit a slot");
+template <int NT, int R>
+__global__ __launch_bounds__(NT) void dbsp_cache_choose_kernel(const dbsp_cache_evict_params p) {
+  static_assert(R <= 32 && NT * R <= kEvictWhole, "16 bits a count, a bit a slot");
   __shared__ uint32_t hist[3 * kDigits];
-  __shared__ int table[R * kNT / 64 + 1];
+  __shared__ int table[R * NT / 64 + 1];
   const int pair = blockIdx.x, t = threadIdx.x;
   const int n = used_of(p, pair), budget = p.budget;
   if (n <= budget) {
@@ -205,28 +225,28 @@ __global__ __launch_bounds__(kNT) void dbsp_cache_choose_kernel(const dbsp_cache
     return;
   }
   uint32_t x[R];
-  load_images<kNT, R>(p, pair, 0, n, x);
-  for (int i = t; i < 3 * kDigits; i += kNT) hist[i] = 0;
+  load_images<NT, R>(p, pair, 0, n, x);
+  for (int i = t; i < 3 * kDigits; i += NT) hist[i] = 0;
   __syncthreads();
   // `left` of the `equal` images that have the limit's digits so far stay, and all above them
   uint32_t limit = 0, left = (uint32_t)budget;
-  count_digits<0, R>(x, n, limit, hist);
+  count_digits<0, NT, R>(x, n, limit, hist);
   __syncthreads();
-  uint32_t equal = pick_digit<0>(my_digits(hist), limit, left);
+  uint32_t equal = pick_digit<0>(my_digits<NT>(hist), limit, left);
   if (equal != left) {
-    count_digits<1, R>(x, n, limit, hist + kDigits);
+    count_digits<1, NT, R>(x, n, limit, hist + kDigits);
     __syncthreads();
-    equal = pick_digit<1>(my_digits(hist + kDigits), limit, left);
+    equal = pick_digit<1>(my_digits<NT>(hist + kDigits), limit, left);
   }
   if (equal != left) {
-    count_digits<2, R>(x, n, limit, hist + 2 * kDigits);
+    count_digits<2, NT, R>(x, n, limit, hist + 2 * kDigits);
     __syncthreads();
-    equal = pick_digit<2>(my_digits(hist + 2 * kDigits), limit, left);
+    equal = pick_digit<2>(my_digits<NT>(hist + 2 * kDigits), limit, left);
   }
   int32_t *holes = p.holes + (int64_t)pair * p.max_moves, *fillers = p.fillers + (int64_t)pair * p.max_moves;
   float* weights = p.weights + (int64_t)pair * p.cap;
   int n_holes, n_fillers;
-  list_moves<kNT, R>(x, 0, n, budget, limit, (int)left, equal != left, 0, table,
+  list_moves<NT, R>(x, 0, n, budget, limit, (int)left, equal != left, 0, table,
                      [&](int, int i, bool hole, bool filler, bool goes, int rank) {
                        if (hole) holes[rank] = i;
                        if (filler) fillers[rank] = i;
@@ -260,14 +280,14 @@ __global__ __launch_bounds__(kNT) void dbsp_cache_part_kernel(const dbsp_cache_e
   uint32_t* digits = p.digits + (int64_t)pair * 3 * kDigits;
   uint32_t limit = 0, left = (uint32_t)budget, equal = 0;
   uint32_t* chosen = p.chosen + pair * 3;
-  two counts[PASS > 0 && PASS < 4 ? PASS : 1];
+  Share<kNT> counts[PASS > 0 && PASS < 4 ? PASS : 1];
   if constexpr (PASS == 4) {
     limit = chosen[0];
     left = chosen[1];
     equal = chosen[2];
   }
 #pragma unroll
-  for (int y = 0; y < PASS && PASS < 4; ++y) counts[y] = my_digits(digits + y * kDigits);
+  for (int y = 0; y < PASS && PASS < 4; ++y) counts[y] = my_digits<kNT>(digits + y * kDigits);
   load_images<kNT, kR>(p, pair, first, n, x);
   if constexpr (PASS > 0 && PASS < 4) equal = pick_digit<0>(counts[0], limit, left);
   if constexpr (PASS > 1 && PASS < 4) equal = pick_digit<1>(counts[1], limit, left);
@@ -280,7 +300,7 @@ __global__ __launch_bounds__(kNT) void dbsp_cache_part_kernel(const dbsp_cache_e
   if constexpr (PASS < 3) {
     for (int i = t; i < kDigits; i += kNT) hist[i] = 0;
     __syncthreads();
-    count_digits<PASS, kR>(x, n - first, limit, hist);
+    count_digits<PASS, kNT, kR>(x, n - first, limit, hist);
     __syncthreads();
     for (int i = t; i < kDigits; i += kNT)
       if (hist[i]) atomicAdd(&digits[PASS * kDigits + i], hist[i]);
@@ -340,22 +360,44 @@ __global__ __launch_bounds__(kNT) void dbsp_cache_part_kernel(const dbsp_cache_e
   }
 }
 
+// LANES 16-byte pieces a row; a workgroup's moves are all in flight at once.
+template <int LANES>
 __global__ __launch_bounds__(256) void dbsp_cache_move_kernel(const dbsp_cache_evict_params p) {
-  const int pair = blockIdx.x, b = pair / p.Hk, hk = pair % p.Hk, t = threadIdx.x;
+  constexpr int ROWS = 256 / LANES, U = kMovesPerGroup / ROWS;
+  const int pair = blockIdx.x, b = pair / p.Hk, hk = pair % p.Hk, t = threadIdx.x, x = t % LANES * 16;
   if (pair % p.Hk == 0 && blockIdx.y == 0 && t == 0 && p.lens[b] > p.budget) p.lens[b] = p.budget;
-  const int lanes = p.row_bytes / 16, x = t % lanes * 16;
-  const int n = min(p.n_moves[pair], ((int)blockIdx.y + 1) * kMovesPerGroup);
-  for (int i = (int)blockIdx.y * kMovesPerGroup + t / lanes; i < n; i += 256 / lanes) {
-    const int64_t from = p.fillers[(int64_t)pair * p.max_moves + i], to = p.holes[(int64_t)pair * p.max_moves + i];
-    unsigned char *k = p.k + b * p.k_sb + hk * p.k_sh + x, *v = p.v + b * p.v_sb + hk * p.v_sh + x;
-    const u32x4 kr = *reinterpret_cast<const u32x4*>(k + from * p.k_st), vr = *reinterpret_cast<const u32x4*>(v + from * p.v_st);
-    *reinterpret_cast<u32x4*>(k + to * p.k_st) = kr;
-    *reinterpret_cast<u32x4*>(v + to * p.v_st) = vr;
-    if (x == 0) {                          // (what a freed slot's next key starts from is nothing; the others' weights are cleared already)
-      const int64_t at = (int64_t)pair * p.cap;
-      p.weights[at + to] = p.weights[at + from];
-      p.positions[at + to] = p.positions[at + from];
-      p.weights[at + from] = 0.f;
+  const int first = (int)blockIdx.y * kMovesPerGroup + t / LANES, n = p.n_moves[pair];
+  if ((int)blockIdx.y * kMovesPerGroup >= n) return;
+  const int32_t *fillers = p.fillers + (int64_t)pair * p.max_moves, *holes = p.holes + (int64_t)pair * p.max_moves;
+  unsigned char *k = p.k + b * p.k_sb + hk * p.k_sh + x, *v = p.v + b * p.v_sb + hk * p.v_sh + x;
+  float* weights = p.weights + (int64_t)pair * p.cap;
+  int32_t* positions = p.positions + (int64_t)pair * p.cap;
+  int64_t from[U], to[U];
+  u32x4 kr[U], vr[U];
+  float w[U];
+  int32_t at[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = min(first + u * ROWS, n - 1);      // (the last move's row again, not stored)
+    from[u] = fillers[i];
+    to[u] = holes[i];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    kr[u] = *reinterpret_cast<const u32x4*>(k + from[u] * p.k_st);
+    vr[u] = *reinterpret_cast<const u32x4*>(v + from[u] * p.v_st);
+    w[u] = weights[from[u]];
+    at[u] = positions[from[u]];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (first + u * ROWS >= n) continue;
+    *reinterpret_cast<u32x4*>(k + to[u] * p.k_st) = kr[u];
+    *reinterpret_cast<u32x4*>(v + to[u] * p.v_st) = vr[u];
+    if (x == 0) {
+      weights[to[u]] = w[u];
+      positions[to[u]] = at[u];
+      weights[from[u]] = 0.f;              // (what a freed slot's next key starts from is nothing; the others' weights are cleared already)
     }
   }
 }
@@ -373,15 +415,19 @@ hipError_t dbsp_launch_cache_evict(const dbsp_cache_evict_params& p, hipStream_t
     dbsp_cache_part_kernel<2><<<grid, kNT, 0, stream>>>(p);
     dbsp_cache_part_kernel<3><<<grid, kNT, 0, stream>>>(p);
     dbsp_cache_part_kernel<4><<<grid, kNT, 0, stream>>>(p);
-  } else if (p.cap <= 4 * kNT) {
-    dbsp_cache_choose_kernel<4><<<pairs, kNT, 0, stream>>>(p);
+  } else if (p.cap <= 1024) {
+    dbsp_cache_choose_kernel<256, 4><<<pairs, 256, 0, stream>>>(p);
+  } else if (p.cap <= 4096) {
+    dbsp_cache_choose_kernel<kMidThreads, 4096 / kMidThreads><<<pairs, kMidThreads, 0, stream>>>(p);
   } else if (p.cap <= 12 * kNT) {
-    dbsp_cache_choose_kernel<12><<<pairs, kNT, 0, stream>>>(p);
+    dbsp_cache_choose_kernel<kNT, 12><<<pairs, kNT, 0, stream>>>(p);
   } else {
-    dbsp_cache_choose_kernel<32><<<pairs, kNT, 0, stream>>>(p);
+    dbsp_cache_choose_kernel<kNT, 32><<<pairs, kNT, 0, stream>>>(p);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  dbsp_cache_move_kernel<<<dim3(pairs, (p.max_moves + kMovesPerGroup - 1) / kMovesPerGroup), 256, 0, stream>>>(p);
+  const dim3 grid(pairs, (p.max_moves + kMovesPerGroup - 1) / kMovesPerGroup);
+  if (p.row_bytes == 256) dbsp_cache_move_kernel<16><<<grid, 256, 0, stream>>>(p);
+  else dbsp_cache_move_kernel<8><<<grid, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
