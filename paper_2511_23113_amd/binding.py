@@ -399,6 +399,17 @@ class KVCache:
         raw = stream if isinstance(stream, int) else stream.cuda_stream
         return raw, raw != now
 
+    def _empty(self, shape, dtype, raw, elsewhere):
+        """A tensor for a call on the stream raw.  Memory that torch's current stream has freed may still be used there, so for a call
+        elsewhere it comes from that stream's; freed, it waits for what the current stream has been given until then."""
+        torch = _torch
+        if not elsewhere:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(raw, device=self.device)):
+            x = torch.empty(shape, dtype=dtype, device=self.device)
+        x.record_stream(torch.cuda.current_stream(self.device))
+        return x
+
     def _workspace(self, workspace, key, ask, raw, elsewhere):
         """The caller's workspace, or one of the size that a call with these sizes (key) needs; its address and size."""
         torch = _torch
@@ -410,9 +421,7 @@ class KVCache:
                 need = self._bytes[key] = out.value
             if need == 0:
                 return None, None, 0
-            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-            if elsewhere:
-                workspace.record_stream(torch.cuda.ExternalStream(raw, device=self.device))
+            workspace = self._empty(need, torch.uint8, raw, elsewhere)
         elif workspace.dtype != torch.uint8 or workspace.device != self.device or not workspace.is_contiguous():
             raise ValueError("the workspace must be a contiguous uint8 tensor on the cache's GPU")
         return workspace, workspace.data_ptr(), workspace.numel()
@@ -436,12 +445,12 @@ def cache_attn_fwd(cache: KVCache, q, q_lens=None, causal: bool = True, decay=No
         raise ValueError("q and the cache differ in the number of sequences")
     raw, elsewhere = cache._on(stream)
     if o is None:
-        o = torch.empty(shape, dtype=q.dtype, device=q.device)
+        o = cache._empty(shape, q.dtype, raw, elsewhere)
     elif o.shape != shape or o.dtype != q.dtype or o.device != q.device or o.stride(3) != 1:
         raise ValueError("o must be as q")
     if lse is None:
         if want_lse:
-            lse = torch.empty((B, H, Nq), dtype=torch.float32, device=q.device)
+            lse = cache._empty((B, H, Nq), torch.float32, raw, elsewhere)
     elif lse.shape != (B, H, Nq) or lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous f32 tensor of [B, H, Nq] on q's GPU")
     if q_lens is not None and (q_lens.shape != (B,) or q_lens.dtype != torch.int32 or q_lens.device != q.device or not q_lens.is_contiguous()):

@@ -343,6 +343,35 @@ def test_two_streams_at_once_and_a_stream_by_argument():
             assert torch.equal(o, want[i][0]) and torch.equal(lse, want[i][1])
 
 
+def test_calls_on_two_streams_do_not_share_memory_that_one_of_them_still_uses():
+    """What a call takes for itself and gives back when it returns, while its kernels wait, is not what a call on another stream gets."""
+    import torch
+    import paper_2511_23113_amd as dbsp
+    q, k, v, lens, pk, pv, w = _state(33)
+    want = dbsp.cache_attn_fwd(dbsp.KVCache(k, v, lens, pk, pv, weights=w), q, decay=0.0)
+    caches = [dbsp.KVCache(k, v, lens, pk, pv, weights=torch.zeros_like(w)) for _ in range(2)]
+    blocks, got, other, real = [], [], torch.cuda.Stream(), dbsp.KVCache._empty
+
+    def noting(*a):
+        x = real(*a)
+        blocks.append(x.data_ptr())
+        return x
+
+    torch.cuda.synchronize()
+    try:
+        dbsp.KVCache._empty = noting
+        for i in range(6):
+            got.append(dbsp.cache_attn_fwd(caches[i % 2], q, decay=0.0, stream=other if i % 2 else None))
+    finally:
+        dbsp.KVCache._empty = real
+    assert len(blocks) == 18 and not {x for i, x in enumerate(blocks) if i // 3 % 2} & {x for i, x in enumerate(blocks) if not i // 3 % 2}
+    torch.cuda.synchronize()
+    used = torch.arange(800, device="cuda") < lens[:, None, None]
+    for o, lse in got:
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    assert all(torch.equal(c.weights * used, w * used) for c in caches)
+
+
 def test_a_workspace_of_the_caller_and_none_that_is_too_small():
     import torch
     import paper_2511_23113_amd as dbsp
