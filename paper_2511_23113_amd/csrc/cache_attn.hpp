@@ -9,6 +9,7 @@
 
 #include "attn_common.hpp"
 #include "cache_params.hpp"
+#include "wave_scan.hpp"
 
 namespace {
 
@@ -105,17 +106,6 @@ __device__ __forceinline__ bool long_row_tile(const dbsp_cache_attn_params& p, i
     row_tile(p, n, it);
   }
   return true;
-}
-
-// Sum over the wave's lanes up to and with this one: within rows of 16 lanes, then from the ends of rows on.
-__device__ __forceinline__ int scan_wave(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr:1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast:15, into rows 1 and 3
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // row_bcast:31, into rows 2 and 3
-  return x;
 }
 
 // Which item this workgroup has; false: none.  All of the workgroup's threads call it.

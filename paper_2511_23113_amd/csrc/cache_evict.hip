@@ -9,9 +9,9 @@
 // and 10 bits from the top, the second and third only among images that agree with the limit so far.  Whole numbers are added, so
 // their order of arrival does not matter.
 //   * Up to 32,768 slots a workgroup has a (sequence, head), its images in registers, read once, and the counts in the LDS; it
-//     stops at the digit at which all images that have it stay.  256 heads of 2064 slots: 9 us, of which the exchanges of a workgroup of 16
-//     waves are most; 96 of 11,500 slots: 21 us, by instructions (46 with four digits of 8 bits, read anew for each; two bits
-//     a step by ballots took 18 and 37).
+//     stops at the digit at which all images that have it stay.  256 heads of 2064 slots: 9 us, of which the exchanges between a
+//     workgroup's 8 waves are most; 96 of 11,500 slots: 18 us, by instructions (46 with four digits of 8 bits, read anew for each; two
+//     bits a step by ballots took twice as long as digits).  Prefix sums of a wave by DPP: 0.7 us less than by way of the LDS.
 //   * Longer ones are cut into workgroups of 8192 slots: three launches count, a fourth counts what each part keeps, a fifth
 //     lists holes and fillers, 5 to 9 us each.  8 heads of 131,100 slots: 69 us with the moves, 431 by a workgroup a head.
 // A last launch moves the rows, 64 moves of a workgroup in flight at once, bound by memory: 96 heads, 1700 rows of K and V each (167 MB
@@ -21,6 +21,7 @@
 #include <cstdint>
 
 #include "cache_params.hpp"
+#include "wave_scan.hpp"
 
 namespace {
 
@@ -28,7 +29,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMovesPerGroup = 64;
 // Threads that choose: 256 up to 1024 slots, kMidThreads up to 4096, kNT from there on.  us with 1024 / 512 / 256: 2048 (sequence, head) pairs of
-// 750 slots 87 / - / 65, of 3000 slots 179 / 160 / 164, 256 of 2064 15.5 / 15.5 / 19, 16 of 3800 14.3 / 15.1 / 19.6.
+// 750 slots 87 / - / 65, of 3000 slots 179 / 160 / 164, 256 of 2064 15.5 / 15.5 / 19, 16 of 3800 14.3 / 15.1 / 19.6.  Images a thread: as many as the capacity needs, in four steps (96 of
+// 11,500 used slots of 16,500 66.1 us with 32, 63.9 with 20).
 constexpr int kNT = 1024;
 constexpr int kMidThreads = 512;
 
@@ -80,11 +82,7 @@ __device__ __forceinline__ void scan_table(int (&table)[R * NT / 64 + 1]) {
       v[y] = i < N ? table[i] : 0;
       mine += v[y];
     }
-    int upto = mine;
-    for (int s = 1; s < 64; s <<= 1) {
-      const int o = __shfl_up(upto, s);
-      if (l >= s) upto += o;
-    }
+    const int upto = scan_wave(mine);
     int before = upto - mine;
 #pragma unroll
     for (int y = 0; y < PER; ++y) {
@@ -186,11 +184,7 @@ __device__ __forceinline__ uint32_t pick_digit(const Share<NT>& s, uint32_t& lim
   uint32_t mine = 0;
 #pragma unroll
   for (int y = 0; y < PER; ++y) mine += s.c[y];
-  uint32_t upto = mine;
-  for (int x = 1; x < 64; x <<= 1) {
-    const uint32_t o = __shfl_up(upto, x);
-    if (l >= x) upto += o;
-  }
+  const uint32_t upto = scan_wave((int)mine);
   if (l == 63) wave_sum[w] = upto;
   __syncthreads();
   uint32_t before = upto - mine;
@@ -220,13 +214,13 @@ __global__ __launch_bounds__(NT) void dbsp_cache_choose_kernel(const dbsp_cache_
   __shared__ int table[R * NT / 64 + 1];
   const int pair = blockIdx.x, t = threadIdx.x;
   const int n = used_of(p, pair), budget = p.budget;
+  for (int i = t; i < 3 * kDigits; i += NT) hist[i] = 0;      // while the length is under way
   if (n <= budget) {
     if (t == 0) p.n_moves[pair] = 0;
     return;
   }
   uint32_t x[R];
   load_images<NT, R>(p, pair, 0, n, x);
-  for (int i = t; i < 3 * kDigits; i += NT) hist[i] = 0;
   __syncthreads();
   // `left` of the `equal` images that have the limit's digits so far stay, and all above them
   uint32_t limit = 0, left = (uint32_t)budget;
@@ -365,10 +359,17 @@ template <int LANES>
 __global__ __launch_bounds__(256) void dbsp_cache_move_kernel(const dbsp_cache_evict_params p) {
   constexpr int ROWS = 256 / LANES, U = kMovesPerGroup / ROWS;
   const int pair = blockIdx.x, b = pair / p.Hk, hk = pair % p.Hk, t = threadIdx.x, x = t % LANES * 16;
-  if (pair % p.Hk == 0 && blockIdx.y == 0 && t == 0 && p.lens[b] > p.budget) p.lens[b] = p.budget;
   const int first = (int)blockIdx.y * kMovesPerGroup + t / LANES, n = p.n_moves[pair];
-  if ((int)blockIdx.y * kMovesPerGroup >= n) return;
   const int32_t *fillers = p.fillers + (int64_t)pair * p.max_moves, *holes = p.holes + (int64_t)pair * p.max_moves;
+  int from32[U], to32[U];                  // asked for with n, not after it; what lies behind the first n is not used
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = min(first + u * ROWS, p.max_moves - 1);
+    from32[u] = fillers[i];
+    to32[u] = holes[i];
+  }
+  if (hk == 0 && blockIdx.y == 0 && t == 0 && p.lens[b] > p.budget) p.lens[b] = p.budget;
+  if ((int)blockIdx.y * kMovesPerGroup >= n) return;
   unsigned char *k = p.k + b * p.k_sb + hk * p.k_sh + x, *v = p.v + b * p.v_sb + hk * p.v_sh + x;
   float* weights = p.weights + (int64_t)pair * p.cap;
   int32_t* positions = p.positions + (int64_t)pair * p.cap;
@@ -378,9 +379,9 @@ __global__ __launch_bounds__(256) void dbsp_cache_move_kernel(const dbsp_cache_e
   int32_t at[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int i = min(first + u * ROWS, n - 1);      // (the last move's row again, not stored)
-    from[u] = fillers[i];
-    to[u] = holes[i];
+    const bool there = first + u * ROWS < n;           // (else a row that is read and not stored)
+    from[u] = there ? from32[u] : 0;
+    to[u] = there ? to32[u] : 0;
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -421,6 +422,8 @@ hipError_t dbsp_launch_cache_evict(const dbsp_cache_evict_params& p, hipStream_t
     dbsp_cache_choose_kernel<kMidThreads, 4096 / kMidThreads><<<pairs, kMidThreads, 0, stream>>>(p);
   } else if (p.cap <= 12 * kNT) {
     dbsp_cache_choose_kernel<kNT, 12><<<pairs, kNT, 0, stream>>>(p);
+  } else if (p.cap <= 20 * kNT) {
+    dbsp_cache_choose_kernel<kNT, 20><<<pairs, kNT, 0, stream>>>(p);
   } else {
     dbsp_cache_choose_kernel<kNT, 32><<<pairs, kNT, 0, stream>>>(p);
   }
