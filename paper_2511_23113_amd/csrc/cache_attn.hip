@@ -65,7 +65,7 @@ __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const 
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) q[y][ks] = *reinterpret_cast<const u32x4*>(src + 32 * ks + 8 * g);
   }
-  for (int x = 8; x > 0; x >>= 1) all_see = min(all_see, __shfl_xor(all_see, x));
+  all_see = over_row(all_see, [](int x, int y) { return min(x, y); });
   all_see = __builtin_amdgcn_readfirstlane(all_see);
 
   const int row_in = l / L::NCH, pch = l % L::NCH;
@@ -251,7 +251,8 @@ void dbsp_cache_attn_kernel(const dbsp_cache_attn_params p) {
   const int limit = p.causal ? max(0, min(len, base + at.t)) : len;       // own keys that it sees
   // a tile whose keys all of the wave's queries see needs no mask
   int all_see = valid ? limit : INT_MAX;
-  for (int s = 16; s > 0; s >>= 1) all_see = min(all_see, __shfl_xor(all_see, s));
+  all_see = over_row(all_see, [](int x, int y) { return min(x, y); });
+  all_see = min(all_see, __shfl_xor(all_see, 16));
   all_see = __builtin_amdgcn_readfirstlane(all_see);
   u32x4 q[L::KS];
   {
@@ -518,12 +519,9 @@ __device__ __forceinline__ void sum_scores(const dbsp_cache_attn_params& p, int 
         sum = sum * __builtin_amdgcn_exp2f(m - up) + __builtin_amdgcn_exp2f(x - up);
         m = up;
       }
-      float top = m;
-#pragma unroll
-      for (int s = 8; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+      const float top = over_row(m, [](float x, float y) { return fmaxf(x, y); });
       sum *= __builtin_amdgcn_exp2f(m - top);
-#pragma unroll
-      for (int s = 8; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
+      sum = over_row(sum, [](float x, float y) { return x + y; });
       ls = __builtin_bit_cast(uint32_t, sum) == 0u ? -INFINITY : top + __builtin_amdgcn_logf(sum);
     } else {
       ls = p.row_lse[((int64_t)b * p.H + hk * p.G + g) * p.Nq + t];

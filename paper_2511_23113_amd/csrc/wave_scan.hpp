@@ -18,4 +18,14 @@ __device__ __forceinline__ int scan_wave(int x) {
   return x;
 }
 
+// f over the 16 lanes of a row, in each of them; all of the row's lanes are active.
+template <class X, class F>
+__device__ __forceinline__ X over_row(X x, F&& f) {
+  auto ror = [](X v, auto by) { return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + decltype(by)::value, 0xf, 0xf, false)); };
+  x = f(x, ror(x, std::integral_constant<int, 8>{}));
+  x = f(x, ror(x, std::integral_constant<int, 4>{}));
+  x = f(x, ror(x, std::integral_constant<int, 2>{}));
+  return f(x, ror(x, std::integral_constant<int, 1>{}));
+}
+
 }  // namespace
