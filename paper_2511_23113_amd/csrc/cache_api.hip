@@ -120,6 +120,18 @@ dbsp_cache_long_cut cut_long(int64_t n, int64_t tiles, int64_t span, int slots) 
   return best;
 }
 
+// Which launches the kernel for many queries has, of those with more than 128 rows a (sequence, KV head): not those of short key lists,
+// as it has one workgroup a compute unit (two at d = 64) and nothing runs beside a workgroup's first loads and last stores, and its
+// tiles of 256 rows leave more of them empty; nor those with little to do, 12 or 16 tiles of 128 rows by 64 keys a compute unit, for
+// which the other kernel has more workgroups.  us, many / few queries' kernel: 1024 (sequence, head) pairs of 200 rows, 250 keys 80 / 66, at
+// d = 64 41 / 34; 512 of 380 rows and keys 77 / 60, 38 / 33, of 512 96.5 / 94.6, 46 / 50; 256 of 620 72 / 63, of 1000 122 / 125, all seen 161 / 173.
+// And 128 of 300 22 / 17, 8 of 300 20 / 12, of 1000 30 / 24, of 1500 32 / 29, of 2000 38 / 39, at d = 64 32 / 27, 32 of 800 36.5 / 37.6, 31 / 26;
+// 8 of 200 over 2300 27 / 23, over 8000 30 / 28, over 16,000 35 / 38, 28 / 26; 160 of 150 over 1000 36 / 44, 27 / 29, 4 of 4000 47 / 60, 37 / 35.
+bool is_many(int64_t rows, int64_t row_tiles, int64_t tiles, int d) {
+  if (rows <= kCacheRows) return false;
+  return d == 128 ? tiles > 10 && row_tiles * tiles > 3000 : tiles > 6 && row_tiles * tiles > 4096;
+}
+
 int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool causal, bool with_weights, Cut& cut) {
   const int rc = check_cache(who, c);
   if (rc != DBSP_OK) return rc;
@@ -135,7 +147,7 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool ca
   const int64_t tiles = p.pre_tiles + (int64_t)(p.cap + kCacheKeys - 1) / kCacheKeys;
   p.pooled = tiles > kCacheWhole && p.pre_tiles > kPooledFrom && p.B > 1 && rows < kCacheRows;
   p.pre_row_tiles = p.pooled ? (int32_t)((all_rows + kCacheRows - 1) / kCacheRows) : 0;
-  p.many = rows > kCacheRows;
+  p.many = is_many(rows, (rows + kCacheRows - 1) / kCacheRows * c->B * c->Hk, tiles, c->d);
   p.own_tile_rows = p.many ? kLongRows : kCacheRows;
   p.own_row_tiles = (int32_t)((rows + p.own_tile_rows - 1) / p.own_tile_rows);
   p.own_rows = (int32_t)std::min<int64_t>(rows, p.own_tile_rows);

@@ -9,9 +9,8 @@
 constexpr int kCacheKeys = 64;         // keys of a tile
 constexpr int kCacheRows = 128;        // rows of a workgroup of the kernel for few queries: four waves of 32
 // Of the kernel for many queries: waves of 64 rows (two of them a workgroup: frames of 1560 queries 1.5 % slower, though they
-// leave 6 % of the rows of their tiles empty and not 13, causal prompts 1.6 % faster).  It takes over where a (sequence, KV head) has more
-// than kCacheRows rows.  us, by the kernel for few / for many: 128 such of 300 rows 39.6 / 22.5, 160 of 150 rows over 1000
-// keys 58 / 39, 8 of 1000 rows 25.4 / 29.9 (too few for either).
+// leave 6 % of the rows of their tiles empty and not 13, causal prompts 1.6 % faster). Which launches
+// are its: cache_api.hip, is_many.
 constexpr int kLongWaves = 4, kLongRows = 64 * kLongWaves;
 constexpr int kLongSlots = 256;        // of its workgroups at a time at d = 128: a compute unit each; at d = 64 twice as many
 // Items that a launch is cut into where there is enough to cut: two rounds of the chip at d = 128, one at d = 64.  us with 512 / 1024 /

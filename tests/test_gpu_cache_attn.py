@@ -155,6 +155,48 @@ def test_against_the_oracle(name, layout):
     check(q, k, v, pk, pv, lens, q_lens, causal, dtype, decay, out_layout=layout, seed=seed)
 
 
+# Many rows over many slots: the kernel for many queries.  Slots far behind the lengths, row tiles cut into parts and whole ones,
+# the longest first or not, rows that end inside a tile.
+MANY = {
+    "rows_129": (2, 3, 1, 43, 128, 100, 50000, [43, 90], None, True, "bf16", 1.0),
+    "frame": (2, 4, 2, 70, 128, 13000, 12000, [210, 140], None, False, "bf16", 1.0),
+    "prompt": (2, 2, 1, 150, 64, 0, 70000, [150, 97], [150, 97], True, "bf16", 1.0),
+    "no_prefix_fp16": (1, 3, 3, 257, 128, 0, 22000, [22000], None, True, "fp16", 0.0),
+    "rows_from_the_end": (2, 10, 2, 130, 128, 20, 8200, [140, 7001], [130, 77], True, "fp16", 1.0),
+    "longest_first": (1, 4, 4, 2100, 64, 0, 4200, [2500], None, True, "bf16", None),
+    "longest_first_all_slots": (1, 4, 4, 1300, 128, 0, 4700, [4700], [1277], True, "bf16", 0.7),
+    "after_others": (1, 2, 1, 200, 128, 48000, 600, [431], None, True, "bf16", 1.0),
+    "weights_in_parts": (1, 4, 2, 620, 64, 0, 13500, [689], None, True, "bf16", 0.5),
+    "weights_of_all_slots": (1, 4, 2, 620, 64, 0, 13500, [13500], None, True, "fp16", 0.0),
+    "frame_weights_in_parts": (1, 3, 1, 500, 128, 15300, 900, [801], [433], False, "fp16", 1.0),
+    "one_kv_head_of_200": (2, 200, 1, 1, 64, 65970, 300, [300, 129], None, True, "fp16", 1.0),
+    "more_new_than_used": (2, 4, 2, 90, 64, 0, 33000, [70, 0], None, True, "bf16", 1.0),
+    "prefix_only": (2, 2, 1, 130, 128, 33000, 0, None, [130, 11], True, "bf16", None),
+    "many_sequences": (26, 2, 2, 600, 64, 0, 1100, [600 - 23 * i for i in range(26)], [600 - 23 * i for i in range(26)], True, "bf16", 1.0),
+    "many_sequences_behind_a_prefix": (9, 6, 3, 650, 128, 20, 670, [670 - 50 * i for i in range(9)], [max(0, 650 - 90 * i) for i in range(9)], True, "fp16", None),
+    "many_sequences_all_see": (9, 6, 3, 650, 128, 20, 670, [670 - 80 * i for i in range(9)], [650 - 60 * i for i in range(9)], False, "bf16", 1.0),
+}
+
+
+@pytest.mark.parametrize("name", MANY)
+def test_many_rows_against_the_oracle(name):
+    B, H, Hk, Nq, d, P, cap, lens, q_lens, causal, dtype, decay = MANY[name]
+    seed = 300 + list(MANY).index(name)
+    q, k, v, pk, pv = make(B, H, Hk, Nq, d, P, cap, dtype, seed, "views")
+    for b in range(B if cap else 0):
+        k[b, :, lens[b]:] = float("nan")
+        v[b, :, lens[b]:] = float("inf")
+    for b in range(B if q_lens is not None else 0):
+        q[b, :, q_lens[b]:] = float("nan")
+    check(q, k, v, pk, pv, lens, q_lens, causal, dtype, decay, out_layout="views", seed=seed)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_scores_that_rise_along_many_rows_keys(dtype):
+    q, k, v, pk, pv = make(2, 4, 2, 90, 128, 12000, 900, dtype, 71, grow=9.0)
+    check(q, k, v, pk, pv, [900, 555], None, True, dtype, 1.0, scale=0.21)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_scores_that_rise_along_the_keys_and_an_explicit_scale(dtype):
     # the running max has to be raised again and again, in the prefix, in the own keys and from part to part
