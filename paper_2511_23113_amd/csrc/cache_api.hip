@@ -182,9 +182,12 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool ca
   const bool keep_scores = with_weights && p.cap > 0 && rows * 128 <= kScoreRows * c->d;
   p.score_pitch = keep_scores ? round_up(p.cap, kCacheKeys) : 0;
   cut.part_w_at = round_up(cut.scores_at + (int64_t)p.B * p.Hk * rows * p.score_pitch * 4, 256);
-  // rows are cut, down to 512 a part, until there are workgroups for two rounds of the chip
+  // Rows are cut: down to 128 a part for two workgroups a compute unit, down to 512 for four.  us with 1 / 2 / 3 / 4 / 6 / 8 / 12 parts: 8 pairs
+  // of 1000 rows, 1000 slots (32 workgroups) 53 / 46 / 44 / 42 / 40 / 38 / 42, 64 of 1200, 300 (128) 69 / 55 / 53 / 50.5 / 50 / 55 / 62, 154 of 776,
+  // 194 (154) 53 / 49 / 45.5 / 50 / 51.5 / 53 / 62, 24 of 1560, 2000 (192) 116 / 111.5 / 107 / 116 / 114 / 120 / 129; of 4096, 4096 at d = 64 (384) 164 / 148.
   const int64_t groups = (int64_t)p.B * p.Hk * ((p.cap + kWeightKeys - 1) / kWeightKeys);
-  p.row_parts = with_weights && p.cap > 0 && !keep_scores ? (int32_t)std::clamp<int64_t>(std::min(4 * kLongSlots / groups, rows / 512), 1, 64) : 1;
+  const int64_t cuts = std::max(std::min(2 * kLongSlots / std::max<int64_t>(groups, 1), rows / 128), std::min(4 * kLongSlots / std::max<int64_t>(groups, 1), rows / 512));
+  p.row_parts = with_weights && p.cap > 0 && !keep_scores ? (int32_t)std::clamp<int64_t>(cuts, 1, 64) : 1;
   cut.bytes = round_up(cut.part_w_at + (p.row_parts > 1 ? (int64_t)p.row_parts * p.B * p.Hk * p.cap * 4 : 0), 256);
   if (!p.split && p.cut.k <= 1 && !with_weights) cut.bytes = 0;      // one launch, and nothing between workgroups
   return DBSP_OK;
