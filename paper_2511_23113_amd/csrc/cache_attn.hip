@@ -19,7 +19,7 @@
 // transposed, S^T = K Q^T and O^T = V^T P^T: a lane holds a query, the packed probabilities are the second product's operand as they
 // lie, and V^T comes from transposing LDS reads (the layouts are those of attn_fwd.hip).  Up to 32 rows are given to all waves, which
 // share the keys (few_rows); more are dealt to them, 32 each (the kernel).  Probabilities are rounded to the inputs' type for the second
-// product, as they must be for the matrix pipe: half a step of it relative to each; sums are of the f32 values.
+// product, as they must be for the matrix pipe: half a step of it relative to each; LSE's sums are of the f32 values.
 //
 // Bound by reading K and V once.  32 sequences of 32 heads on 8 KV heads over 4400 own keys each (577 MB): 120 us, 4.8 TB/s, where a large copy
 // reaches 5.0; 8 KV heads over 123,000 keys (506 MB) 95 us, 5.3 TB/s; without any of its arithmetic the kernel takes 3 to 8 % less.
@@ -93,15 +93,19 @@ __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const 
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) v_rd[dt] = mine + L::TILE + key * L::ROWB + (((2 * dt + (a4 >> 1)) ^ L::v_swz(key)) << 4) + (a4 & 1) * 8;
   }
-  f32x4 o[NR][DT];
+  // rounded[y]: sums of the rounded probabilities, by one more MFMA against ones, all four alike.  O is divided by them, so that the
+  // rounding of a key that has most of its row's attention drops out (fp16, 30 rows: 2-norm error 3.2e-4 by the others' sum); LSE is of `sum`.
+  f32x4 o[NR][DT], rounded[NR];
   float mc[NR], sum[NR];
 #pragma unroll
   for (int y = 0; y < NR; ++y) {
     mc[y] = -FLT_MAX;
     sum[y] = 0.f;
+    rounded[y] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[y][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  const u32x2 ones = {T::pack(1.f, 1.f), T::pack(1.f, 1.f)};
   const float c = p.scale_log2;
   float* scores = p.scores && own ? p.scores + ((int64_t)s.b * p.Hk + s.hk) * p.own_rows * p.score_pitch : nullptr;
 
@@ -147,6 +151,7 @@ __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const 
         const float to = fmaxf(mc[y], top * c), f = __builtin_amdgcn_exp2f(mc[y] - to);
         mc[y] = to;
         sum[y] *= f;
+        rounded[y] *= f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[y][dt] *= f;
 #pragma unroll
@@ -159,10 +164,12 @@ __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const 
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int y = 0; y < NR; ++y) o[y][dt] = T::mfma16(vf[dt], pb[y], o[y][dt]);
+#pragma unroll
+    for (int y = 0; y < NR; ++y) rounded[y] = T::mfma16(ones, pb[y], rounded[y]);
   }
 
   // the waves' results: [wave][row][16-byte chunk of the head dim, by row swizzled]
-  __shared__ float mcs[4][16 * NR], sums[4][16 * NR];
+  __shared__ float mcs[4][16 * NR], sums[4][16 * NR], rounds[4][16 * NR];
   __syncthreads();                         // everybody has read its last tile
   f32x4* const os = reinterpret_cast<f32x4*>(lds);
 #pragma unroll
@@ -172,6 +179,7 @@ __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const 
     if (g == 0) {
       mcs[w][16 * y + n] = mc[y];
       sums[w][16 * y + n] = sum[y];
+      rounds[w][16 * y + n] = rounded[y][0];
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) os[(w * 16 * NR + 16 * y + n) * CH + ((4 * dt + g) ^ n)] = o[y][dt];
@@ -186,16 +194,17 @@ __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const 
     float m = mcs[0][in];
 #pragma unroll
     for (int x = 1; x < 4; ++x) m = fmaxf(m, mcs[x][in]);
-    float all = 0.f;
+    float all = 0.f, all_rounded = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const float f = __builtin_amdgcn_exp2f(mcs[x][in] - m);
       all += f * sums[x][in];
+      all_rounded += f * rounds[x][in];
       acc += f * os[(x * 16 * NR + in) * CH + (ch ^ (in & 15))];
     }
     const bool none = __builtin_bit_cast(uint32_t, all) == 0u;
-    acc *= none ? 0.f : 1.f / all;
+    acc *= none ? 0.f : 1.f / all_rounded;
     const float lse2 = none ? -INFINITY : m + __builtin_amdgcn_logf(all);
     const int h = s.hk * p.G + at.g;
     if (it.slot >= 0) {

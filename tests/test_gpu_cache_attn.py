@@ -204,6 +204,34 @@ def test_scores_that_rise_along_the_keys_and_an_explicit_scale(dtype):
     check(q, k, v, pk, pv, [900, 555], None, True, dtype, 1.0, scale=0.21)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_a_key_that_has_most_of_a_rows_attention_costs_no_rounding(dtype, d):
+    """The rounding of a probability p_i by a factor 1 + e_i, |e_i| <= h, moves sum p_i v_i / sum p_i by e_i p_i (v_i - O) where both sums are
+    of the rounded ones: O is off by at most h sum p_i |v_i - O| and its own rounding, h |O|, not by h sum p_i |v_i|."""
+    import torch
+    import paper_2511_23113_amd as dbsp
+    h = torch.finfo(torch_types(dtype)).eps / 2
+    q, k, v, _, _ = make(6, 4, 2, 2, d, 0, 700, dtype, 72)
+    q = (q.float() * 4).to(q.dtype)
+    lens = torch.tensor([700, 600, 500, 64, 333, 699], dtype=torch.int32, device="cuda")
+    o, lse = dbsp.cache_attn_fwd(dbsp.KVCache(k, v, lens), q, causal=False)
+    for b in range(6):
+        n = int(lens[b])
+        kk, vv = (x[b, :, :n].double().cpu().repeat_interleave(2, 0) for x in (k, v))
+        x = q[b].double().cpu() @ kk.transpose(1, 2) / d ** 0.5
+        P = torch.softmax(x, -1)
+        O = P @ vv
+        spread = (P[..., None] * (vv[:, None] - O[:, :, None]).abs()).sum(2)
+        top = vv.abs().max()
+        # scores: f32 sums of d products; fp16: probabilities below its normal range, half a step of 2^-24 each, of a row whose sum is at least 1
+        score_err = 4 * d * 2.0 ** -24 * (q[b].double().abs().cpu() @ kk.abs().transpose(1, 2) / d ** 0.5).max()
+        tol = h * O.abs() * (1 + 2 * h) + h * (1 + 4 * h) * spread + 2 * score_err * top + (n * 2.0 ** -25 * top if dtype == "fp16" else 0) + 2.0 ** -20 * top
+        off = (o[b].double().cpu() - O).abs()
+        assert (off <= tol).all(), f"{float((off / tol).max()):.3g} of the tolerance"
+        assert (lse[b].double().cpu() - torch.logsumexp(x, -1)).abs().max() <= score_err + 2.0 ** -20 * (1 + x.abs().max())
+
+
 def test_lengths_out_of_range_are_taken_as_the_nearest_in_range():
     import torch
     import paper_2511_23113_amd as dbsp
