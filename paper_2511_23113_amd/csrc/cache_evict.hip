@@ -13,7 +13,7 @@
 //     workgroup's 8 waves are most; 96 of 11,500 slots: 18 us, by instructions (46 with four digits of 8 bits, read anew for each; two
 //     bits a step by ballots took twice as long as digits).  Prefix sums of a wave by DPP: 0.7 us less than by way of the LDS.
 //   * Longer ones are cut into workgroups of 8192 slots: three launches count, a fourth counts what each part keeps, a fifth
-//     lists holes and fillers, 5 to 9 us each.  8 heads of 131,100 slots: 69 us with the moves, 431 by a workgroup a head.
+//     lists holes and fillers, 5 to 8 us each.  8 heads of 131,100 slots: 66 us with the moves, 431 by a workgroup a head.
 // A last launch moves the rows, 64 moves of a workgroup in flight at once, bound by memory: 96 heads, 1700 rows of K and V each (167 MB
 // read and written) 38 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
