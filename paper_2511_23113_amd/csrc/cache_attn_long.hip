@@ -38,7 +38,7 @@ void dbsp_cache_attn_long_kernel(const dbsp_cache_attn_params p) {
   constexpr int ROWS = 64 * NW, SHARE = 64 / NW, COPIES = SHARE / L::RPC;
   constexpr int SUB = 2 * L::KS;           // sub-slots of a step
   constexpr int KP = 3, VP = 2;            // places
-  constexpr int kBias = 3072;
+  constexpr int kBias = 3 * 1024;
   static_assert(COPIES <= 4, "a group's copies share a destination");
   __shared__ __attribute__((aligned(1024))) unsigned char lds[(KP + VP) * L::TILE];
   const uint32_t lds_base = (uint32_t)(uintptr_t)(LDS_PTR(unsigned char))lds;
