@@ -212,7 +212,7 @@ __device__ __forceinline__ void few_rows(const dbsp_cache_attn_params& p, const 
       *reinterpret_cast<f32x4*>(p.part_o + pr * D + 4 * ch) = acc;
       if (ch == 0) p.part_lse[pr] = lse2;
     } else {
-      *reinterpret_cast<u32x2*>(p.o + at.b * p.o_sb + h * p.o_sh + at.t * p.o_st + 4 * ch) = u32x2{T::pack(acc.x, acc.y), T::pack(acc.z, acc.w)};
+      *reinterpret_cast<u32x2*>(p.o + at.b * p.o_sb + h * p.o_sh + at.t * p.o_st + 4 * ch) = u32x2{T::pack_o(acc.x, acc.y), T::pack_o(acc.z, acc.w)};
       if (ch == 0) {
         const int64_t q_row = ((int64_t)at.b * p.H + h) * p.Nq + at.t;
         if (p.lse) p.lse[q_row] = lse2 * 0.69314718055994531f;
@@ -492,7 +492,7 @@ __device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
   if (!mine) return;
   const bool none = __builtin_bit_cast(uint32_t, sum) == 0u;
   acc *= none ? 0.f : 1.f / sum;
-  *reinterpret_cast<u32x2*>(p.o + b * p.o_sb + h * p.o_sh + t * p.o_st + x) = u32x2{T::pack(acc.x, acc.y), T::pack(acc.z, acc.w)};
+  *reinterpret_cast<u32x2*>(p.o + b * p.o_sb + h * p.o_sh + t * p.o_st + x) = u32x2{T::pack_o(acc.x, acc.y), T::pack_o(acc.z, acc.w)};
   if (x == 0) {
     const int64_t q_row = ((int64_t)b * p.H + h) * p.Nq + t;
     const float lse2 = none ? -INFINITY : m + __builtin_amdgcn_logf(sum);

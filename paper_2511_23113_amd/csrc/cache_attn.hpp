@@ -34,6 +34,7 @@ struct Bf16 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16x2(a, b); }
+  static __device__ __forceinline__ uint32_t pack_o(float a, float b) { return pack(a, b); }
 };
 struct Fp16 {
   static __device__ __forceinline__ f32x4 mfma32(u32x4 a, u32x4 b, f32x4 c) {
@@ -49,6 +50,13 @@ struct Fp16 {
     f32x2 f = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2));      // round to nearest even
   }
+  // Of O: no larger than the largest v, 65504 at most, but the rounded probabilities may sum to 1 + 2^-11, and from 65520 on a number is
+  // rounded to infinity.  Those that are finite in f32 stop at 65504 (by their bits: NaNs are not regarded in these files, and stay).
+  static __device__ __forceinline__ float within(float x) {
+    constexpr uint32_t kTop = 0x477fe000u;       // 65504
+    return (__builtin_bit_cast(uint32_t, x) & 0x7fffffffu) - kTop < 0x7f800000u - kTop ? __builtin_copysignf(65504.f, x) : x;
+  }
+  static __device__ __forceinline__ uint32_t pack_o(float a, float b) { return pack(within(a), within(b)); }
 };
 
 // Of a d-wide K or V tile in the LDS: rows unpadded, 16-byte chunks XOR-swizzled inside each row (K by the row, so that the
@@ -265,7 +273,7 @@ __device__ __forceinline__ void store_row(const dbsp_cache_attn_params& p, const
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<u32x2*>(to + 32 * dt + 8 * i) = u32x2{T::pack(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv), T::pack(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv)};
+      *reinterpret_cast<u32x2*>(to + 32 * dt + 8 * i) = u32x2{T::pack_o(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv), T::pack_o(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv)};
   if (g == 0) {
     const int64_t q_row = ((int64_t)at.b * p.H + h) * p.Nq + at.t;
     if (p.lse) p.lse[q_row] = lse2 * 0.69314718055994531f;
