@@ -405,7 +405,9 @@ class KVCache:
         torch = _torch
         if not elsewhere:
             return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(torch.cuda.ExternalStream(raw, device=self.device)):
+        # (an ExternalStream of handle 0 would be some stream of torch's pool, not the default stream)
+        on = torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(on):
             x = torch.empty(shape, dtype=dtype, device=self.device)
         x.record_stream(torch.cuda.current_stream(self.device))
         return x

@@ -3,8 +3,6 @@
 import numpy as np
 import pytest
 
-from oracle import cache as oc
-
 pytestmark = pytest.mark.gpu
 
 # B, H, Hk, Nq, d, P, cap, lens: up to 32 rows a (sequence, KV head), 33 .. 128, more over few and over many tiles, and parts that are joined
