@@ -396,7 +396,11 @@ class KVCache:
         now = torch._C._cuda_getCurrentRawStream(self._index)
         if stream is None:
             return now, False
-        raw = stream if isinstance(stream, int) else stream.cuda_stream
+        if isinstance(stream, int):
+            return stream, stream != now
+        if getattr(stream, "device", self.device) != self.device:
+            raise ValueError("the stream is of another device than the cache")
+        raw = stream.cuda_stream
         return raw, raw != now
 
     def _empty(self, shape, dtype, raw, elsewhere):

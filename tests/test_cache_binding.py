@@ -56,3 +56,11 @@ def test_a_calls_memory_comes_from_the_stream_that_its_kernels_run_on(cache, str
     assert got == raw
     x = cache._empty((4,), torch.uint8, got, elsewhere)
     assert x.raw == raw and x.recorded == recorded
+
+
+def test_a_stream_of_another_device_is_refused(cache):
+    with pytest.raises(ValueError, match="another device"):
+        cache._on(Stream(0x9000, torch.device("cuda", 1)))
+    cache._index = 1                       # and so is a cache of another device than the current one
+    with pytest.raises(ValueError, match="another device"):
+        cache._on(None)
