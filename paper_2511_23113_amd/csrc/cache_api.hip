@@ -45,6 +45,7 @@ bool distinct(const int64_t* size, const int64_t* stride, int64_t d) {
 }
 
 constexpr int64_t kMost = INT_MAX / 2;
+constexpr int64_t kMostThreads = UINT32_MAX;       // of a launch along a dimension: HIP has no more
 
 int check_cache(const char* who, const dbsp_cache* c) {
   if (!c) return fail(who, DBSP_EINVAL, "null cache");
@@ -190,6 +191,14 @@ int lay_out(const char* who, const dbsp_cache* c, int32_t H, int32_t Nq, bool ca
   p.row_parts = with_weights && p.cap > 0 && !keep_scores ? (int32_t)std::clamp<int64_t>(cuts, 1, 64) : 1;
   cut.bytes = round_up(cut.part_w_at + (p.row_parts > 1 ? (int64_t)p.row_parts * p.B * p.Hk * p.cap * 4 : 0), 256);
   if (!p.split && p.cut.k <= 1 && !with_weights) cut.bytes = 0;      // one launch, and nothing between workgroups
+  // the finishing launch: rows that are joined, 1024 / d of them a workgroup or one, and (sequence, KV head) pairs whose scores are summed
+  const bool cut_up = many && p.cut.k > 1;
+  const int64_t joined = cut_up ? (int64_t)p.cut.dies * p.cut.tail * p.own_rows : p.split ? q_rows : 0, by = joined <= kMergeRows ? 1 : 1024 / c->d;
+  const int64_t merges = (joined + by - 1) / by, pairs = (int64_t)p.B * p.Hk, sums = keep_scores ? pairs * ((p.cap + kScoreSlots - 1) / kScoreSlots) : 0;
+  if (std::max({cut.grid, merges + sums, with_weights ? pairs : 0}) > kMostThreads / 256) return fail(who, DBSP_ESHAPE, "too many queries or sequences");
+  p.merge_groups = (int32_t)merges;
+  p.merge_by_row = by == 1;
+  p.sum_groups = (int32_t)sums;
   return DBSP_OK;
 }
 
@@ -204,6 +213,7 @@ int lay_out_evict(const char* who, const dbsp_cache* c, int32_t budget, Moves& m
   m.most = std::min<int64_t>(budget, std::max(0, c->capacity - budget));
   m.parts = c->capacity > kEvictWhole ? (c->capacity + kEvictPart - 1) / kEvictPart : 0;
   const int64_t pairs = (int64_t)c->B * c->Hk;
+  if (pairs > kMostThreads / evict_threads(c->capacity)) return fail(who, DBSP_ESHAPE, "too many sequences");
   m.holes_at = round_up(pairs * 4, 256);
   m.fillers_at = m.holes_at + round_up(pairs * m.most * 4, 256);
   m.digits_at = m.fillers_at + round_up(pairs * m.most * 4, 256);

@@ -501,11 +501,9 @@ __device__ __forceinline__ void merge_rows(const dbsp_cache_attn_params& p) {
   }
 }
 
-constexpr int kSlots = 1024;       // a workgroup's, four a thread
-
 __device__ __forceinline__ void sum_scores(const dbsp_cache_attn_params& p, int group) {
   __shared__ float row_lse[kScoreRows];
-  const int per_pair = (p.cap + kSlots - 1) / kSlots, pair = group / per_pair, slot0 = group % per_pair * kSlots;
+  const int per_pair = (p.cap + kScoreSlots - 1) / kScoreSlots, pair = group / per_pair, slot0 = group % per_pair * kScoreSlots;
   const int b = pair / p.Hk, hk = pair % p.Hk, len = len_of(p, b), tid = threadIdx.x;
   if (slot0 >= len) return;
   const int rows = q_len_of(p, b) * p.G, slot = slot0 + 4 * tid;
@@ -566,7 +564,7 @@ __global__ __launch_bounds__(256) void dbsp_cache_finish_kernel(const dbsp_cache
 }
 
 template <class T, int D>
-hipError_t launch(dbsp_cache_attn_params p, int grid, hipStream_t stream) {
+hipError_t launch(const dbsp_cache_attn_params& p, int grid, hipStream_t stream) {
   hipError_t e;
   if (p.many) {
     e = dbsp_launch_cache_attn_long(p, D, std::is_same_v<T, Fp16>, grid, stream);
@@ -575,15 +573,8 @@ hipError_t launch(dbsp_cache_attn_params p, int grid, hipStream_t stream) {
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
-  constexpr int UNITS = 256 / (D / 4);
-  const bool cut_long = p.many && p.cut.k > 1;
-  const int64_t rows = cut_long ? (int64_t)p.cut.dies * p.cut.tail * p.own_rows : (int64_t)p.B * p.H * p.Nq;
-  const int64_t sums = p.scores ? (int64_t)p.B * p.Hk * ((p.cap + kSlots - 1) / kSlots) : 0;
-  const bool all_ways = rows <= kMergeRows;
-  p.merge_groups = !p.split && !cut_long ? 0 : (int)(all_ways ? rows : (rows + UNITS - 1) / UNITS);
-  if (p.merge_groups + sums > 0) {
-    const unsigned groups = (unsigned)(p.merge_groups + sums);
-    if (all_ways) dbsp_cache_finish_kernel<T, D, UNITS><<<groups, 256, 0, stream>>>(p);
+  if (const int groups = p.merge_groups + p.sum_groups; groups > 0) {
+    if (p.merge_by_row) dbsp_cache_finish_kernel<T, D, 256 / (D / 4)><<<groups, 256, 0, stream>>>(p);
     else dbsp_cache_finish_kernel<T, D, 1><<<groups, 256, 0, stream>>>(p);
     e = hipGetLastError();
   }

@@ -28,11 +28,8 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMovesPerGroup = 64;
-// Threads that choose: 256 up to 1024 slots, kMidThreads up to 4096, kNT from there on.  us with 1024 / 512 / 256: 2048 (sequence, head) pairs of
-// 750 slots 87 / - / 65, of 3000 slots 179 / 160 / 164, 256 of 2064 15.5 / 15.5 / 19, 16 of 3800 14.3 / 15.1 / 19.6.  Images a thread: as many as the capacity needs, in four steps (96 of
-// 11,500 used slots of 16,500 66.1 us with 32, 63.9 with 20).
-constexpr int kNT = 1024;
-constexpr int kMidThreads = 512;
+// Images a thread: as many as the capacity needs, in four steps (96 of 11,500 used slots of 16,500 66.1 us with 32, 63.9 with 20).
+constexpr int kNT = evict_threads(kEvictWhole);
 
 // Larger weight, larger image; what must stay comes last.
 __device__ __forceinline__ uint32_t image(float w, bool stays) {
@@ -416,10 +413,10 @@ hipError_t dbsp_launch_cache_evict(const dbsp_cache_evict_params& p, hipStream_t
     dbsp_cache_part_kernel<2><<<grid, kNT, 0, stream>>>(p);
     dbsp_cache_part_kernel<3><<<grid, kNT, 0, stream>>>(p);
     dbsp_cache_part_kernel<4><<<grid, kNT, 0, stream>>>(p);
-  } else if (p.cap <= 1024) {
+  } else if (evict_threads(p.cap) == 256) {
     dbsp_cache_choose_kernel<256, 4><<<pairs, 256, 0, stream>>>(p);
-  } else if (p.cap <= 4096) {
-    dbsp_cache_choose_kernel<kMidThreads, 4096 / kMidThreads><<<pairs, kMidThreads, 0, stream>>>(p);
+  } else if (evict_threads(p.cap) == 512) {
+    dbsp_cache_choose_kernel<512, 8><<<pairs, 512, 0, stream>>>(p);
   } else if (p.cap <= 12 * kNT) {
     dbsp_cache_choose_kernel<kNT, 12><<<pairs, kNT, 0, stream>>>(p);
   } else if (p.cap <= 20 * kNT) {

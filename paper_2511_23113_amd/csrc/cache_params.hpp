@@ -32,8 +32,12 @@ constexpr int kWeightKeys = 256;       // own keys of a workgroup that forms the
 // Rows up to which a workgroup joins the parts of one, else of 8 or 16.  us with 1024 / 4096 / 8192: 5040 rows of 7 parts at d = 64
 // 27.1 / 27.1 / 34.3; 96 rows of 205 parts took 53 us of a launch by the eight, and take 9.
 constexpr int kMergeRows = 4096;
+constexpr int kScoreSlots = 1024;      // own keys of a workgroup that sums kept scores, four a thread
 constexpr int kEvictWhole = 32768;     // slots that a workgroup chooses among by itself: what its registers hold; and those of a
 constexpr int kEvictPart = 8192;       // part where there are more
+// Threads that choose among so many slots.  us with 1024 / 512 / 256: 2048 (sequence, head) pairs of 750 slots 87 / - / 65, of 3000 slots
+// 179 / 160 / 164, 256 of 2064 15.5 / 15.5 / 19, 16 of 3800 14.3 / 15.1 / 19.6.
+constexpr int evict_threads(int slots) { return slots <= 1024 ? 256 : slots <= 4096 ? 512 : 1024; }
 
 // How a launch of the kernel for many queries is cut: its row tiles, `per` for each of `dies` dies (workgroup number mod 8), of which
 // the first `whole` are one item each and the `tail` others `k` parts, so that the last round of workgroups ends together.
@@ -75,7 +79,8 @@ struct dbsp_cache_attn_params {
   int64_t score_pitch;
   int32_t row_parts;                   // parts into which the rows are cut for the weights of own keys, and f32 [row_parts][B,Hk,cap]
   float* part_w;                       // for their sums where there are more than one
-  int32_t merge_groups;                // set by dbsp_launch_cache_attn
+  // workgroups of the finishing launch: those that join parts, a row each with merge_by_row, and those that sum kept scores
+  int32_t merge_groups, merge_by_row, sum_groups;
 };
 
 struct dbsp_cache_evict_params {
