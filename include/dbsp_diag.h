@@ -34,6 +34,22 @@ int dbsp_mfma_probe(double* tflops, double* clock_ghz, void* stream);
  */
 int dbsp_plan_run_order(const dbsp_plan* plan, int32_t* partition_of, int32_t* items, int32_t* local, int32_t* staged);
 
+/*
+ * dbsp_cache_attn_layout -- how dbsp_cache_attn_fwd lays a call of these sizes out (host only; the arguments of
+ * dbsp_cache_attn_workspace).  Errors: as there.
+ */
+typedef struct dbsp_cache_layout {
+  int32_t many;               /* 1: the kernel for many queries, 0: the one for few */
+  int32_t pooled;             /* 1: the prefix is read by the rows of all sequences together */
+  int32_t joined;             /* 1: row tiles' keys are cut into parts, whose results a second launch joins */
+  int32_t join_by_row;        /* with `joined`: 1: a workgroup joins one row, 0: several */
+  int32_t row_tiles, cut, parts; /* with `many`: row tiles in all, of each die's how many are cut, and into how many parts */
+  int32_t longest_first;      /* with `many`: row tiles run by their keys, the most first */
+  int32_t scores_kept;        /* with weights: 1: from scores that the attention kernel keeps, 0: from scores formed anew */
+  int32_t weight_parts;       /* and there: parts of the rows */
+} dbsp_cache_layout;
+int dbsp_cache_attn_layout(const dbsp_cache* cache, int32_t H, int32_t Nq, int32_t causal, int32_t with_weights, dbsp_cache_layout* layout);
+
 #ifdef __cplusplus
 }
 #endif

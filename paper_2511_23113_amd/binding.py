@@ -29,6 +29,7 @@ EXPORTS = (
     "dbsp_plan_busy", "dbsp_plan_tail_takes", "dbsp_plan_pair_rows", "dbsp_plan_calibrate", "dbsp_plan_destroy", "dbsp_plan_release", "dbsp_last_error",
     "dbsp_partition_heads", "dbsp_partition_blocks", "dbsp_ring_work", "dbsp_fit_cost_model", "dbsp_mfma_probe", "dbsp_plan_run_order",
     "dbsp_cache_attn_fwd", "dbsp_cache_attn_workspace", "dbsp_cache_evict", "dbsp_cache_evict_workspace",
+    "dbsp_cache_attn_layout",
 )
 
 
@@ -51,6 +52,11 @@ class CacheDesc(C.Structure):
                 ("prefix_k", C.c_void_p), ("prefix_v", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
                 ("prefix_k_stride", C.c_int64 * 2), ("prefix_v_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
                 ("lens", C.c_void_p), ("weights", C.c_void_p), ("positions", C.c_void_p)]
+
+
+class CacheLayout(C.Structure):
+    """dbsp_cache_layout of dbsp_diag.h."""
+    _fields_ = [(name, C.c_int32) for name in ("many", "pooled", "joined", "join_by_row", "row_tiles", "cut", "parts", "longest_first", "scores_kept", "weight_parts")]
 
 
 _lib = None
@@ -109,6 +115,8 @@ def load_library(path: str | None = None):
     lib.dbsp_cache_attn_fwd.restype = C.c_int
     lib.dbsp_cache_attn_workspace.argtypes = [cache, i32, i32, i32, i32, i64p]
     lib.dbsp_cache_attn_workspace.restype = C.c_int
+    lib.dbsp_cache_attn_layout.argtypes = [cache, i32, i32, i32, i32, C.POINTER(CacheLayout)]
+    lib.dbsp_cache_attn_layout.restype = C.c_int
     lib.dbsp_cache_evict.argtypes = [cache, i32, i32, vp, vp, i64, vp]
     lib.dbsp_cache_evict.restype = C.c_int
     lib.dbsp_cache_evict_workspace.argtypes = [cache, i32, i64p]

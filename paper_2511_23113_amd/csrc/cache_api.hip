@@ -8,6 +8,7 @@
 
 #include "cache_params.hpp"
 #include "dbsp.h"
+#include "dbsp_diag.h"
 #include "plan.hpp"
 
 namespace {
@@ -234,6 +235,26 @@ int dbsp_cache_attn_workspace(const dbsp_cache* cache, int32_t H, int32_t Nq, in
   const int rc = lay_out(who, cache, H, Nq, causal != 0, with_weights != 0, cut);
   *bytes = rc == DBSP_OK ? cut.bytes : 0;
   return rc;
+}
+
+int dbsp_cache_attn_layout(const dbsp_cache* cache, int32_t H, int32_t Nq, int32_t causal, int32_t with_weights, dbsp_cache_layout* layout) {
+  const char* who = "dbsp_cache_attn_layout";
+  if (!layout) return fail(who, DBSP_EINVAL, "null pointer");
+  Cut cut;
+  *layout = {};
+  if (const int rc = lay_out(who, cache, H, Nq, causal != 0, with_weights != 0, cut); rc != DBSP_OK) return rc;
+  const dbsp_cache_attn_params& p = cut.p;
+  layout->many = p.many;
+  layout->pooled = p.pooled;
+  layout->joined = p.merge_groups > 0;
+  layout->join_by_row = p.merge_groups > 0 && p.merge_by_row;
+  layout->row_tiles = p.cut.items;
+  layout->cut = p.cut.tail;
+  layout->parts = p.cut.k;
+  layout->longest_first = p.cut.longest_first;
+  layout->scores_kept = p.score_pitch > 0;
+  layout->weight_parts = with_weights && p.cap > 0 && p.score_pitch == 0 ? p.row_parts : 0;
+  return DBSP_OK;
 }
 
 int dbsp_cache_attn_fwd(const dbsp_cache* cache, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token, void* o,

@@ -1,0 +1,48 @@
+"""How calls over a key/value cache are laid out: each case of test_gpu_cache_paths.py takes the way that it is there for (host only)."""
+
+import ctypes as C
+
+import pytest
+
+from paper_2511_23113_amd import binding as B
+from test_abi_cache import FAKE, desc
+from test_gpu_cache_paths import PATHS
+
+
+def layout(B_, H, Hk, Nq, d, P, cap, causal, weights):
+    own, pre = (Hk * cap * d, cap * d, d), (P * d, d)
+    cache = desc(B=B_, Hk=Hk, d=d, n_prefix=P, capacity=cap, k_stride=own, v_stride=own, prefix_k_stride=pre, prefix_v_stride=pre)
+    out = B.CacheLayout()
+    assert B.load_library().dbsp_cache_attn_layout(C.byref(cache), H, Nq, causal, weights, C.byref(out)) == B.DBSP_OK
+    return out
+
+
+def tiles_an_item(c, pooled):
+    """Of a launch of the kernel for few queries: 1 .. 4 tiles as there are 256 items or more, and more where there would be more items
+    than are aimed at; all of a row tile's keys, the prefix's where it is not pooled, or as many parts as that."""
+    def tiles(n):
+        return -(-n // 64)
+    rows = c["Nq"] * c["H"] // c["Hk"]
+    unit = c["Hk"] * -(-rows // 128)
+    total = unit * sum(tiles(n) + (0 if pooled else tiles(c["P"])) for n in c["lens"])
+    if pooled:
+        total += c["Hk"] * -(-rows * c["B"] // 128) * tiles(c["P"])
+    target = 1024 if rows <= 32 else 1024 * 32 // c["d"]
+    return max(1, min(4, total // 256), -(-total // target))
+
+
+@pytest.mark.parametrize("name", PATHS)
+def test_a_case_takes_its_way(name):
+    c = PATHS[name]
+    got = layout(c["B"], c["H"], c["Hk"], c["Nq"], c["d"], c["P"], c["cap"], c["causal"], c["decay"] is not None)
+    assert {k: getattr(got, k) for k in c["layout"]} == c["layout"]
+    if c["chunk"] is not None:
+        assert not got.many and got.joined and tiles_an_item(c, got.pooled) == c["chunk"]
+
+
+def test_errors():
+    lib, out = B.load_library(), B.CacheLayout(many=7)
+    assert lib.dbsp_cache_attn_layout(C.byref(desc()), 4, 1, 1, 1, None) == B.DBSP_EINVAL
+    assert lib.dbsp_cache_attn_layout(None, 4, 1, 1, 1, C.byref(out)) == B.DBSP_EINVAL and out.many == 0
+    assert lib.dbsp_cache_attn_layout(C.byref(desc()), 3, 1, 1, 1, C.byref(out)) == B.DBSP_ESHAPE
+    assert lib.dbsp_cache_attn_layout(C.byref(desc(k=FAKE + 8)), 4, 1, 1, 1, C.byref(out)) == B.DBSP_EINVAL
