@@ -265,13 +265,17 @@ typedef struct dbsp_cache {
  * q_lens: device, int32 [B]: new tokens of each sequence, taken as 0 below 0 and as Nq above it; NULL: Nq each.  Rows t >= q_lens[b]
  *      of o and lse are left as they were, whatever q holds there.
  * A query without a key gets O = 0, LSE = -inf.  K and V must be finite in every used slot and in the prefix (a key that a query
- * does not see has probability zero, which an infinite value does not survive); slots from lens[b] on are never read.
+ * does not see has probability zero, which an infinite value does not survive); slots from lens[b] on are never read.  Scores s are f32: one
+ * of 2^26 or more in magnitude makes its row's O, LSE and weights mean nothing, and their rounding, some d 2^-24 of scale sum |q k| (LSE's: 2^-24
+ * of it), is what probabilities and weights are off by, relative.  bf16 values beyond 2^80 in magnitude may overflow the f32 sums that O is formed from.
  * softmax_scale <= 0 selects 1 / sqrt(d), else it lies between 1e-30 and 1e30.  f32 accumulation; the same call gives the same bits.
  * decay: below 0 leaves the cache's weights alone; else, for every own key in use,
  *      weights[b, hk, j] = decay * weights[b, hk, j] + sum over the heads h of hk and t < q_lens[b] of exp(s - LSE)
  *      (0: what was there is not read; 1: the sum over all calls), in f32; weights from lens[b] on are left as they were.
  * workspace: device, 256-byte aligned, of at least the size that dbsp_cache_attn_workspace gives for the same cache, H, Nq,
  *      causal and whether decay >= 0 (NULL where that is 0); written by the call, holds nothing between calls.  Calls under way at the same time need one each.
+ *      Its size goes by the capacity, as lengths are on the device.  With decay >= 0 and at most 48 rows (24 at d = 64) Nq G it has their scores,
+ *      4 bytes a row and slot: up to three quarters of the size of k (8 sequences of 8 KV heads, 48 rows, 131,072 slots: 1.6 GB).
  * stream: a hipStream_t (NULL = default stream).  The call only enqueues kernels, under capture too; lens and q_lens are read on
  * the device, so that a graph's replays follow what they hold then.
  * Errors: DBSP_EINVAL, DBSP_ESHAPE (H is no multiple of Hk, sizes too large), DBSP_EHIP.

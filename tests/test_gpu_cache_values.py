@@ -70,3 +70,45 @@ def test_infinities_and_nan_in_a_query_stay_its_own():
         o[0, 1, Nq // 2], lse[0, 1, Nq // 2] = want[0, 1, Nq // 2], want_lse[0, 1, Nq // 2]
         # other running maxima: probabilities rounded anew, half a step each, and O
         assert ((o.float() - want.float()).abs() <= 4 * 2.0 ** -11 * v.float().abs().max()).all() and (lse - want_lse).abs().max() <= 1e-5
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("H, Nq, cap, P", [(2, 2, 250, 0), (2, 2, 250, 900), (4, 20, 250, 0), (4, 20, 250, 900), (2, 250, 700, 0), (2, 250, 40000, 0)])
+def test_scores_as_large_as_they_may_be(H, Nq, cap, P, dtype):
+    """Scores of up to 2^26, whole multiples of 2^18 and so exact in f32: a row has the value of its largest score's key.  That key's probability is formed
+    against a running max that is rounded to f32, a factor of at most 2^4 for all of the row's keys alike; LSE holds it."""
+    import torch
+    import paper_2511_23113_amd as dbsp
+    B, d, dt = 3, 64, {"bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+    g = torch.Generator(device="cuda").manual_seed(H * Nq + P)
+    sign = torch.where(torch.rand(B, H, Nq, device="cuda", generator=g) < 0.5, -1.0, 1.0)
+    q = torch.zeros(B, H, Nq, d, device="cuda")
+    q[..., 0] = 256 * sign
+    n = 250
+    k = torch.zeros(B, 1, cap, d, device="cuda")
+    k[:, 0, :n, 0] = torch.stack([torch.randperm(n, device="cuda", generator=g) for _ in range(B)]) + 5.0
+    v = torch.randn(B, 1, cap, d, device="cuda", generator=g).to(dt)
+    pk, pv = torch.zeros(1, P, d, device="cuda"), torch.randn(1, P, d, device="cuda", generator=g).to(dt)
+    pk[..., 0] = 100.0 + torch.arange(P, device="cuda") % 3           # neither the largest nor the smallest
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    cache = dbsp.KVCache(k.to(dt), v, lens, *((pk.to(dt), pv) if P else ()))
+    o, lse = dbsp.cache_attn_fwd(cache, q.to(dt), causal=False, softmax_scale=1024.0)
+    at = torch.where(sign > 0, k[:, 0, :n, 0].argmax(-1)[:, None, None], k[:, 0, :n, 0].argmin(-1)[:, None, None])
+    want = v[torch.arange(B, device="cuda")[:, None, None], 0, at].double()
+    top = 2.0 ** 18 * torch.where(sign > 0, n + 4.0, -5.0).double()
+    h = torch.finfo(dt).eps / 2
+    assert ((o.double() - want).abs() <= 2 * h * want.abs() * (1 + h)).all()
+    assert ((lse.double() - top).abs() <= 2.0 ** -22 * top.abs()).all()
+
+
+@pytest.mark.parametrize("H, Nq, cap", [(2, 2, 300), (2, 2, 3000), (4, 20, 300), (4, 20, 3000), (2, 250, 300), (2, 250, 40000)])
+def test_bf16_values_of_up_to_2_to_the_80(H, Nq, cap):
+    """f32 sums of 40,000 keys' values, with probabilities of up to 2^10 before they are divided by their sum, stay below 2^106."""
+    import torch
+    import paper_2511_23113_amd as dbsp
+    g = torch.Generator(device="cuda").manual_seed(cap)
+    q, k = (torch.randn(2, n, m, 64, device="cuda", generator=g).bfloat16() for n, m in ((H, Nq), (1, cap)))
+    v = torch.full((2, 1, cap, 64), 2.0 ** 80, device="cuda").bfloat16()
+    lens = torch.full((2,), cap, dtype=torch.int32, device="cuda")
+    o, _ = dbsp.cache_attn_fwd(dbsp.KVCache(k, v, lens), q, causal=False)
+    assert (o.double() / 2.0 ** 80 - 1).abs().max() <= 2 * 2.0 ** -8 * 1.01
