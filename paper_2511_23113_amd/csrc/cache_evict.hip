@@ -28,7 +28,8 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMovesPerGroup = 64;
-// Images a thread: as many as the capacity needs, in four steps (96 of 11,500 used slots of 16,500 66.1 us with 32, 63.9 with 20).
+// Images a thread: as many as the capacity needs, in four steps.  us of a call with 20 / 32: 8 (sequence, head) pairs of 13,000 slots 24.9 / 28.2, 96
+// 46.6 / 49.8, 600 154 / 164, 8 of 20,000 31.0 / 34.7, 96 of 10,000 - 20,000 106.7 / 109.0, 600 of 20,000 187 / 198.
 constexpr int kNT = evict_threads(kEvictWhole);
 
 // Larger weight, larger image; what must stay comes last.

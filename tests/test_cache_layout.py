@@ -40,6 +40,11 @@ def test_a_case_takes_its_way(name):
         assert not got.many and got.joined and tiles_an_item(c, got.pooled) == c["chunk"]
 
 
+def test_rows_are_joined_by_a_workgroup_each_up_to_2048():
+    assert layout(16, 16, 4, 8, 64, 3000, 700, 1, 0).join_by_row == 1      # 2048
+    assert layout(16, 20, 4, 7, 64, 3000, 700, 1, 0).join_by_row == 0      # 2240
+
+
 def test_errors():
     lib, out = B.load_library(), B.CacheLayout(many=7)
     assert lib.dbsp_cache_attn_layout(C.byref(desc()), 4, 1, 1, 1, None) == B.DBSP_EINVAL
