@@ -2,14 +2,15 @@
 //   W[b, hk, slot] = decay W + sum over the rows (token, head of the group) that see the slot of exp2(scale_log2 q.k - LSE2[row]),
 // the scores formed anew, LSE2 (to base 2) from the attention kernel or the merge behind it.
 //
-// Bound by the matrix pipe and the vector pipe alike: 2 d flops and an exponential a (row, key).  A workgroup has 256 keys of
+// 2 d flops and an exponential a (row, key).  Bound by the vector pipe: at d = 128 a step of 32 keys by 32 rows has 8 MFMAs and 51 other vector instructions, and 33
+// more are its share of a tile's copies (addresses from two 64-bit strides) and of its rows; masked steps 33 again, the others jump over them.  A workgroup has 256 keys of
 // a (sequence, KV head), 64 a wave with K as an operand in registers, and goes over the rows in steps of 32, Q by way of the LDS, 64 rows at a
 // time in three places (64 keys a wave, as each operand of Q then feeds two MFMAs).  As in cache_attn_long.hip a step is a sequence
 // of fenced sub-slots: an MFMA of the next step's S^T = K Q^T, two exponentials of this one's, an operand read.  Lane r has
 // row r of a step and sums 32 keys; the lanes are added once, at the end.  Where there are fewer workgroups than the chip
 // holds the rows are cut into p.row_parts, whose sums a small launch adds (2 KV heads of 4 query heads each, 4096 causal queries: 387 us
 // attention included without, 120 so).
-// Measured: 80 (sequence, head) pairs of 4680 keys and 1560 queries (150 GFLOP) 195 us, 770 TFLOP/s; with 32 keys a wave and Q by way of
+// Measured: 80 (sequence, head) pairs of 4680 keys and 1560 queries (150 GFLOP) 180 - 195 us, 770 - 830 TFLOP/s; with 32 keys a wave and Q by way of
 // registers 320.
 #include <hip/hip_runtime.h>
 
