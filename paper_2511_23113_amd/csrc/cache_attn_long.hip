@@ -11,7 +11,8 @@
 // The running max is not looked for: probabilities are formed against it as it stands, and only where a lane's sum of a unit's 16
 // passes kRaiseAt (some score is far above it) is it raised, O rescaled and the unit's probabilities formed anew.
 // Measured: 40 heads of 2 sequences, 1560 queries over 12,870 keys, d = 128 (822 GFLOP) 771 us, 1066 TFLOP/s where a large bf16 product
-// reaches 1212 (750 - 810 from card to card once the clock has settled, up to 990 in the first dozen launches of a process); 16 heads on 4, 8192 causal queries, 249 us, 1100 TFLOP/s.  The first loses 13 % to its last row tiles, which hold 24 rows of
+// reaches 1212 (750 - 810 from card to card once the clock has settled, up to 990 in the first dozen launches of a process); 16 heads on 4, 8192
+// causal queries, 249 us, 1100 TFLOP/s.  The first loses 13 % to its last row tiles, which hold 24 rows of
 // 256.  A tile of 64 keys takes a wave 3300 clocks, 2048 of them MFMAs; leaving out the operand reads takes 17 % off, the copies
 // 8 %, the exponentials 9 %, the barrier 1 % (wrong results, same addresses).  At d = 64 two exponentials for every one at d = 128 and
 // MFMA bound it: 48 heads, 4101 causal queries (119 GFLOP) 149 us, 800 TFLOP/s.

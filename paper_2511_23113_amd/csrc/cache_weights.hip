@@ -2,8 +2,9 @@
 //   W[b, hk, slot] = decay W + sum over the rows (token, head of the group) that see the slot of exp2(scale_log2 q.k - LSE2[row]),
 // the scores formed anew, LSE2 (to base 2) from the attention kernel or the merge behind it.
 //
-// 2 d flops and an exponential a (row, key).  Bound by the vector pipe: at d = 128 a step of 32 keys by 32 rows has 8 MFMAs and 51 other vector instructions, and 33
-// more are its share of a tile's copies (addresses from two 64-bit strides) and of its rows; masked steps 33 again, the others jump over them.  A workgroup has 256 keys of
+// 2 d flops and an exponential a (row, key).  Bound by the vector pipe: at d = 128 a step of 32 keys by 32 rows has 8 MFMAs and 51 other vector
+// instructions, and 33 more are its share of a tile's copies (addresses from two 64-bit strides), of its rows and of the kernel's ends; a masked step has
+// another 33, which the others jump over.  A workgroup has 256 keys of
 // a (sequence, KV head), 64 a wave with K as an operand in registers, and goes over the rows in steps of 32, Q by way of the LDS, 64 rows at a
 // time in three places (64 keys a wave, as each operand of Q then feeds two MFMAs).  As in cache_attn_long.hip a step is a sequence
 // of fenced sub-slots: an MFMA of the next step's S^T = K Q^T, two exponentials of this one's, an operand read.  Lane r has

@@ -6,6 +6,7 @@ import pytest
 
 from paper_2511_23113_amd import binding as B
 from test_abi_cache import FAKE, desc
+from test_gpu_cache_attn import MANY
 from test_gpu_cache_paths import PATHS
 
 
@@ -38,6 +39,12 @@ def test_a_case_takes_its_way(name):
     assert {k: getattr(got, k) for k in c["layout"]} == c["layout"]
     if c["chunk"] is not None:
         assert not got.many and got.joined and tiles_an_item(c, got.pooled) == c["chunk"]
+
+
+@pytest.mark.parametrize("name", MANY)
+def test_cases_of_many_rows_go_to_the_kernel_for_many_queries(name):
+    B_, H, Hk, Nq, d, P, cap, _, _, causal, _, decay = MANY[name]
+    assert layout(B_, H, Hk, Nq, d, P, cap, causal, decay is not None).many == 1
 
 
 def test_rows_are_joined_by_a_workgroup_each_up_to_2048():
