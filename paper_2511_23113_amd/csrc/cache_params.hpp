@@ -32,7 +32,7 @@ constexpr int kWeightKeys = 256;       // own keys of a workgroup that forms the
 // Rows up to which a workgroup joins the parts of one, else of 8 or 16: so much the better the more parts a row has.  us of a call by one /
 // by several: 300 rows 14.4 / 20.9, behind 60,000 keys 45 / 68, 480 at d = 64 14.5 / 23.4, 768 23.0 / 23.8, behind 20,000 37 / 46, 1000 at d = 64
 // 19.0 / 19.4, 1536 behind 8000 28.6 / 30.6, behind 40,000 58.8 / 61.8; but 1920 behind 2000 27.3 / 25.0, 2304 of 3000 own keys 70.8 / 66.5, 2560 behind
-// 16,384 120.6 / 118, 3072 of 4000 30.1 / 25.7, 3072 of one KV head behind 60,000 117 / 117, 3200 at d = 64 28.6 / 23.3, 5040 37.0 / 28.4, 12,000 50 / 29.
+// 16,384 120.6 / 118, 2400 at d = 64 behind 60,000 70.4 / 70.2, 3200 behind 4096 28.6 / 23.3, 5040 37.0 / 28.4, 12,000 of 1500 own keys 50 / 29.
 constexpr int kMergeRows = 2048;
 constexpr int kScoreSlots = 1024;      // own keys of a workgroup that sums kept scores, four a thread
 constexpr int kEvictWhole = 32768;     // slots that a workgroup chooses among by itself: what its registers hold; and those of a
