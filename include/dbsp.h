@@ -301,6 +301,137 @@ int dbsp_cache_evict(const dbsp_cache* cache, int32_t budget, int32_t sinks, con
 int dbsp_cache_evict_workspace(const dbsp_cache* cache, int32_t budget, int64_t* bytes);
 
 /*
+ * Queries and keys as attention takes them, out of a projection's output: each head's norm and the rotation by its token's position in one
+ * pass, from any strides to any strides.  A row is one head of one token, x[0 .. d - 1]:
+ *   norm:      n = (x - mu) r gain + bias,  r = 1 / sqrt(mean((x - mu)^2) + eps),  mu = 0 (DBSP_NORM_RMS) or mean(x) (DBSP_NORM_LAYER);
+ *              n = x (DBSP_NORM_NONE);
+ *   rotation:  pair p (of R = sum of pairs[]; the first pairs[0] belong to axis 0, and so on) has the angle
+ *              a = position[its axis] * freqs[p], and (n1, n2) becomes (n1 cos a - n2 sin a, n1 sin a + n2 cos a).  Its places are
+ *              (2p, 2p + 1), or with `halves` (p, p + R).  Places from 2R on keep n.
+ * Norms and rotations are f32, angles 64 bits (off by 2^-51 |position freq| and 2^-22 at most); the result is rounded once.
+ */
+enum { DBSP_NORM_NONE = 0, DBSP_NORM_RMS = 1, DBSP_NORM_LAYER = 2 };
+typedef struct dbsp_head_norm {
+  int32_t kind;               /* DBSP_NORM_* */
+  int32_t gains_f32;          /* 1: gains and biases are f32, 0: of the rows' type */
+  float eps;                  /* positive and finite; not looked at with DBSP_NORM_NONE */
+  /* device, [d], 16-byte aligned, shared by all heads; a NULL gain is 1, a NULL bias 0.  Not looked at with DBSP_NORM_NONE */
+  const void *q_gain, *k_gain, *q_bias, *k_bias;
+} dbsp_head_norm;
+typedef struct dbsp_rotary {
+  int32_t axes;               /* 0 (no rotation) to 4 */
+  int32_t halves;             /* 0: pairs are neighbours; 1: R apart, R a multiple of 4 */
+  int32_t pairs[4];           /* of every axis, at least 1; at most d / 2 in all */
+  const double* freqs;        /* HOST, [R]: radians per unit of position, finite; read during the call only */
+} dbsp_rotary;
+
+/*
+ * dbsp_qk_norm_rope_fwd -- of N tokens of B sequences, H query heads and Hk key heads (k == NULL: no keys, Hk is not looked at).
+ *
+ * dtype: DBSP_BF16 or DBSP_FP16, of q, k and their results alike.  d: 64 or 128.
+ * q, k:  device, [B, H, N, d] and [B, Hk, N, d] with strides in elements (batch, head, token; multiples of 8, at least 0, a token's at most
+ *        2^24; that of a dimension of one is not looked at; d has stride 1), 16-byte aligned.
+ * q_out, k_out: device, written, as q and k with strides of their own, no two elements in one place.  They overlap no input, but may be
+ *        q and k themselves with the same strides.
+ * norm, rotary: host, may be NULL (none).  positions: device, int32 [B, N, axes] with strides in elements (batch, token; at least 0; an axis' is 1),
+ *        or NULL with at most one axis: a token's place in its sequence, 0 .. N - 1.
+ * An infinite value or a NaN spoils its own row only.  With a norm, bf16 values of 2^60 or more in magnitude overflow its sums.
+ * stream: a hipStream_t (NULL = default stream).  The call only enqueues one kernel, under capture too.
+ * Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large), DBSP_EHIP.
+ */
+int dbsp_qk_norm_rope_fwd(int32_t dtype, int32_t B, int32_t N, int32_t d, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
+                          void* q_out, int64_t q_out_batch, int64_t q_out_head, int64_t q_out_token, int32_t H, const void* k, int64_t k_batch,
+                          int64_t k_head, int64_t k_token, void* k_out, int64_t k_out_batch, int64_t k_out_head, int64_t k_out_token, int32_t Hk,
+                          const dbsp_head_norm* norm, const dbsp_rotary* rotary, const int32_t* positions, int64_t pos_batch, int64_t pos_token,
+                          void* stream);
+
+/*
+ * dbsp_qk_norm_rope_bwd -- the gradients of a dbsp_qk_norm_rope_fwd call with the same arguments: from q, k and the gradients dq_out, dk_out of
+ * its results those of q, k and of gains and biases,
+ *   dn = the rotation by -a of dy,  dgain = sum dn (x - mu) r,  dbias = sum dn,  e = dn gain,
+ *   dx = r (e - mean(e (x - mu) r) (x - mu) r - [DBSP_NORM_LAYER: mean(e)]),  dx = dn without a norm,
+ * the sums over all rows of all tokens, heads and sequences.
+ *
+ * dq, dk: device, written, as q_out and k_out above (they may be dq_out and dk_out with the same strides).  Every row's gradient is
+ *        written: where tokens are padding, zeros in dq_out and dk_out keep them out of all gradients.
+ * grads: device, f32 [4, d] contiguous, 16-byte aligned, written: of q's gain, k's gain, q's bias, k's bias (zeros for k == NULL; those of gains
+ *        that are NULL as if they were there); NULL: not formed, and must be NULL without a norm.
+ * workspace: device, 256-byte aligned, of the size that dbsp_qk_norm_rope_bwd_workspace gives (NULL where that is 0, as without grads); written by
+ *        the call, holds nothing between calls.  Calls under way at the same time need one each.
+ * f32 accumulation; the same call gives the same bits.  stream, errors: as above; enqueues one kernel, and a second one for grads.
+ */
+int dbsp_qk_norm_rope_bwd(int32_t dtype, int32_t B, int32_t N, int32_t d, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
+                          const void* dq_out, int64_t dq_out_batch, int64_t dq_out_head, int64_t dq_out_token, void* dq, int64_t dq_batch,
+                          int64_t dq_head, int64_t dq_token, int32_t H, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token,
+                          const void* dk_out, int64_t dk_out_batch, int64_t dk_out_head, int64_t dk_out_token, void* dk, int64_t dk_batch,
+                          int64_t dk_head, int64_t dk_token, int32_t Hk, const dbsp_head_norm* norm, const dbsp_rotary* rotary,
+                          const int32_t* positions, int64_t pos_batch, int64_t pos_token, float* grads, void* workspace, int64_t workspace_bytes,
+                          void* stream);
+int dbsp_qk_norm_rope_bwd_workspace(int32_t B, int32_t N, int32_t d, int32_t H, int32_t Hk, int64_t* bytes);
+
+/*
+ * A paged key/value cache: keys and values in the pages of a pool that sequences of any lengths share, in the caller's memory.  Page
+ * pages[b][i] of the pool holds the slots i * page_size .. of sequence b, in any order of pages; what the table names may be
+ * changed between calls (pages appended, given back, shared by sequences with the same beginning).  An entry that is no page of the pool
+ * (negative, or n_pages and more) means that its slots hold no keys: they are not written, and no query sees them.
+ * G query heads share a KV head as above.  The struct is read during the calls only; calls that use the same cache must not overlap on the
+ * device where one of them writes what another uses.
+ */
+typedef struct dbsp_paged_cache {
+  int32_t dtype;              /* DBSP_BF16 or DBSP_FP16: of K, V, Q and O alike */
+  int32_t B, Hk, d;           /* sequences, KV heads, head dim (64 or 128) */
+  int32_t n_pages, page_size; /* of the pool; a page's slots may be any number */
+  int32_t max_pages;          /* entries of a sequence's table; it has max_pages * page_size slots, below 2^30 */
+  void *k, *v;                /* device, [n_pages, Hk, page_size, d], 16-byte aligned */
+  /* strides in elements, of page, head and slot; d has stride 1.  Multiples of 8, at least 0, a slot's at most 2^24 (that of a dimension of one is
+   * not looked at).  dbsp_paged_append writes k and v: no two of their elements may share a place */
+  int64_t k_stride[3], v_stride[3];
+  const int32_t* pages;       /* device, int32 [B, max_pages], the sequences pages_stride elements apart (at least max_pages) */
+  int64_t pages_stride;
+  const int32_t* lens;        /* device, int32 [B]: used slots; taken as 0 below 0 and as max_pages * page_size above it */
+} dbsp_paged_cache;
+
+/*
+ * dbsp_paged_append -- writes the keys and values of each sequence's newest tokens into its last used slots, token t of n = new_lens[b] into
+ * slot lens[b] - n + t: lens counts the new tokens already, and is not written.  Keys get norm and rotation on the way (see
+ * dbsp_qk_norm_rope_fwd), values none, and so do the tokens' queries, which go to q_out (q == NULL: none).
+ *
+ * k, v: device, [B, Hk, Nn, d]; q, q_out: device, [B, H, Nn, d], all with strides in elements as for dbsp_qk_norm_rope_fwd; q_out overlaps
+ *       no other, but may be q with the same strides.  None of them overlaps the pool.
+ * new_lens: device, int32 [B], taken as 0 below 0 and as Nn above it; NULL: Nn each.  Tokens t >= new_lens[b] are not looked at, and their rows
+ *       of q_out are left as they were; so are the rows of tokens whose slot would lie before slot 0 (new_lens[b] > lens[b]).
+ * norm, rotary: as for dbsp_qk_norm_rope_fwd.  positions: device, int32 [B, Nn, axes] with strides as there; NULL with at most one axis: a
+ *       token's position is its slot.
+ * Tokens whose page is none (see dbsp_paged_cache) are not written; their queries are.  Where two tokens have one place, by a page that two sequences
+ * share, either of them is there afterwards.
+ * stream: as above; enqueues one kernel.  Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large), DBSP_EHIP.
+ */
+int dbsp_paged_append(const dbsp_paged_cache* cache, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token, const void* v,
+                      int64_t v_batch, int64_t v_head, int64_t v_token, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
+                      void* q_out, int64_t q_out_batch, int64_t q_out_head, int64_t q_out_token, int32_t H, int32_t Nn, const int32_t* new_lens,
+                      const dbsp_head_norm* norm, const dbsp_rotary* rotary, const int32_t* positions, int64_t pos_batch, int64_t pos_token,
+                      void* stream);
+
+/*
+ * dbsp_paged_attn_fwd -- attention of each sequence's Nq newest tokens over its pages:
+ *   s = softmax_scale q.k,  LSE = ln(sum exp(s)),  O = sum exp(s - LSE) v,
+ * the sums over the slots j < lens[b] whose page is there, and with `causal` for query t only j <= lens[b] - q_lens[b] + t.  Made for one token or
+ * a few: K and V are read once for every 32 rows Nq G of a KV head (64 at d = 64).
+ *
+ * q, o, lse, q_lens, H, Nq, causal, softmax_scale, stream: as for dbsp_cache_attn_fwd, with the same limits: K and V are finite in
+ *      every used slot whose page is there; nothing else of the pool is read.
+ * workspace: device, 256-byte aligned, of at least the size that dbsp_paged_attn_workspace gives for the same cache, H and Nq (NULL where that
+ *      is 0); written by the call, holds nothing between calls.  Calls under way at the same time need one each.
+ * The call only enqueues kernels, under capture too; lens, q_lens and pages are read on the device, so that a graph's replays follow what
+ * they hold then.  The same call gives the same bits, in whatever order the pages lie.
+ * Errors: DBSP_EINVAL, DBSP_ESHAPE (H is no multiple of Hk, sizes too large), DBSP_EHIP.
+ */
+int dbsp_paged_attn_fwd(const dbsp_paged_cache* cache, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token, void* o,
+                        int64_t o_batch, int64_t o_head, int64_t o_token, float* lse, const int32_t* q_lens, int32_t H, int32_t Nq,
+                        int32_t causal, float softmax_scale, void* workspace, int64_t workspace_bytes, void* stream);
+int dbsp_paged_attn_workspace(const dbsp_paged_cache* cache, int32_t H, int32_t Nq, int64_t* bytes);
+
+/*
  * imbalance_ratio -- Eq. 1 on a host matrix work[periods][partitions] (row-major, int64, >= 0):
  * rho = sum_i max_g work[i][g] / (sum_{i,g} work[i][g] / partitions), in double.  Zero total
  * work gives 1.0.  Errors: DBSP_EINVAL (null pointer, non-positive size, negative entry).

@@ -11,22 +11,29 @@ from .binding import (  # noqa: F401
     DBSP_ESHAPE,
     DBSP_OK,
     DbspError,
+    HeadNorm,
     KVCache,
     MODE_BALANCED,
     MODE_NAIVE,
     MODE_REWARD,
     MODE_ROUNDS,
+    PagedKVCache,
     Plan,
+    Rotary,
     cache_attn_fwd,
     cache_evict,
     fit_cost_model,
     imbalance_ratio,
     load_library,
     mfma_probe,
+    paged_append,
+    paged_attn_fwd,
     partition_blocks,
     partition_heads,
     plan_sparse_attn,
     plan_sparse_attn_reuse,
+    qk_norm_rope_bwd,
+    qk_norm_rope_fwd,
     ring_work,
     sparse_attn_fwd,
 )

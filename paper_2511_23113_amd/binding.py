@@ -30,6 +30,8 @@ EXPORTS = (
     "dbsp_partition_heads", "dbsp_partition_blocks", "dbsp_ring_work", "dbsp_fit_cost_model", "dbsp_mfma_probe", "dbsp_plan_run_order",
     "dbsp_cache_attn_fwd", "dbsp_cache_attn_workspace", "dbsp_cache_evict", "dbsp_cache_evict_workspace",
     "dbsp_cache_attn_layout",
+    "dbsp_qk_norm_rope_fwd", "dbsp_qk_norm_rope_bwd", "dbsp_qk_norm_rope_bwd_workspace",
+    "dbsp_paged_append", "dbsp_paged_attn_fwd", "dbsp_paged_attn_workspace",
 )
 
 
@@ -57,6 +59,21 @@ class CacheDesc(C.Structure):
 class CacheLayout(C.Structure):
     """dbsp_cache_layout of dbsp_diag.h."""
     _fields_ = [(name, C.c_int32) for name in ("many", "pooled", "joined", "join_by_row", "row_tiles", "cut", "parts", "longest_first", "scores_kept", "weight_parts")]
+
+
+class HeadNormDesc(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("gains_f32", C.c_int32), ("eps", C.c_float), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p),
+                ("q_bias", C.c_void_p), ("k_bias", C.c_void_p)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("axes", C.c_int32), ("halves", C.c_int32), ("pairs", C.c_int32 * 4), ("freqs", C.POINTER(C.c_double))]
+
+
+class PagedCacheDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("Hk", C.c_int32), ("d", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("max_pages", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("pages", C.c_void_p), ("pages_stride", C.c_int64), ("lens", C.c_void_p)]
 
 
 _lib = None
@@ -121,6 +138,20 @@ def load_library(path: str | None = None):
     lib.dbsp_cache_evict.restype = C.c_int
     lib.dbsp_cache_evict_workspace.argtypes = [cache, i32, i64p]
     lib.dbsp_cache_evict_workspace.restype = C.c_int
+    norm, rotary, paged, rows = C.POINTER(HeadNormDesc), C.POINTER(RotaryDesc), C.POINTER(PagedCacheDesc), [vp, i64, i64, i64]
+    at = [vp, i64, i64]
+    lib.dbsp_qk_norm_rope_fwd.argtypes = [i32] * 4 + (rows + rows + [i32]) * 2 + [norm, rotary] + at + [vp]
+    lib.dbsp_qk_norm_rope_fwd.restype = C.c_int
+    lib.dbsp_qk_norm_rope_bwd.argtypes = [i32] * 4 + (rows + rows + rows + [i32]) * 2 + [norm, rotary] + at + [vp, vp, i64, vp]
+    lib.dbsp_qk_norm_rope_bwd.restype = C.c_int
+    lib.dbsp_qk_norm_rope_bwd_workspace.argtypes = [i32] * 5 + [i64p]
+    lib.dbsp_qk_norm_rope_bwd_workspace.restype = C.c_int
+    lib.dbsp_paged_append.argtypes = [paged] + rows * 4 + [i32, i32, vp, norm, rotary] + at + [vp]
+    lib.dbsp_paged_append.restype = C.c_int
+    lib.dbsp_paged_attn_fwd.argtypes = [paged] + rows * 2 + [vp, vp, i32, i32, i32, f32, vp, i64, vp]
+    lib.dbsp_paged_attn_fwd.restype = C.c_int
+    lib.dbsp_paged_attn_workspace.argtypes = [paged, i32, i32, i64p]
+    lib.dbsp_paged_attn_workspace.restype = C.c_int
     lib.dbsp_plan_destroy.argtypes = [vp]
     lib.dbsp_plan_destroy.restype = None
     lib.dbsp_plan_release.argtypes = [vp]
@@ -341,7 +372,55 @@ def _torch_module():
     return _torch
 
 
-class KVCache:
+class _OnDevice:
+    """What has tensors on a GPU (device, _index) and is called on streams."""
+
+    def _on(self, stream):
+        """The raw stream, and whether tensors made on torch's current one are used on another."""
+        torch = _torch
+        if self._index != torch._C._cuda_getDevice():
+            raise ValueError("the cache lives on another device than the current one")
+        now = torch._C._cuda_getCurrentRawStream(self._index)
+        if stream is None:
+            return now, False
+        if isinstance(stream, int):
+            return stream, stream != now
+        if getattr(stream, "device", self.device) != self.device:
+            raise ValueError("the stream is of another device than the cache")
+        raw = stream.cuda_stream
+        return raw, raw != now
+
+    def _empty(self, shape, dtype, raw, elsewhere):
+        """A tensor for a call on the stream raw.  Memory that torch's current stream has freed may still be used there, so for a call
+        elsewhere it comes from that stream's; freed, it waits for what the current stream has been given until then."""
+        torch = _torch
+        if not elsewhere:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        # (an ExternalStream of handle 0 would be some stream of torch's pool, not the default stream)
+        on = torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(on):
+            x = torch.empty(shape, dtype=dtype, device=self.device)
+        x.record_stream(torch.cuda.current_stream(self.device))
+        return x
+
+    def _workspace(self, workspace, key, ask, raw, elsewhere):
+        """The caller's workspace, or one of the size that a call with these sizes (key) needs; its address and size."""
+        torch = _torch
+        if workspace is None:
+            need = self._bytes.get(key)
+            if need is None:
+                out = C.c_int64()
+                _check(ask(self._at, *key, C.byref(out)))
+                need = self._bytes[key] = out.value
+            if need == 0:
+                return None, None, 0
+            workspace = self._empty(need, torch.uint8, raw, elsewhere)
+        elif workspace.dtype != torch.uint8 or workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError("the workspace must be a contiguous uint8 tensor on the cache's GPU")
+        return workspace, workspace.data_ptr(), workspace.numel()
+
+
+class KVCache(_OnDevice):
     """A key/value cache of the caller's tensors (see dbsp.h: dbsp_cache), for cache_attn_fwd and cache_evict.
 
     k, v: [B, Hk, capacity, d], bf16 or fp16 on one GPU, d in (64, 128) dense, other strides multiples of 8 elements; the first
@@ -395,50 +474,6 @@ class KVCache:
         other._desc.B = other.B = B
         other._at, other._bytes = C.byref(other._desc), {}
         return other
-
-    def _on(self, stream):
-        """The raw stream, and whether tensors made on torch's current one are used on another."""
-        torch = _torch
-        if self._index != torch._C._cuda_getDevice():
-            raise ValueError("the cache lives on another device than the current one")
-        now = torch._C._cuda_getCurrentRawStream(self._index)
-        if stream is None:
-            return now, False
-        if isinstance(stream, int):
-            return stream, stream != now
-        if getattr(stream, "device", self.device) != self.device:
-            raise ValueError("the stream is of another device than the cache")
-        raw = stream.cuda_stream
-        return raw, raw != now
-
-    def _empty(self, shape, dtype, raw, elsewhere):
-        """A tensor for a call on the stream raw.  Memory that torch's current stream has freed may still be used there, so for a call
-        elsewhere it comes from that stream's; freed, it waits for what the current stream has been given until then."""
-        torch = _torch
-        if not elsewhere:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        # (an ExternalStream of handle 0 would be some stream of torch's pool, not the default stream)
-        on = torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream(self.device)
-        with torch.cuda.stream(on):
-            x = torch.empty(shape, dtype=dtype, device=self.device)
-        x.record_stream(torch.cuda.current_stream(self.device))
-        return x
-
-    def _workspace(self, workspace, key, ask, raw, elsewhere):
-        """The caller's workspace, or one of the size that a call with these sizes (key) needs; its address and size."""
-        torch = _torch
-        if workspace is None:
-            need = self._bytes.get(key)
-            if need is None:
-                out = C.c_int64()
-                _check(ask(self._at, *key, C.byref(out)))
-                need = self._bytes[key] = out.value
-            if need == 0:
-                return None, None, 0
-            workspace = self._empty(need, torch.uint8, raw, elsewhere)
-        elif workspace.dtype != torch.uint8 or workspace.device != self.device or not workspace.is_contiguous():
-            raise ValueError("the workspace must be a contiguous uint8 tensor on the cache's GPU")
-        return workspace, workspace.data_ptr(), workspace.numel()
 
 
 def cache_attn_fwd(cache: KVCache, q, q_lens=None, causal: bool = True, decay=None, o=None, lse=None, softmax_scale: float = 0.0,
@@ -499,6 +534,295 @@ def cache_evict(cache: KVCache, budget: int, sinks: int = 0, keep_from=None, str
     rc = _lib.dbsp_cache_evict(cache._at, budget, sinks, None if keep_from is None else keep_from.data_ptr(), at, size, raw)
     if rc:
         _check(rc)
+
+
+_NORMS = {"rms": 1, "layer": 2}
+
+
+class HeadNorm:
+    """The norm of each head of queries and keys (see dbsp.h: dbsp_head_norm): kind "rms" or "layer"; gains and biases are [d] tensors on the
+    GPU, all f32 or all of the rows' type, and a missing one is 1 or 0.  The object keeps the tensors, which the caller goes on writing."""
+
+    def __init__(self, q_gain=None, k_gain=None, q_bias=None, k_bias=None, kind: str = "rms", eps: float = 1e-6):
+        torch = _torch_module()
+        load_library()
+        if kind not in _NORMS:
+            raise ValueError('kind is "rms" or "layer"')
+        self.given = {name: x for name, x in (("q_gain", q_gain), ("k_gain", k_gain), ("q_bias", q_bias), ("k_bias", k_bias)) if x is not None}
+        self.kind, self.eps, self.dtype, self.device, self.d = kind, float(eps), None, None, None
+        desc = HeadNormDesc(kind=_NORMS[kind], eps=self.eps)
+        for name, x in self.given.items():
+            if x.dtype not in (torch.float32, torch.bfloat16, torch.float16) or x.dim() != 1 or not x.is_cuda or not x.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous [d] tensor of f32, bf16 or fp16 on the GPU")
+            if self.dtype is not None and (x.dtype != self.dtype or x.device != self.device or x.shape[0] != self.d):
+                raise ValueError("gains and biases differ in type, device or size")
+            self.dtype, self.device, self.d = x.dtype, x.device, x.shape[0]
+            setattr(desc, name, x.data_ptr())
+        desc.gains_f32 = self.dtype == torch.float32
+        self._desc, self._at = desc, C.byref(desc)
+
+    def _of(self, x):
+        """What a call on tensors like x passes on."""
+        if self.d is not None and (self.device != x.device or self.d != x.shape[-1] or (self.dtype != x.dtype and not self._desc.gains_f32)):
+            raise ValueError("gains and biases must be [d], f32 or of the rows' type, on their GPU")
+        return self._at
+
+
+class Rotary:
+    """A rotation by positions on one to four axes (see dbsp.h: dbsp_rotary).  pairs: how many pairs of a head each axis turns; pair i of an
+    axis with n of them by theta^(-i / n) a unit, or freqs says so for all pairs, axis by axis.  halves: a pair's two places are R apart (R all
+    pairs) instead of neighbours."""
+
+    def __init__(self, pairs, theta: float = 10000.0, halves: bool = False, freqs=None):
+        load_library()
+        self.pairs = tuple(int(n) for n in pairs)
+        if not 1 <= len(self.pairs) <= 4 or min(self.pairs) < 1:
+            raise ValueError("a rotation has one to four axes of at least one pair each")
+        self.halves = bool(halves)
+        self.freqs = tuple(float(f) for f in freqs) if freqs is not None else tuple(float(theta) ** (-i / n) for n in self.pairs for i in range(n))
+        if len(self.freqs) != sum(self.pairs):
+            raise ValueError("freqs must hold one value per pair")
+        self._freqs = (C.c_double * len(self.freqs))(*self.freqs)
+        desc = RotaryDesc(axes=len(self.pairs), halves=self.halves, freqs=self._freqs)
+        desc.pairs[:len(self.pairs)] = self.pairs
+        self._desc, self._at = desc, C.byref(desc)
+
+
+class _Rows(_OnDevice):
+    """Where a call of q's type and device runs."""
+
+    def __init__(self, device):
+        self.device, self._index = device, device.index
+
+
+_rows_on = {}
+
+
+def _on_rows(device):
+    here = _rows_on.get(device)
+    if here is None:
+        here = _rows_on[device] = _Rows(device)
+    return here
+
+
+def _check_rows(name, x, like, shape):
+    if x.shape != shape or x.dtype != like.dtype or x.device != like.device or x.stride(3) != 1:
+        raise ValueError(f"{name} must be {list(shape)} of the same type on the same GPU, with a dense last dimension")
+
+
+def _positions(positions, rotary, B, N, device):
+    """Address and strides (batch, token) of positions [N, axes] or [B, N, axes]."""
+    if positions is None or rotary is None:
+        return None, 0, 0
+    torch = _torch
+    axes, shape = len(rotary.pairs), positions.shape
+    if positions.dtype != torch.int32 or positions.device != device or len(shape) not in (2, 3) or shape[-2:] != (N, axes) or positions.stride(-1) != 1 and axes > 1:
+        raise ValueError("positions must be int32 [N, axes] or [B, N, axes] on the same GPU, with a dense last dimension")
+    if len(shape) == 3 and shape[0] != B:
+        raise ValueError("positions and tokens differ in the number of sequences")
+    return positions.data_ptr(), positions.stride(0) if len(shape) == 3 else 0, positions.stride(-2)
+
+
+def _first_rows(q):
+    torch = _torch_module()
+    if q.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float16) or not q.is_cuda or q.stride(3) != 1:
+        raise ValueError("q must be [B, H, N, d] in bf16 or fp16 on a GPU, with a dense last dimension")
+    return torch
+
+
+def _k_shape(q, k):
+    B, _, N, d = q.shape
+    if k.dim() != 4:
+        raise ValueError("k must be [B, Hk, N, d]")
+    return (B, k.shape[1], N, d)
+
+
+def qk_norm_rope_fwd(q, k=None, norm: HeadNorm = None, rotary: Rotary = None, positions=None, q_out=None, k_out=None, stream=None):
+    """Queries [B, H, N, d] and keys [B, Hk, N, d] of a projection (any strides: views into its output) with each head's norm and the rotation
+    by positions (int32 [N, axes] or [B, N, axes]; None with one axis: 0 .. N - 1), as contiguous tensors or in q_out and k_out
+    (see dbsp.h: dbsp_qk_norm_rope_fwd).  Enqueues on `stream` (default: torch's current stream) and returns (q_out, k_out)."""
+    _first_rows(q)
+    lib = load_library()
+    B, H, N, d = q.shape
+    here = _on_rows(q.device)
+    raw, elsewhere = here._on(stream)
+    if q_out is None:
+        q_out = here._empty(q.shape, q.dtype, raw, elsewhere)
+    else:
+        _check_rows("q_out", q_out, q, q.shape)
+    Hk, k_at, k_s, k_out_at, k_out_s = 0, None, (0, 0, 0), None, (0, 0, 0)
+    if k is not None:
+        shape = _k_shape(q, k)
+        _check_rows("k", k, q, shape)
+        Hk = shape[1]
+        if k_out is None:
+            k_out = here._empty(shape, q.dtype, raw, elsewhere)
+        else:
+            _check_rows("k_out", k_out, q, shape)
+        k_at, k_s, k_out_at, k_out_s = k.data_ptr(), k.stride(), k_out.data_ptr(), k_out.stride()
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    pos, pos_b, pos_t = _positions(positions, rotary, B, N, q.device)
+    q_s, o_s = q.stride(), q_out.stride()
+    rc = lib.dbsp_qk_norm_rope_fwd(q.dtype == _torch.float16, B, N, d, q.data_ptr(), q_s[0], q_s[1], q_s[2], q_out.data_ptr(), o_s[0], o_s[1], o_s[2], H,
+                                   k_at, k_s[0], k_s[1], k_s[2], k_out_at, k_out_s[0], k_out_s[1], k_out_s[2], Hk,
+                                   None if norm is None else norm._of(q), None if rotary is None else rotary._at, pos, pos_b, pos_t, raw)
+    if rc:
+        _check(rc)
+    return q_out, k_out
+
+
+def qk_norm_rope_bwd(q, k, dq_out, dk_out, norm: HeadNorm = None, rotary: Rotary = None, positions=None, dq=None, dk=None, stream=None, workspace=None):
+    """Gradients of a qk_norm_rope_fwd call: from its q, k (or None), norm, rotary and positions and the gradients of its results, those of q and k
+    (contiguous tensors, or dq and dk, which may be views into the gradient of a projection's output), and of the gains and biases that the
+    norm has, f32 [d] by name (see dbsp.h: dbsp_qk_norm_rope_bwd).  Enqueues on `stream` and returns (dq, dk, gains)."""
+    torch = _first_rows(q)
+    lib = load_library()
+    B, H, N, d = q.shape
+    here = _on_rows(q.device)
+    raw, elsewhere = here._on(stream)
+    _check_rows("dq_out", dq_out, q, q.shape)
+    if dq is None:
+        dq = here._empty(q.shape, q.dtype, raw, elsewhere)
+    else:
+        _check_rows("dq", dq, q, q.shape)
+    Hk, none = 0, (None, (0, 0, 0))
+    k_, dk_out_, dk_ = none, none, none
+    if k is not None:
+        shape = _k_shape(q, k)
+        _check_rows("k", k, q, shape)
+        if dk_out is None:
+            raise ValueError("k without dk_out")
+        _check_rows("dk_out", dk_out, q, shape)
+        Hk = shape[1]
+        if dk is None:
+            dk = here._empty(shape, q.dtype, raw, elsewhere)
+        else:
+            _check_rows("dk", dk, q, shape)
+        k_, dk_out_, dk_ = ((x.data_ptr(), x.stride()) for x in (k, dk_out, dk))
+    elif dk_out is not None or dk is not None:
+        raise ValueError("dk_out or dk without k")
+    norm_at = None if norm is None else norm._of(q)
+    grads = at = None
+    size = 0
+    if norm is not None and norm.given:
+        grads = here._empty((4, d), torch.float32, raw, elsewhere)
+        if workspace is None:
+            need = C.c_int64()
+            _check(lib.dbsp_qk_norm_rope_bwd_workspace(B, N, d, H, Hk, C.byref(need)))
+            workspace = here._empty(need.value, torch.uint8, raw, elsewhere)
+        elif workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
+            raise ValueError("the workspace must be a contiguous uint8 tensor on q's GPU")
+        at, size = workspace.data_ptr(), workspace.numel()
+    pos, pos_b, pos_t = _positions(positions, rotary, B, N, q.device)
+    q_s, y_s, x_s = q.stride(), dq_out.stride(), dq.stride()
+    rc = lib.dbsp_qk_norm_rope_bwd(q.dtype == torch.float16, B, N, d, q.data_ptr(), q_s[0], q_s[1], q_s[2], dq_out.data_ptr(), y_s[0], y_s[1], y_s[2],
+                                   dq.data_ptr(), x_s[0], x_s[1], x_s[2], H, k_[0], k_[1][0], k_[1][1], k_[1][2], dk_out_[0], dk_out_[1][0], dk_out_[1][1],
+                                   dk_out_[1][2], dk_[0], dk_[1][0], dk_[1][1], dk_[1][2], Hk, norm_at, None if rotary is None else rotary._at,
+                                   pos, pos_b, pos_t, None if grads is None else grads.data_ptr(), at, size, raw)
+    if rc:
+        _check(rc)
+    names = ("q_gain", "k_gain", "q_bias", "k_bias")
+    return dq, dk, {} if grads is None else {name: grads[names.index(name)] for name in norm.given if k is not None or name[0] == "q"}
+
+
+class PagedKVCache(_OnDevice):
+    """A key/value cache in pages of the caller's tensors (see dbsp.h: dbsp_paged_cache), for paged_append and paged_attn_fwd.
+
+    k, v: the pool, [n_pages, Hk, page_size, d], bf16 or fp16 on one GPU, d in (64, 128) dense, other strides multiples of 8 elements (a pool of
+    [n_pages, page_size, Hk, d] goes in as its transpose(1, 2)).  pages: int32 [B, max_pages], the pages of each sequence's slots, an entry that
+    is no page where a sequence has none.  lens: int32 [B], used slots.  The object keeps the tensors, which the caller goes on writing;
+    other tensors make another object."""
+
+    def __init__(self, k, v, pages, lens):
+        torch = _torch_module()
+        load_library()
+        if k.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("keys and values are bf16 or fp16")
+        for name, x in (("k", k), ("v", v)):
+            if x.dim() != 4 or x.dtype != k.dtype or not x.is_cuda or x.device != k.device or x.shape != k.shape or x.stride(3) != 1:
+                raise ValueError(f"{name} must be a tensor of [n_pages, Hk, page_size, d] on the cache's GPU, with a dense last dimension")
+        if pages.dim() != 2 or pages.dtype != torch.int32 or pages.device != k.device or (pages.shape[1] > 1 and pages.stride(1) != 1):
+            raise ValueError("pages must be int32 [B, max_pages] on the cache's GPU, with a dense last dimension")
+        if lens.shape != pages.shape[:1] or lens.dtype != torch.int32 or lens.device != k.device or not lens.is_contiguous():
+            raise ValueError("lens must be a contiguous int32 tensor of [B] on the cache's GPU")
+        self.k, self.v, self.pages, self.lens = k, v, pages, lens
+        self.dtype, self.device, self._index = k.dtype, k.device, k.device.index
+        self.B, self.max_pages = pages.shape
+        self.n_pages, self.Hk, self.page_size, self.d = k.shape
+        desc = PagedCacheDesc(dtype=k.dtype == torch.float16, B=self.B, Hk=self.Hk, d=self.d, n_pages=self.n_pages, page_size=self.page_size,
+                              max_pages=self.max_pages, k=k.data_ptr(), v=v.data_ptr(), pages=pages.data_ptr(), pages_stride=pages.stride(0), lens=lens.data_ptr())
+        desc.k_stride[:], desc.v_stride[:] = k.stride()[:3], v.stride()[:3]
+        self._desc, self._at, self._bytes = desc, C.byref(desc), {}
+
+
+def paged_append(cache: PagedKVCache, k, v, new_lens=None, q=None, q_out=None, norm: HeadNorm = None, rotary: Rotary = None, positions=None, stream=None):
+    """Writes the keys and values [B, Hk, Nn, d] of each sequence's newest tokens into its last used slots (cache.lens counts them already), keys
+    with norm and rotation on the way, and beside them the tokens' queries q [B, H, Nn, d] into q_out (see dbsp.h: dbsp_paged_append).  new_lens:
+    int32 [B] on the GPU, if not all Nn tokens are there; the others' rows of q_out are left as they were, so pass it then.  positions:
+    int32 [Nn, axes] or [B, Nn, axes], None with one axis: the tokens' slots.  Enqueues on `stream` and returns q_out (None without q)."""
+    torch = _torch
+    lib = _lib
+    if k.dim() != 4:
+        raise ValueError("k must be [B, Hk, Nn, d]")
+    B, Nn, d = cache.B, k.shape[2], cache.d
+    shape = (B, cache.Hk, Nn, d)
+    _check_rows("k", k, cache.k, shape)
+    _check_rows("v", v, cache.k, shape)
+    raw, elsewhere = cache._on(stream)
+    H, q_at, q_s, o_at, o_s = 0, None, (0, 0, 0), None, (0, 0, 0)
+    if q is not None:
+        H = q.shape[1]
+        _check_rows("q", q, k, (B, H, Nn, d))
+        if q_out is None:
+            q_out = cache._empty(q.shape, q.dtype, raw, elsewhere)
+        else:
+            _check_rows("q_out", q_out, k, q.shape)
+        q_at, q_s, o_at, o_s = q.data_ptr(), q.stride(), q_out.data_ptr(), q_out.stride()
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if new_lens is not None and (new_lens.shape != (B,) or new_lens.dtype != torch.int32 or new_lens.device != k.device or not new_lens.is_contiguous()):
+        raise ValueError("new_lens must be a contiguous int32 tensor of [B] on the cache's GPU")
+    pos, pos_b, pos_t = _positions(positions, rotary, B, Nn, k.device)
+    k_s, v_s = k.stride(), v.stride()
+    rc = lib.dbsp_paged_append(cache._at, k.data_ptr(), k_s[0], k_s[1], k_s[2], v.data_ptr(), v_s[0], v_s[1], v_s[2], q_at, q_s[0], q_s[1], q_s[2],
+                               o_at, o_s[0], o_s[1], o_s[2], H, Nn, None if new_lens is None else new_lens.data_ptr(),
+                               None if norm is None else norm._of(k), None if rotary is None else rotary._at, pos, pos_b, pos_t, raw)
+    if rc:
+        _check(rc)
+    return q_out
+
+
+def paged_attn_fwd(cache: PagedKVCache, q, q_lens=None, causal: bool = True, o=None, lse=None, softmax_scale: float = 0.0, stream=None, want_lse: bool = True,
+                   workspace=None):
+    """Attention of each sequence's newest tokens, q [B, H, Nq, d], over its pages (see dbsp.h: dbsp_paged_attn_fwd; the new tokens' keys are written
+    before).  q_lens: int32 [B] on the GPU, if not all Nq tokens are there; the others' rows of o and lse are left as they were, so pass o
+    and lse then.  Enqueues on `stream` (default: torch's current stream) and returns (o, lse)."""
+    torch = _torch
+    shape, q_s = q.shape, q.stride()
+    if len(shape) != 4 or q.dtype != cache.dtype or q.device != cache.device or shape[0] != cache.B or shape[3] != cache.d or q_s[3] != 1:
+        raise ValueError("q must be [B, H, Nq, d] of the cache's sequences, type and head dim on its GPU, with a dense last dimension")
+    B, H, Nq, _ = shape
+    raw, elsewhere = cache._on(stream)
+    if o is None:
+        o = cache._empty(shape, q.dtype, raw, elsewhere)
+    elif o.shape != shape or o.dtype != q.dtype or o.device != q.device or o.stride(3) != 1:
+        raise ValueError("o must be as q")
+    if lse is None:
+        if want_lse:
+            lse = cache._empty((B, H, Nq), torch.float32, raw, elsewhere)
+    elif lse.shape != (B, H, Nq) or lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous f32 tensor of [B, H, Nq] on q's GPU")
+    if q_lens is not None and (q_lens.shape != (B,) or q_lens.dtype != torch.int32 or q_lens.device != q.device or not q_lens.is_contiguous()):
+        raise ValueError("q_lens must be a contiguous int32 tensor of [B] on q's GPU")
+    lib = _lib
+    workspace, at, size = cache._workspace(workspace, (H, Nq), lib.dbsp_paged_attn_workspace, raw, elsewhere)
+    o_s = o.stride()
+    rc = lib.dbsp_paged_attn_fwd(cache._at, q.data_ptr(), q_s[0], q_s[1], q_s[2], o.data_ptr(), o_s[0], o_s[1], o_s[2], None if lse is None else lse.data_ptr(),
+                                 None if q_lens is None else q_lens.data_ptr(), H, Nq, causal, softmax_scale, at, size, raw)
+    if rc:
+        _check(rc)
+    return o, lse
 
 
 def imbalance_ratio(work) -> float:

@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libdbsp.so")
 
 SOURCES = ["planner.cpp", "dual_balance.cpp", "cost_model.cpp", "api.hip", "attn_fwd.hip", "mfma_probe.hip",
            "cache_api.hip", "cache_attn.hip", "cache_attn_long.hip",
-           "cache_weights.hip", "cache_evict.hip"]
+           "cache_weights.hip", "cache_evict.hip", "rows_api.hip", "rows.hip", "paged_api.hip", "paged_attn.hip"]
 
 # Per-file extra flags.  The attention kernels never rely on NaN propagation; without NaN
 # handling the max chains of the softmax compile to v_max3_f32.  (Host-side argument checks in
@@ -26,6 +26,7 @@ SOURCES = ["planner.cpp", "dual_balance.cpp", "cost_model.cpp", "api.hip", "attn
 HOST_LAYOUT = ["-falign-functions=64"]
 EXTRA_FLAGS = {"planner.cpp": HOST_LAYOUT, "dual_balance.cpp": HOST_LAYOUT, "attn_fwd.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-sched-strategy=iterative-ilp", "-mllvm", "-amdgpu-mfma-vgpr-form"],
                "cache_attn.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "paged_attn.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
                "cache_weights.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
                "cache_attn_long.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-sched-strategy=iterative-ilp", "-mllvm", "-amdgpu-mfma-vgpr-form"]}
 

@@ -6,47 +6,12 @@
 #include <cmath>
 #include <string>
 
+#include "api_checks.hpp"
 #include "cache_params.hpp"
 #include "dbsp.h"
 #include "dbsp_diag.h"
-#include "plan.hpp"
 
 namespace {
-
-int fail(const char* who, int code, const char* what) { return dbsp_set_error(code, std::string(who) + ": " + what); }
-
-int done(const char* who, hipError_t e) {
-  if (e == hipSuccess) return DBSP_OK;
-  (void)hipGetLastError();
-  return dbsp_set_error(DBSP_EHIP, std::string(who) + ": " + hipGetErrorString(e));
-}
-
-bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-
-// Strides (the token's last) are ones that the kernels can go by; that of a dimension of one says nothing.
-bool strides_ok(const int64_t* size, const int64_t* s, int n) {
-  for (int i = 0; i < n; ++i)
-    if (size[i] > 1 && (s[i] < 0 || s[i] % 8 != 0 || s[i] > (int64_t)1 << (i == n - 1 ? 24 : 40))) return false;
-  return true;
-}
-int64_t step(int64_t size, int64_t stride) { return size > 1 ? stride : 0; }
-
-// No two elements of a tensor with these sizes and strides (its last dimension dense, d long) share a place: in the order of their
-// strides each dimension steps over all that the ones before it reach.
-bool distinct(const int64_t* size, const int64_t* stride, int64_t d) {
-  int order[3] = {0, 1, 2};
-  std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
-  __int128 reach = d;
-  for (int i : order) {
-    if (size[i] <= 1) continue;
-    if (stride[i] < reach) return false;
-    reach += (__int128)stride[i] * (size[i] - 1);
-  }
-  return true;
-}
-
-constexpr int64_t kMost = INT_MAX / 2;
-constexpr int64_t kMostThreads = UINT32_MAX;       // of a launch along a dimension: HIP has no more
 
 int check_cache(const char* who, const dbsp_cache* c) {
   if (!c) return fail(who, DBSP_EINVAL, "null cache");
@@ -76,8 +41,6 @@ struct Cut {             // how an attention call is laid out
   dbsp_cache_attn_params p;
   int64_t grid, row_lse_at, part_o_at, part_lse_at, scores_at, part_w_at, bytes;
 };
-
-int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // Of a launch of n row tiles on a chip that holds `slots` workgroups at a time.  They have `tiles` key tiles each: whole rounds of row
 // tiles go as they are, and the last one or two are cut into parts that fill their rounds.  Or causality leaves the first

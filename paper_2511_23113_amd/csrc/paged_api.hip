@@ -1,0 +1,179 @@
+// C ABI of the paged key/value cache's operators: argument checks, workspaces, launches.
+#include <cmath>
+
+#include "paged_params.hpp"
+#include "rows_api.hpp"
+
+namespace {
+
+constexpr int64_t kMostSlots = (int64_t)1 << 30;
+
+int check_paged(const char* who, const dbsp_paged_cache* c) {
+  if (!c) return fail(who, DBSP_EINVAL, "null cache");
+  if (c->dtype != DBSP_BF16 && c->dtype != DBSP_FP16) return fail(who, DBSP_EINVAL, "dtype must be DBSP_BF16 or DBSP_FP16");
+  if (c->d != 64 && c->d != 128) return fail(who, DBSP_EINVAL, "head dim must be 64 or 128");
+  if (c->B <= 0 || c->Hk <= 0) return fail(who, DBSP_EINVAL, "B and Hk must be positive");
+  if (c->n_pages <= 0 || c->page_size <= 0 || c->max_pages <= 0) return fail(who, DBSP_EINVAL, "n_pages, page_size and max_pages must be positive");
+  if ((int64_t)c->max_pages * c->page_size >= kMostSlots || (int64_t)c->B * c->Hk > kMost) return fail(who, DBSP_ESHAPE, "the cache is too large");
+  if (!c->k || !c->v || !c->pages || !c->lens) return fail(who, DBSP_EINVAL, "null pointer (k, v, pages or lens)");
+  const int64_t size[3] = {c->n_pages, c->Hk, c->page_size};
+  if (!strides_ok(size, c->k_stride, 3) || !strides_ok(size, c->v_stride, 3) || !aligned(c->k, 16) || !aligned(c->v, 16))
+    return fail(who, DBSP_EINVAL, "k and v must be 16-byte aligned, their strides multiples of 8 and a slot's at most 2^24");
+  if (c->B > 1 && (c->pages_stride < c->max_pages || c->pages_stride > (int64_t)1 << 40)) return fail(who, DBSP_EINVAL, "pages_stride must be at least max_pages");
+  if (!aligned(c->pages, 4) || !aligned(c->lens, 4)) return fail(who, DBSP_EINVAL, "pages and lens must be 4-byte aligned");
+  return DBSP_OK;
+}
+
+struct Cut {             // how an attention call is laid out
+  dbsp_paged_attn_params p;
+  int64_t grid, part_o_at, part_lse_at, bytes;
+};
+
+int lay_out(const char* who, const dbsp_paged_cache* c, int32_t H, int32_t Nq, Cut& cut) {
+  const int rc = check_paged(who, c);
+  if (rc != DBSP_OK) return rc;
+  if (H <= 0 || Nq <= 0) return fail(who, DBSP_EINVAL, "H and Nq must be positive");
+  if (H % c->Hk != 0) return fail(who, DBSP_ESHAPE, "H must be a multiple of the cache's KV heads");
+  dbsp_paged_attn_params& p = cut.p;
+  p = {};
+  p.B = c->B; p.H = H; p.Hk = c->Hk; p.G = H / c->Hk; p.Nq = Nq;
+  p.n_pages = c->n_pages; p.page_size = c->page_size; p.max_pages = c->max_pages; p.cap = c->max_pages * c->page_size;
+  const int64_t rows = (int64_t)Nq * p.G, q_rows = (int64_t)p.B * H * Nq;
+  if (rows > kMost || q_rows > kMost) return fail(who, DBSP_ESHAPE, "too many queries");
+  const int tile_rows = paged_tile_rows(rows, c->d);
+  const int64_t row_tiles = (rows + tile_rows - 1) / tile_rows, all = row_tiles * p.B * p.Hk, tiles = (p.cap + kPagedKeys - 1) / kPagedKeys;
+  p.row_tiles = (int32_t)row_tiles;
+  p.own_rows = (int32_t)std::min<int64_t>(rows, tile_rows);
+  p.split = all < kPagedTarget && tiles > kPagedWhole;
+  p.target = kPagedTarget;
+  // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / target of them
+  const int64_t items = p.split ? std::min(all * tiles, p.target + all) : all;
+  cut.grid = round_up(items, 8) + (p.split ? 8 : 0);
+  const int64_t by = q_rows <= kPagedMergeRows ? 1 : 1024 / c->d, merges = p.split ? (q_rows + by - 1) / by : 0;
+  if (std::max(cut.grid, merges) > kMostThreads / 256) return fail(who, DBSP_ESHAPE, "too many queries or sequences");
+  p.merge_groups = (int32_t)merges;
+  p.merge_by_row = by == 1;
+  const int64_t part_rows = p.split ? items * p.own_rows : 0;
+  cut.part_o_at = round_up(2 * (int64_t)p.B * 4, 256);
+  cut.part_lse_at = cut.part_o_at + part_rows * c->d * 4;
+  cut.bytes = p.split ? round_up(cut.part_lse_at + part_rows * 4, 256) : 0;
+  return DBSP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dbsp_paged_append(const dbsp_paged_cache* cache, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token, const void* v,
+                      int64_t v_batch, int64_t v_head, int64_t v_token, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
+                      void* q_out, int64_t q_out_batch, int64_t q_out_head, int64_t q_out_token, int32_t H, int32_t Nn, const int32_t* new_lens,
+                      const dbsp_head_norm* norm, const dbsp_rotary* rotary, const int32_t* positions, int64_t pos_batch, int64_t pos_token,
+                      void* stream) {
+  const char* who = "dbsp_paged_append";
+  dbsp_rows_params p = {};
+  int kind = 0, rc = check_paged(who, cache);
+  bool halves = false;
+  if (rc == DBSP_OK) rc = dbsp_rows_settle(who, norm, rotary, positions, pos_batch, pos_token, cache->B, Nn, cache->d, p, kind, halves);
+  if (rc != DBSP_OK) return rc;
+  const int32_t B = cache->B, Hk = cache->Hk, d = cache->d;
+  if (q && H <= 0) return fail(who, DBSP_EINVAL, "H must be positive");
+  const int64_t size[3] = {cache->n_pages, Hk, cache->page_size};
+  if (!distinct(size, cache->k_stride, d) || !distinct(size, cache->v_stride, d)) return fail(who, DBSP_EINVAL, "elements of the pool's k or v overlap");
+  if (!aligned(new_lens, 4)) return fail(who, DBSP_EINVAL, "new_lens must be 4-byte aligned");
+  // queries, keys, values
+  const dbsp_rows_tensor in[3] = {{q, q_batch, q_head, q_token}, {k, k_batch, k_head, k_token}, {v, v_batch, v_head, v_token}};
+  static const char* const names[3] = {"q", "k", "v"};
+  for (int i = q ? 0 : 1; i < 3; ++i) {
+    dbsp_rows_part& part = p.part[i];
+    part.heads = i == 0 ? H : Hk;
+    if ((rc = dbsp_rows_check(who, names[i], in[i], false, B, part.heads, Nn, d)) != DBSP_OK) return rc;
+    part.x = static_cast<const uint16_t*>(in[i].x);
+    part.x_sb = step(B, in[i].batch);
+    part.x_sh = step(part.heads, in[i].head);
+    part.x_st = step(Nn, in[i].token);
+    part.plain = i == 2 || (kind == DBSP_NORM_NONE && p.turned == 0);
+    if (kind != DBSP_NORM_NONE && i < 2) {
+      part.gain = i == 0 ? norm->q_gain : norm->k_gain;
+      part.bias = i == 0 ? norm->q_bias : norm->k_bias;
+    }
+    if (i == 0) continue;
+    const int64_t* stride = i == 1 ? cache->k_stride : cache->v_stride;
+    part.pool = static_cast<uint16_t*>(i == 1 ? cache->k : cache->v);
+    part.page_s = step(size[0], stride[0]);
+    part.y_sh = step(size[1], stride[1]);
+    part.y_st = step(size[2], stride[2]);
+  }
+  if (q) {
+    const dbsp_rows_tensor out = {q_out, q_out_batch, q_out_head, q_out_token};
+    if ((rc = dbsp_rows_check(who, "q_out", out, true, B, H, Nn, d)) != DBSP_OK) return rc;
+    p.part[0].y = static_cast<uint16_t*>(q_out);
+    p.part[0].y_sb = step(B, q_out_batch);
+    p.part[0].y_sh = step(H, q_out_head);
+    p.part[0].y_st = step(Nn, q_out_token);
+  }
+  p.lens = cache->lens;
+  p.new_lens = new_lens;
+  p.pages = cache->pages;
+  p.pages_stride = step(B, cache->pages_stride);
+  p.n_pages = cache->n_pages;
+  p.page_size = cache->page_size;
+  p.cap = cache->max_pages * cache->page_size;
+  if ((rc = dbsp_rows_deal(who, p, d, kRowGroups)) != DBSP_OK) return rc;
+  return done(who, dbsp_launch_rows(p, d, cache->dtype == DBSP_FP16, kind, halves, true, static_cast<hipStream_t>(stream)));
+}
+
+int dbsp_paged_attn_workspace(const dbsp_paged_cache* cache, int32_t H, int32_t Nq, int64_t* bytes) {
+  const char* who = "dbsp_paged_attn_workspace";
+  if (!bytes) return fail(who, DBSP_EINVAL, "null pointer");
+  Cut cut;
+  const int rc = lay_out(who, cache, H, Nq, cut);
+  *bytes = rc == DBSP_OK ? cut.bytes : 0;
+  return rc;
+}
+
+int dbsp_paged_attn_fwd(const dbsp_paged_cache* cache, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token, void* o,
+                        int64_t o_batch, int64_t o_head, int64_t o_token, float* lse, const int32_t* q_lens, int32_t H, int32_t Nq,
+                        int32_t causal, float softmax_scale, void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* who = "dbsp_paged_attn_fwd";
+  if (!(softmax_scale == softmax_scale) || softmax_scale > 1e30f || (softmax_scale > 0.f && softmax_scale < 1e-30f))
+    return fail(who, DBSP_EINVAL, "softmax_scale must be 0 or between 1e-30 and 1e30");
+  Cut cut;
+  int rc = lay_out(who, cache, H, Nq, cut);
+  if (rc != DBSP_OK) return rc;
+  if ((rc = dbsp_rows_check(who, "q", {q, q_batch, q_head, q_token}, false, cache->B, H, Nq, cache->d)) != DBSP_OK) return rc;
+  if ((rc = dbsp_rows_check(who, "o", {o, o_batch, o_head, o_token}, true, cache->B, H, Nq, cache->d)) != DBSP_OK) return rc;
+  if (!aligned(lse, 4) || !aligned(q_lens, 4)) return fail(who, DBSP_EINVAL, "lse and q_lens must be 4-byte aligned");
+  if (!workspace && cut.bytes > 0) return fail(who, DBSP_EINVAL, "null pointer (workspace)");
+  if (!aligned(workspace, 256)) return fail(who, DBSP_EINVAL, "the workspace must be 256-byte aligned");
+  if (workspace_bytes < cut.bytes)
+    return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": the workspace holds " + std::to_string(workspace_bytes) + " bytes, the call needs " + std::to_string(cut.bytes));
+  dbsp_paged_attn_params& p = cut.p;
+  p.q = static_cast<const uint16_t*>(q);
+  p.o = static_cast<uint16_t*>(o);
+  p.k = static_cast<const unsigned char*>(cache->k);
+  p.v = static_cast<const unsigned char*>(cache->v);
+  p.lse = lse;
+  p.lens = cache->lens;
+  p.q_lens = q_lens;
+  p.pages = cache->pages;
+  p.pages_stride = step(p.B, cache->pages_stride);
+  p.q_sb = step(p.B, q_batch); p.q_sh = step(H, q_head); p.q_st = step(Nq, q_token);
+  p.o_sb = step(p.B, o_batch); p.o_sh = step(H, o_head); p.o_st = step(Nq, o_token);
+  p.k_sp = step(p.n_pages, cache->k_stride[0]) * 2; p.k_sh = step(p.Hk, cache->k_stride[1]) * 2; p.k_ss = (int32_t)(step(p.page_size, cache->k_stride[2]) * 2);
+  p.v_sp = step(p.n_pages, cache->v_stride[0]) * 2; p.v_sh = step(p.Hk, cache->v_stride[1]) * 2; p.v_ss = (int32_t)(step(p.page_size, cache->v_stride[2]) * 2);
+  // Slots are below 2^31, so with 2^s >= page_size the quotient by it is slot * ceil(2^(31 + s) / page_size) >> (31 + s): the product is
+  // too large by slot / 2^(31 + s) < 2^-s <= 1 / page_size of a quotient at most.
+  int s = 0;
+  while (((int64_t)1 << s) < p.page_size) ++s;
+  p.page_shift = 31 + s;
+  p.page_mul = (uint32_t)((((uint64_t)1 << p.page_shift) + p.page_size - 1) / p.page_size);
+  p.causal = causal != 0;
+  p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->d)) * 1.4426950408889634f;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  p.table = reinterpret_cast<int32_t*>(ws);
+  p.part_o = reinterpret_cast<float*>(ws + cut.part_o_at);
+  p.part_lse = reinterpret_cast<float*>(ws + cut.part_lse_at);
+  return done(who, dbsp_launch_paged_attn(p, cache->d, cache->dtype == DBSP_FP16, (int)cut.grid, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
