@@ -161,12 +161,7 @@ int dbsp_paged_attn_fwd(const dbsp_paged_cache* cache, const void* q, int64_t q_
   p.o_sb = step(p.B, o_batch); p.o_sh = step(H, o_head); p.o_st = step(Nq, o_token);
   p.k_sp = step(p.n_pages, cache->k_stride[0]) * 2; p.k_sh = step(p.Hk, cache->k_stride[1]) * 2; p.k_ss = (int32_t)(step(p.page_size, cache->k_stride[2]) * 2);
   p.v_sp = step(p.n_pages, cache->v_stride[0]) * 2; p.v_sh = step(p.Hk, cache->v_stride[1]) * 2; p.v_ss = (int32_t)(step(p.page_size, cache->v_stride[2]) * 2);
-  // Slots are below 2^31, so with 2^s >= page_size the quotient by it is slot * ceil(2^(31 + s) / page_size) >> (31 + s): the product is
-  // too large by slot / 2^(31 + s) < 2^-s <= 1 / page_size of a quotient at most.
-  int s = 0;
-  while (((int64_t)1 << s) < p.page_size) ++s;
-  p.page_shift = 31 + s;
-  p.page_mul = (uint32_t)((((uint64_t)1 << p.page_shift) + p.page_size - 1) / p.page_size);
+  paged_divisor(p.page_size, p.page_mul, p.page_shift);
   p.causal = causal != 0;
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->d)) * 1.4426950408889634f;
   unsigned char* ws = static_cast<unsigned char*>(workspace);

@@ -36,7 +36,7 @@ __device__ __forceinline__ void copy_lane4(uint64_t from, uint32_t dst) {
 
 __device__ __forceinline__ int paged_len(const dbsp_paged_attn_params& p, int b) { return max(0, min(p.lens[b], p.cap)); }
 __device__ __forceinline__ int paged_q_len(const dbsp_paged_attn_params& p, int b) { return p.q_lens ? max(0, min(p.q_lens[b], p.Nq)) : p.Nq; }
-__device__ __forceinline__ int page_of(const dbsp_paged_attn_params& p, int slot) { return (int)(((uint64_t)(uint32_t)slot * p.page_mul) >> p.page_shift); }
+__device__ __forceinline__ int page_of(const dbsp_paged_attn_params& p, int slot) { return paged_quotient(slot, p.page_mul, p.page_shift); }
 
 struct PagedItem {
   int b, hk, rt;         // sequence, KV head, row tile

@@ -12,6 +12,15 @@ constexpr int kPagedTarget = 1024;     // items that a launch is cut into where 
 constexpr int kPagedWhole = 10;        // tiles that are not cut
 constexpr int kPagedMergeRows = 2048;  // rows up to which a workgroup joins the parts of one
 
+// slot / page_size as slot * mul >> shift, for slots below 2^31: with 2^s >= page_size, mul = 2^(31 + s) / page_size rounded up is too large by
+// less than 1, so the product by less than slot / 2^(31 + s) < 2^-s <= 1 / page_size of the quotient.
+inline void paged_divisor(int page_size, uint32_t& mul, uint32_t& shift) {
+  shift = 31;
+  while (((int64_t)1 << (shift - 31)) < page_size) ++shift;
+  mul = (uint32_t)((((uint64_t)1 << shift) + page_size - 1) / page_size);
+}
+__host__ __device__ inline int paged_quotient(int slot, uint32_t mul, uint32_t shift) { return (int)(((uint64_t)(uint32_t)slot * mul) >> shift); }
+
 struct dbsp_paged_attn_params {
   const uint16_t* q;
   const unsigned char *k, *v;
@@ -23,7 +32,7 @@ struct dbsp_paged_attn_params {
   int32_t k_ss, v_ss;                              // in bytes: slot
   int64_t pages_stride;
   int32_t B, H, Hk, G, Nq, n_pages, page_size, max_pages, cap;
-  uint32_t page_mul, page_shift;       // slot / page_size = slot * page_mul >> page_shift
+  uint32_t page_mul, page_shift;       // see paged_quotient
   int32_t causal, split, target;
   int32_t row_tiles, own_rows;         // of a (sequence, KV head); rows of a partial result
   float scale_log2;                    // softmax scale * log2(e)
