@@ -26,8 +26,8 @@ def test_m0_is_the_copies_own(lines):
 def test_the_compiler_waits_for_no_memory_inside_the_loop(lines):
     # the copies are waited for by count, and the compiler does not know of them: a wait of its own in the loop over tiles would be one for all
     # that are under way.  The loop: between the wait in front of the next tile's copies and the wait for this one's
-    waits = [i for i, line in enumerate(lines) if re.match(r"s_waitcnt vmcnt\((8|4)\) lgkmcnt\(0\)$", line)]
-    ends = [i for i, line in enumerate(lines) if re.match(r"s_waitcnt vmcnt\((9|5)\)$", line)]
+    own = [i for i, line in enumerate(lines) if lines[i - 1] == ";;#ASMSTART" and "vmcnt" in line and "vmcnt(0)" not in line]
+    waits, ends = own[::2], own[1::2]
     assert len(waits) == len(ends) > 0
     for first, last in zip(waits, ends):
         assert first < last
