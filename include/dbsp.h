@@ -325,48 +325,50 @@ typedef struct dbsp_rotary {
   const double* freqs;        /* HOST, [R]: radians per unit of position, finite; read during the call only */
 } dbsp_rotary;
 
+/* Rows of a tensor [B, heads, N, d]: device, 16-byte aligned, strides in elements of batch, head and token (multiples of 8, at least 0, a token's
+ * at most 2^24; that of a dimension of one is not looked at); d has stride 1. */
+typedef struct dbsp_heads {
+  void* x;
+  int64_t stride[3];
+} dbsp_heads;
+typedef struct dbsp_qk_rows {
+  int32_t dtype;              /* DBSP_BF16 or DBSP_FP16: of all rows */
+  int32_t B, N, d;            /* sequences, tokens of each, head dim (64 or 128) */
+  int32_t H, Hk;              /* query heads, key heads (Hk is not looked at where k.x == NULL: no keys) */
+  dbsp_heads q, k;
+  dbsp_heads q_out, k_out;    /* the results, or in the backward pass their gradients */
+  const int32_t* positions;   /* device, int32 [B, N, axes], or NULL with at most one axis: a token's place in its sequence, 0 .. N - 1 */
+  int64_t pos_stride[2];      /* in elements, of batch and token, at least 0 (that of a dimension of one is not looked at); an axis' is 1 */
+} dbsp_qk_rows;
+
 /*
- * dbsp_qk_norm_rope_fwd -- of N tokens of B sequences, H query heads and Hk key heads (k == NULL: no keys, Hk is not looked at).
+ * dbsp_qk_norm_rope_fwd -- q_out and k_out from q and k.
  *
- * dtype: DBSP_BF16 or DBSP_FP16, of q, k and their results alike.  d: 64 or 128.
- * q, k:  device, [B, H, N, d] and [B, Hk, N, d] with strides in elements (batch, head, token; multiples of 8, at least 0, a token's at most
- *        2^24; that of a dimension of one is not looked at; d has stride 1), 16-byte aligned.
- * q_out, k_out: device, written, as q and k with strides of their own, no two elements in one place.  They overlap no input, but may be
- *        q and k themselves with the same strides.
- * norm, rotary: host, may be NULL (none).  positions: device, int32 [B, N, axes] with strides in elements (batch, token; at least 0; an axis' is 1),
- *        or NULL with at most one axis: a token's place in its sequence, 0 .. N - 1.
+ * q_out, k_out: written, no two elements of one in one place.  They overlap no input, but may be q and k themselves with the same strides.
+ * norm, rotary: host, may be NULL (none).  All structs are read during the call only.
  * An infinite value or a NaN spoils its own row only.  With a norm, bf16 values of 2^60 or more in magnitude overflow its sums.
  * stream: a hipStream_t (NULL = default stream).  The call only enqueues one kernel, under capture too.
  * Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large), DBSP_EHIP.
  */
-int dbsp_qk_norm_rope_fwd(int32_t dtype, int32_t B, int32_t N, int32_t d, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
-                          void* q_out, int64_t q_out_batch, int64_t q_out_head, int64_t q_out_token, int32_t H, const void* k, int64_t k_batch,
-                          int64_t k_head, int64_t k_token, void* k_out, int64_t k_out_batch, int64_t k_out_head, int64_t k_out_token, int32_t Hk,
-                          const dbsp_head_norm* norm, const dbsp_rotary* rotary, const int32_t* positions, int64_t pos_batch, int64_t pos_token,
-                          void* stream);
+int dbsp_qk_norm_rope_fwd(const dbsp_qk_rows* rows, const dbsp_head_norm* norm, const dbsp_rotary* rotary, void* stream);
 
 /*
- * dbsp_qk_norm_rope_bwd -- the gradients of a dbsp_qk_norm_rope_fwd call with the same arguments: from q, k and the gradients dq_out, dk_out of
- * its results those of q, k and of gains and biases,
+ * dbsp_qk_norm_rope_bwd -- the gradients of a dbsp_qk_norm_rope_fwd call with the same arguments, but for q_out and k_out, which hold (and are read)
+ * the gradients dy of its results: those of q, k and of gains and biases,
  *   dn = the rotation by -a of dy,  dgain = sum dn (x - mu) r,  dbias = sum dn,  e = dn gain,
  *   dx = r (e - mean(e (x - mu) r) (x - mu) r - [DBSP_NORM_LAYER: mean(e)]),  dx = dn without a norm,
  * the sums over all rows of all tokens, heads and sequences.
  *
- * dq, dk: device, written, as q_out and k_out above (they may be dq_out and dk_out with the same strides).  Every row's gradient is
- *        written: where tokens are padding, zeros in dq_out and dk_out keep them out of all gradients.
- * grads: device, f32 [4, d] contiguous, 16-byte aligned, written: of q's gain, k's gain, q's bias, k's bias (zeros for k == NULL; those of gains
+ * dq, dk: written (dk is not looked at where k.x == NULL), no two elements of one in one place.  They overlap no input, but may be q_out and k_out
+ *        with the same strides.  Every row's gradient is written: where tokens are padding, zeros in q_out and k_out keep them out of all gradients.
+ * grads: device, f32 [4, d] contiguous, 16-byte aligned, written: of q's gain, k's gain, q's bias, k's bias (zeros without keys; those of gains
  *        that are NULL as if they were there); NULL: not formed, and must be NULL without a norm.
- * workspace: device, 256-byte aligned, of the size that dbsp_qk_norm_rope_bwd_workspace gives (NULL where that is 0, as without grads); written by
- *        the call, holds nothing between calls.  Calls under way at the same time need one each.
+ * workspace: device, 256-byte aligned, of the size that dbsp_qk_norm_rope_bwd_workspace gives (Hk 0 without keys); not looked at without grads.
+ *        Written by the call, holds nothing between calls.  Calls under way at the same time need one each.
  * f32 accumulation; the same call gives the same bits.  stream, errors: as above; enqueues one kernel, and a second one for grads.
  */
-int dbsp_qk_norm_rope_bwd(int32_t dtype, int32_t B, int32_t N, int32_t d, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
-                          const void* dq_out, int64_t dq_out_batch, int64_t dq_out_head, int64_t dq_out_token, void* dq, int64_t dq_batch,
-                          int64_t dq_head, int64_t dq_token, int32_t H, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token,
-                          const void* dk_out, int64_t dk_out_batch, int64_t dk_out_head, int64_t dk_out_token, void* dk, int64_t dk_batch,
-                          int64_t dk_head, int64_t dk_token, int32_t Hk, const dbsp_head_norm* norm, const dbsp_rotary* rotary,
-                          const int32_t* positions, int64_t pos_batch, int64_t pos_token, float* grads, void* workspace, int64_t workspace_bytes,
-                          void* stream);
+int dbsp_qk_norm_rope_bwd(const dbsp_qk_rows* rows, const dbsp_heads* dq, const dbsp_heads* dk, const dbsp_head_norm* norm,
+                          const dbsp_rotary* rotary, float* grads, void* workspace, int64_t workspace_bytes, void* stream);
 int dbsp_qk_norm_rope_bwd_workspace(int32_t B, int32_t N, int32_t d, int32_t H, int32_t Hk, int64_t* bytes);
 
 /*
@@ -383,8 +385,8 @@ typedef struct dbsp_paged_cache {
   int32_t n_pages, page_size; /* of the pool; a page's slots may be any number */
   int32_t max_pages;          /* entries of a sequence's table; it has max_pages * page_size slots, below 2^30 */
   void *k, *v;                /* device, [n_pages, Hk, page_size, d], 16-byte aligned */
-  /* strides in elements, of page, head and slot; d has stride 1.  Multiples of 8, at least 0, a slot's at most 2^24 (that of a dimension of one is
-   * not looked at).  dbsp_paged_append writes k and v: no two of their elements may share a place */
+  /* strides in elements, of page, head and slot; d has stride 1.  Multiples of 8, at least 0, a slot's at most 2^24, a page's at most 2^30 (that of
+   * a dimension of one is not looked at).  dbsp_paged_append writes k and v: no two of their elements may share a place */
   int64_t k_stride[3], v_stride[3];
   const int32_t* pages;       /* device, int32 [B, max_pages], the sequences pages_stride elements apart (at least max_pages) */
   int64_t pages_stride;
@@ -396,21 +398,18 @@ typedef struct dbsp_paged_cache {
  * slot lens[b] - n + t: lens counts the new tokens already, and is not written.  Keys get norm and rotation on the way (see
  * dbsp_qk_norm_rope_fwd), values none, and so do the tokens' queries, which go to q_out (q == NULL: none).
  *
- * k, v: device, [B, Hk, Nn, d]; q, q_out: device, [B, H, Nn, d], all with strides in elements as for dbsp_qk_norm_rope_fwd; q_out overlaps
- *       no other, but may be q with the same strides.  None of them overlaps the pool.
- * new_lens: device, int32 [B], taken as 0 below 0 and as Nn above it; NULL: Nn each.  Tokens t >= new_lens[b] are not looked at, and their rows
+ * rows: the new tokens, N of them a sequence at most: k [B, Hk, N, d], q and q_out [B, H, N, d] (q.x == NULL: none, H and q_out are not looked at);
+ *       k_out is not looked at.  dtype, B, d and Hk are the cache's.  positions: NULL with at most one axis: a token's position is its slot.
+ * v:    [B, Hk, N, d].  q_out overlaps no other, but may be q with the same strides.  Nothing here overlaps the pool.
+ * new_lens: device, int32 [B], taken as 0 below 0 and as N above it; NULL: N each.  Tokens t >= new_lens[b] are not looked at, and their rows
  *       of q_out are left as they were; so are the rows of tokens whose slot would lie before slot 0 (new_lens[b] > lens[b]).
- * norm, rotary: as for dbsp_qk_norm_rope_fwd.  positions: device, int32 [B, Nn, axes] with strides as there; NULL with at most one axis: a
- *       token's position is its slot.
+ * norm, rotary: as for dbsp_qk_norm_rope_fwd.
  * Tokens whose page is none (see dbsp_paged_cache) are not written; their queries are.  Where two tokens have one place, by a page that two sequences
  * share, either of them is there afterwards.
- * stream: as above; enqueues one kernel.  Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large), DBSP_EHIP.
+ * stream: as above; enqueues one kernel.  Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large, or not the cache's), DBSP_EHIP.
  */
-int dbsp_paged_append(const dbsp_paged_cache* cache, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token, const void* v,
-                      int64_t v_batch, int64_t v_head, int64_t v_token, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
-                      void* q_out, int64_t q_out_batch, int64_t q_out_head, int64_t q_out_token, int32_t H, int32_t Nn, const int32_t* new_lens,
-                      const dbsp_head_norm* norm, const dbsp_rotary* rotary, const int32_t* positions, int64_t pos_batch, int64_t pos_token,
-                      void* stream);
+int dbsp_paged_append(const dbsp_paged_cache* cache, const dbsp_qk_rows* rows, const dbsp_heads* v, const int32_t* new_lens,
+                      const dbsp_head_norm* norm, const dbsp_rotary* rotary, void* stream);
 
 /*
  * dbsp_paged_attn_fwd -- attention of each sequence's Nq newest tokens over its pages:

@@ -10,6 +10,7 @@ from __future__ import annotations
 import copy
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -68,6 +69,13 @@ class HeadNormDesc(C.Structure):
 
 class RotaryDesc(C.Structure):
     _fields_ = [("axes", C.c_int32), ("halves", C.c_int32), ("pairs", C.c_int32 * 4), ("freqs", C.POINTER(C.c_double))]
+
+
+# dbsp_heads and dbsp_qk_rows of dbsp.h, packed in one call: a structure's fields cost as much as an argument each.
+_HEADS = struct.Struct("@P3q")
+_QK_ROWS = struct.Struct("@6i" + "P3q" * 4 + "P2q")
+_NO_HEADS = (0, 0, 0, 0)
+_NO_POSITIONS = (0, 0, 0)
 
 
 class PagedCacheDesc(C.Structure):
@@ -138,17 +146,16 @@ def load_library(path: str | None = None):
     lib.dbsp_cache_evict.restype = C.c_int
     lib.dbsp_cache_evict_workspace.argtypes = [cache, i32, i64p]
     lib.dbsp_cache_evict_workspace.restype = C.c_int
-    norm, rotary, paged, rows = C.POINTER(HeadNormDesc), C.POINTER(RotaryDesc), C.POINTER(PagedCacheDesc), [vp, i64, i64, i64]
-    at = [vp, i64, i64]
-    lib.dbsp_qk_norm_rope_fwd.argtypes = [i32] * 4 + (rows + rows + [i32]) * 2 + [norm, rotary] + at + [vp]
+    norm, rotary, paged, packed = C.POINTER(HeadNormDesc), C.POINTER(RotaryDesc), C.POINTER(PagedCacheDesc), C.c_char_p
+    lib.dbsp_qk_norm_rope_fwd.argtypes = [packed, norm, rotary, vp]
     lib.dbsp_qk_norm_rope_fwd.restype = C.c_int
-    lib.dbsp_qk_norm_rope_bwd.argtypes = [i32] * 4 + (rows + rows + rows + [i32]) * 2 + [norm, rotary] + at + [vp, vp, i64, vp]
+    lib.dbsp_qk_norm_rope_bwd.argtypes = [packed, packed, packed, norm, rotary, vp, vp, i64, vp]
     lib.dbsp_qk_norm_rope_bwd.restype = C.c_int
     lib.dbsp_qk_norm_rope_bwd_workspace.argtypes = [i32] * 5 + [i64p]
     lib.dbsp_qk_norm_rope_bwd_workspace.restype = C.c_int
-    lib.dbsp_paged_append.argtypes = [paged] + rows * 4 + [i32, i32, vp, norm, rotary] + at + [vp]
+    lib.dbsp_paged_append.argtypes = [paged, packed, packed, vp, norm, rotary, vp]
     lib.dbsp_paged_append.restype = C.c_int
-    lib.dbsp_paged_attn_fwd.argtypes = [paged] + rows * 2 + [vp, vp, i32, i32, i32, f32, vp, i64, vp]
+    lib.dbsp_paged_attn_fwd.argtypes = [paged] + [vp, i64, i64, i64] * 2 + [vp, vp, i32, i32, i32, f32, vp, i64, vp]
     lib.dbsp_paged_attn_fwd.restype = C.c_int
     lib.dbsp_paged_attn_workspace.argtypes = [paged, i32, i32, i64p]
     lib.dbsp_paged_attn_workspace.restype = C.c_int
@@ -558,12 +565,13 @@ class HeadNorm:
                 raise ValueError("gains and biases differ in type, device or size")
             self.dtype, self.device, self.d = x.dtype, x.device, x.shape[0]
             setattr(desc, name, x.data_ptr())
-        desc.gains_f32 = self.dtype == torch.float32
+        self._wide, self._index = self.dtype is torch.float32, None if self.device is None else self.device.index
+        desc.gains_f32 = self._wide
         self._desc, self._at = desc, C.byref(desc)
 
     def _of(self, x):
         """What a call on tensors like x passes on."""
-        if self.d is not None and (self.device != x.device or self.d != x.shape[-1] or (self.dtype != x.dtype and not self._desc.gains_f32)):
+        if self.d is not None and (self._index != x.get_device() or self.d != x.shape[-1] or not (self._wide or self.dtype is x.dtype)):
             raise ValueError("gains and biases must be [d], f32 or of the rows' type, on their GPU")
         return self._at
 
@@ -583,147 +591,132 @@ class Rotary:
         if len(self.freqs) != sum(self.pairs):
             raise ValueError("freqs must hold one value per pair")
         self._freqs = (C.c_double * len(self.freqs))(*self.freqs)
-        desc = RotaryDesc(axes=len(self.pairs), halves=self.halves, freqs=self._freqs)
+        self.axes = len(self.pairs)
+        desc = RotaryDesc(axes=self.axes, halves=self.halves, freqs=self._freqs)
         desc.pairs[:len(self.pairs)] = self.pairs
         self._desc, self._at = desc, C.byref(desc)
 
 
 class _Rows(_OnDevice):
-    """Where a call of q's type and device runs."""
+    """Where calls on rows of a GPU run, and the sizes of workspaces that they have asked for."""
 
-    def __init__(self, device):
-        self.device, self._index = device, device.index
+    def __init__(self, index):
+        self.device, self._index, self._at, self._bytes = _torch.device("cuda", index), index, None, {}
 
 
 _rows_on = {}
 
 
-def _on_rows(device):
-    here = _rows_on.get(device)
-    if here is None:
-        here = _rows_on[device] = _Rows(device)
-    return here
-
-
-def _check_rows(name, x, like, shape):
-    if x.shape != shape or x.dtype != like.dtype or x.device != like.device or x.stride(3) != 1:
-        raise ValueError(f"{name} must be {list(shape)} of the same type on the same GPU, with a dense last dimension")
-
-
-def _positions(positions, rotary, B, N, device):
-    """Address and strides (batch, token) of positions [N, axes] or [B, N, axes]."""
-    if positions is None or rotary is None:
-        return None, 0, 0
-    torch = _torch
-    axes, shape = len(rotary.pairs), positions.shape
-    if positions.dtype != torch.int32 or positions.device != device or len(shape) not in (2, 3) or shape[-2:] != (N, axes) or positions.stride(-1) != 1 and axes > 1:
-        raise ValueError("positions must be int32 [N, axes] or [B, N, axes] on the same GPU, with a dense last dimension")
-    if len(shape) == 3 and shape[0] != B:
-        raise ValueError("positions and tokens differ in the number of sequences")
-    return positions.data_ptr(), positions.stride(0) if len(shape) == 3 else 0, positions.stride(-2)
-
-
-def _first_rows(q):
+def _on_rows(q):
+    """What q's calls run on; q is a tensor that they can begin with."""
     torch = _torch_module()
     if q.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float16) or not q.is_cuda or q.stride(3) != 1:
         raise ValueError("q must be [B, H, N, d] in bf16 or fp16 on a GPU, with a dense last dimension")
-    return torch
+    index = q.get_device()
+    here = _rows_on.get(index)
+    if here is None:
+        load_library()
+        here = _rows_on[index] = _Rows(index)
+    return here
 
 
-def _k_shape(q, k):
-    B, _, N, d = q.shape
-    if k.dim() != 4:
-        raise ValueError("k must be [B, Hk, N, d]")
-    return (B, k.shape[1], N, d)
+def _heads(name, x, shape, dtype, index):
+    """Address and strides (batch, head, token) of rows."""
+    s = x.stride()
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != index or s[3] != 1:
+        raise ValueError(f"{name} must be {list(shape)} of the same type on the same GPU, with a dense last dimension")
+    return x.data_ptr(), s[0], s[1], s[2]
+
+
+def _positions(positions, rotary, B, N, index):
+    """Address and strides (batch, token) of positions [N, axes] or [B, N, axes]."""
+    if positions is None or rotary is None:
+        return _NO_POSITIONS
+    shape, s = positions.shape, positions.stride()
+    tokens = shape == (N, rotary.axes)
+    if not (tokens or shape == (B, N, rotary.axes)) or positions.dtype is not _torch.int32 or positions.get_device() != index or (s[-1] != 1 and rotary.axes > 1):
+        raise ValueError("positions must be int32 [N, axes] or [B, N, axes] on the same GPU, with a dense last dimension")
+    return positions.data_ptr(), 0 if tokens else s[0], s[-2]
 
 
 def qk_norm_rope_fwd(q, k=None, norm: HeadNorm = None, rotary: Rotary = None, positions=None, q_out=None, k_out=None, stream=None):
     """Queries [B, H, N, d] and keys [B, Hk, N, d] of a projection (any strides: views into its output) with each head's norm and the rotation
     by positions (int32 [N, axes] or [B, N, axes]; None with one axis: 0 .. N - 1), as contiguous tensors or in q_out and k_out
     (see dbsp.h: dbsp_qk_norm_rope_fwd).  Enqueues on `stream` (default: torch's current stream) and returns (q_out, k_out)."""
-    _first_rows(q)
-    lib = load_library()
-    B, H, N, d = q.shape
-    here = _on_rows(q.device)
+    here = _on_rows(q)
     raw, elsewhere = here._on(stream)
+    shape, dtype, index, q_s = q.shape, q.dtype, here._index, q.stride()
+    B, H, N, d = shape
     if q_out is None:
-        q_out = here._empty(q.shape, q.dtype, raw, elsewhere)
-    else:
-        _check_rows("q_out", q_out, q, q.shape)
-    Hk, k_at, k_s, k_out_at, k_out_s = 0, None, (0, 0, 0), None, (0, 0, 0)
+        q_out = here._empty(shape, dtype, raw, elsewhere)
+    Hk, k_at, k_out_at = 0, _NO_HEADS, _NO_HEADS
     if k is not None:
-        shape = _k_shape(q, k)
-        _check_rows("k", k, q, shape)
-        Hk = shape[1]
+        if k.dim() == 4:
+            Hk = k.shape[1]
+        shape_k = (B, Hk, N, d)
+        k_at = _heads("k", k, shape_k, dtype, index)
         if k_out is None:
-            k_out = here._empty(shape, q.dtype, raw, elsewhere)
-        else:
-            _check_rows("k_out", k_out, q, shape)
-        k_at, k_s, k_out_at, k_out_s = k.data_ptr(), k.stride(), k_out.data_ptr(), k_out.stride()
+            k_out = here._empty(shape_k, dtype, raw, elsewhere)
+        k_out_at = _heads("k_out", k_out, shape_k, dtype, index)
     elif k_out is not None:
         raise ValueError("k_out without k")
-    pos, pos_b, pos_t = _positions(positions, rotary, B, N, q.device)
-    q_s, o_s = q.stride(), q_out.stride()
-    rc = lib.dbsp_qk_norm_rope_fwd(q.dtype == _torch.float16, B, N, d, q.data_ptr(), q_s[0], q_s[1], q_s[2], q_out.data_ptr(), o_s[0], o_s[1], o_s[2], H,
-                                   k_at, k_s[0], k_s[1], k_s[2], k_out_at, k_out_s[0], k_out_s[1], k_out_s[2], Hk,
-                                   None if norm is None else norm._of(q), None if rotary is None else rotary._at, pos, pos_b, pos_t, raw)
+    rows = _QK_ROWS.pack(dtype is _torch.float16, B, N, d, H, Hk, q.data_ptr(), q_s[0], q_s[1], q_s[2], *k_at, *_heads("q_out", q_out, shape, dtype, index),
+                         *k_out_at, *_positions(positions, rotary, B, N, index))
+    rc = _lib.dbsp_qk_norm_rope_fwd(rows, None if norm is None else norm._of(q), None if rotary is None else rotary._at, raw)
     if rc:
         _check(rc)
     return q_out, k_out
+
+
+_GAINS = ("q_gain", "k_gain", "q_bias", "k_bias")
 
 
 def qk_norm_rope_bwd(q, k, dq_out, dk_out, norm: HeadNorm = None, rotary: Rotary = None, positions=None, dq=None, dk=None, stream=None, workspace=None):
     """Gradients of a qk_norm_rope_fwd call: from its q, k (or None), norm, rotary and positions and the gradients of its results, those of q and k
     (contiguous tensors, or dq and dk, which may be views into the gradient of a projection's output), and of the gains and biases that the
     norm has, f32 [d] by name (see dbsp.h: dbsp_qk_norm_rope_bwd).  Enqueues on `stream` and returns (dq, dk, gains)."""
-    torch = _first_rows(q)
-    lib = load_library()
-    B, H, N, d = q.shape
-    here = _on_rows(q.device)
+    here = _on_rows(q)
     raw, elsewhere = here._on(stream)
-    _check_rows("dq_out", dq_out, q, q.shape)
+    shape, dtype, index, q_s = q.shape, q.dtype, here._index, q.stride()
+    B, H, N, d = shape
     if dq is None:
-        dq = here._empty(q.shape, q.dtype, raw, elsewhere)
-    else:
-        _check_rows("dq", dq, q, q.shape)
-    Hk, none = 0, (None, (0, 0, 0))
-    k_, dk_out_, dk_ = none, none, none
+        dq = here._empty(shape, dtype, raw, elsewhere)
+    Hk, k_at, k_out_at, dk_at = 0, _NO_HEADS, _NO_HEADS, None
     if k is not None:
-        shape = _k_shape(q, k)
-        _check_rows("k", k, q, shape)
+        if k.dim() == 4:
+            Hk = k.shape[1]
+        shape_k = (B, Hk, N, d)
+        k_at = _heads("k", k, shape_k, dtype, index)
         if dk_out is None:
             raise ValueError("k without dk_out")
-        _check_rows("dk_out", dk_out, q, shape)
-        Hk = shape[1]
+        k_out_at = _heads("dk_out", dk_out, shape_k, dtype, index)
         if dk is None:
-            dk = here._empty(shape, q.dtype, raw, elsewhere)
-        else:
-            _check_rows("dk", dk, q, shape)
-        k_, dk_out_, dk_ = ((x.data_ptr(), x.stride()) for x in (k, dk_out, dk))
+            dk = here._empty(shape_k, dtype, raw, elsewhere)
+        dk_at = _HEADS.pack(*_heads("dk", dk, shape_k, dtype, index))
     elif dk_out is not None or dk is not None:
         raise ValueError("dk_out or dk without k")
-    norm_at = None if norm is None else norm._of(q)
-    grads = at = None
-    size = 0
-    if norm is not None and norm.given:
-        grads = here._empty((4, d), torch.float32, raw, elsewhere)
-        if workspace is None:
-            need = C.c_int64()
-            _check(lib.dbsp_qk_norm_rope_bwd_workspace(B, N, d, H, Hk, C.byref(need)))
-            workspace = here._empty(need.value, torch.uint8, raw, elsewhere)
-        elif workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
-            raise ValueError("the workspace must be a contiguous uint8 tensor on q's GPU")
-        at, size = workspace.data_ptr(), workspace.numel()
-    pos, pos_b, pos_t = _positions(positions, rotary, B, N, q.device)
-    q_s, y_s, x_s = q.stride(), dq_out.stride(), dq.stride()
-    rc = lib.dbsp_qk_norm_rope_bwd(q.dtype == torch.float16, B, N, d, q.data_ptr(), q_s[0], q_s[1], q_s[2], dq_out.data_ptr(), y_s[0], y_s[1], y_s[2],
-                                   dq.data_ptr(), x_s[0], x_s[1], x_s[2], H, k_[0], k_[1][0], k_[1][1], k_[1][2], dk_out_[0], dk_out_[1][0], dk_out_[1][1],
-                                   dk_out_[1][2], dk_[0], dk_[1][0], dk_[1][1], dk_[1][2], Hk, norm_at, None if rotary is None else rotary._at,
-                                   pos, pos_b, pos_t, None if grads is None else grads.data_ptr(), at, size, raw)
+    rows = _QK_ROWS.pack(dtype is _torch.float16, B, N, d, H, Hk, q.data_ptr(), q_s[0], q_s[1], q_s[2], *k_at, *_heads("dq_out", dq_out, shape, dtype, index),
+                         *k_out_at, *_positions(positions, rotary, B, N, index))
+    dq_at = _HEADS.pack(*_heads("dq", dq, shape, dtype, index))
+    norm_at, grads, grads_at, at, size, gains = None, None, None, None, 0, {}
+    if norm is not None:
+        norm_at = norm._of(q)
+        if norm.given:
+            grads = here._empty((4, d), _torch.float32, raw, elsewhere)
+            grads_at = grads.data_ptr()
+            if len(here._bytes) > 1000:              # (a program whose sizes never come back)
+                here._bytes.clear()
+            workspace, at, size = here._workspace(workspace, (B, N, d, H, Hk), _grads_workspace, raw, elsewhere)
+    rc = _lib.dbsp_qk_norm_rope_bwd(rows, dq_at, dk_at, norm_at, None if rotary is None else rotary._at, grads_at, at, size, raw)
     if rc:
         _check(rc)
-    names = ("q_gain", "k_gain", "q_bias", "k_bias")
-    return dq, dk, {} if grads is None else {name: grads[names.index(name)] for name in norm.given if k is not None or name[0] == "q"}
+    if grads is not None:
+        gains = {name: x for name, x in zip(_GAINS, grads.unbind()) if name in norm.given and (k is not None or name[0] == "q")}
+    return dq, dk, gains
+
+
+def _grads_workspace(_, *sizes):
+    return _lib.dbsp_qk_norm_rope_bwd_workspace(*sizes)
 
 
 class PagedKVCache(_OnDevice):
@@ -761,33 +754,31 @@ def paged_append(cache: PagedKVCache, k, v, new_lens=None, q=None, q_out=None, n
     with norm and rotation on the way, and beside them the tokens' queries q [B, H, Nn, d] into q_out (see dbsp.h: dbsp_paged_append).  new_lens:
     int32 [B] on the GPU, if not all Nn tokens are there; the others' rows of q_out are left as they were, so pass it then.  positions:
     int32 [Nn, axes] or [B, Nn, axes], None with one axis: the tokens' slots.  Enqueues on `stream` and returns q_out (None without q)."""
-    torch = _torch
-    lib = _lib
+    B, Hk, d, dtype, index = cache.B, cache.Hk, cache.d, cache.dtype, cache._index
     if k.dim() != 4:
         raise ValueError("k must be [B, Hk, Nn, d]")
-    B, Nn, d = cache.B, k.shape[2], cache.d
-    shape = (B, cache.Hk, Nn, d)
-    _check_rows("k", k, cache.k, shape)
-    _check_rows("v", v, cache.k, shape)
+    Nn = k.shape[2]
+    shape = (B, Hk, Nn, d)
     raw, elsewhere = cache._on(stream)
-    H, q_at, q_s, o_at, o_s = 0, None, (0, 0, 0), None, (0, 0, 0)
+    H, q_at, o_at = 0, _NO_HEADS, _NO_HEADS
     if q is not None:
         H = q.shape[1]
-        _check_rows("q", q, k, (B, H, Nn, d))
+        shape_q = (B, H, Nn, d)
+        q_at = _heads("q", q, shape_q, dtype, index)
         if q_out is None:
-            q_out = cache._empty(q.shape, q.dtype, raw, elsewhere)
-        else:
-            _check_rows("q_out", q_out, k, q.shape)
-        q_at, q_s, o_at, o_s = q.data_ptr(), q.stride(), q_out.data_ptr(), q_out.stride()
+            q_out = cache._empty(shape_q, dtype, raw, elsewhere)
+        o_at = _heads("q_out", q_out, shape_q, dtype, index)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    if new_lens is not None and (new_lens.shape != (B,) or new_lens.dtype != torch.int32 or new_lens.device != k.device or not new_lens.is_contiguous()):
-        raise ValueError("new_lens must be a contiguous int32 tensor of [B] on the cache's GPU")
-    pos, pos_b, pos_t = _positions(positions, rotary, B, Nn, k.device)
-    k_s, v_s = k.stride(), v.stride()
-    rc = lib.dbsp_paged_append(cache._at, k.data_ptr(), k_s[0], k_s[1], k_s[2], v.data_ptr(), v_s[0], v_s[1], v_s[2], q_at, q_s[0], q_s[1], q_s[2],
-                               o_at, o_s[0], o_s[1], o_s[2], H, Nn, None if new_lens is None else new_lens.data_ptr(),
-                               None if norm is None else norm._of(k), None if rotary is None else rotary._at, pos, pos_b, pos_t, raw)
+    new_at = None
+    if new_lens is not None:
+        if new_lens.shape != (B,) or new_lens.dtype is not _torch.int32 or new_lens.get_device() != index or not new_lens.is_contiguous():
+            raise ValueError("new_lens must be a contiguous int32 tensor of [B] on the cache's GPU")
+        new_at = new_lens.data_ptr()
+    rows = _QK_ROWS.pack(dtype is _torch.float16, B, Nn, d, H, Hk, *q_at, *_heads("k", k, shape, dtype, index), *o_at, *_NO_HEADS,
+                         *_positions(positions, rotary, B, Nn, index))
+    rc = _lib.dbsp_paged_append(cache._at, rows, _HEADS.pack(*_heads("v", v, shape, dtype, index)), new_at, None if norm is None else norm._of(k),
+                                None if rotary is None else rotary._at, raw)
     if rc:
         _check(rc)
     return q_out
@@ -798,27 +789,24 @@ def paged_attn_fwd(cache: PagedKVCache, q, q_lens=None, causal: bool = True, o=N
     """Attention of each sequence's newest tokens, q [B, H, Nq, d], over its pages (see dbsp.h: dbsp_paged_attn_fwd; the new tokens' keys are written
     before).  q_lens: int32 [B] on the GPU, if not all Nq tokens are there; the others' rows of o and lse are left as they were, so pass o
     and lse then.  Enqueues on `stream` (default: torch's current stream) and returns (o, lse)."""
-    torch = _torch
-    shape, q_s = q.shape, q.stride()
-    if len(shape) != 4 or q.dtype != cache.dtype or q.device != cache.device or shape[0] != cache.B or shape[3] != cache.d or q_s[3] != 1:
+    shape, q_s, dtype, index = q.shape, q.stride(), cache.dtype, cache._index
+    if len(shape) != 4 or q.dtype is not dtype or q.get_device() != index or shape[0] != cache.B or shape[3] != cache.d or q_s[3] != 1:
         raise ValueError("q must be [B, H, Nq, d] of the cache's sequences, type and head dim on its GPU, with a dense last dimension")
     B, H, Nq, _ = shape
     raw, elsewhere = cache._on(stream)
     if o is None:
-        o = cache._empty(shape, q.dtype, raw, elsewhere)
-    elif o.shape != shape or o.dtype != q.dtype or o.device != q.device or o.stride(3) != 1:
-        raise ValueError("o must be as q")
+        o = cache._empty(shape, dtype, raw, elsewhere)
+    o_at, *o_s = _heads("o", o, shape, dtype, index)
     if lse is None:
         if want_lse:
-            lse = cache._empty((B, H, Nq), torch.float32, raw, elsewhere)
-    elif lse.shape != (B, H, Nq) or lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
+            lse = cache._empty((B, H, Nq), _torch.float32, raw, elsewhere)
+    elif lse.shape != (B, H, Nq) or lse.dtype is not _torch.float32 or lse.get_device() != index or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous f32 tensor of [B, H, Nq] on q's GPU")
-    if q_lens is not None and (q_lens.shape != (B,) or q_lens.dtype != torch.int32 or q_lens.device != q.device or not q_lens.is_contiguous()):
+    if q_lens is not None and (q_lens.shape != (B,) or q_lens.dtype is not _torch.int32 or q_lens.get_device() != index or not q_lens.is_contiguous()):
         raise ValueError("q_lens must be a contiguous int32 tensor of [B] on q's GPU")
     lib = _lib
     workspace, at, size = cache._workspace(workspace, (H, Nq), lib.dbsp_paged_attn_workspace, raw, elsewhere)
-    o_s = o.stride()
-    rc = lib.dbsp_paged_attn_fwd(cache._at, q.data_ptr(), q_s[0], q_s[1], q_s[2], o.data_ptr(), o_s[0], o_s[1], o_s[2], None if lse is None else lse.data_ptr(),
+    rc = lib.dbsp_paged_attn_fwd(cache._at, q.data_ptr(), q_s[0], q_s[1], q_s[2], o_at, *o_s, None if lse is None else lse.data_ptr(),
                                  None if q_lens is None else q_lens.data_ptr(), H, Nq, causal, softmax_scale, at, size, raw)
     if rc:
         _check(rc)

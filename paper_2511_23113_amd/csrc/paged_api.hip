@@ -6,8 +6,6 @@
 
 namespace {
 
-constexpr int64_t kMostSlots = (int64_t)1 << 30;
-
 int check_paged(const char* who, const dbsp_paged_cache* c) {
   if (!c) return fail(who, DBSP_EINVAL, "null cache");
   if (c->dtype != DBSP_BF16 && c->dtype != DBSP_FP16) return fail(who, DBSP_EINVAL, "dtype must be DBSP_BF16 or DBSP_FP16");
@@ -19,6 +17,7 @@ int check_paged(const char* who, const dbsp_paged_cache* c) {
   const int64_t size[3] = {c->n_pages, c->Hk, c->page_size};
   if (!strides_ok(size, c->k_stride, 3) || !strides_ok(size, c->v_stride, 3) || !aligned(c->k, 16) || !aligned(c->v, 16))
     return fail(who, DBSP_EINVAL, "k and v must be 16-byte aligned, their strides multiples of 8 and a slot's at most 2^24");
+  if (c->n_pages > 1 && (c->k_stride[0] > (int64_t)1 << 30 || c->v_stride[0] > (int64_t)1 << 30)) return fail(who, DBSP_EINVAL, "the pages of k and v must be at most 2^30 elements apart");
   if (c->B > 1 && (c->pages_stride < c->max_pages || c->pages_stride > (int64_t)1 << 40)) return fail(who, DBSP_EINVAL, "pages_stride must be at least max_pages");
   if (!aligned(c->pages, 4) || !aligned(c->lens, 4)) return fail(who, DBSP_EINVAL, "pages and lens must be 4-byte aligned");
   return DBSP_OK;
@@ -44,19 +43,22 @@ int lay_out(const char* who, const dbsp_paged_cache* c, int32_t H, int32_t Nq, C
   const int64_t row_tiles = (rows + tile_rows - 1) / tile_rows, all = row_tiles * p.B * p.Hk, tiles = (p.cap + kPagedKeys - 1) / kPagedKeys;
   p.row_tiles = (int32_t)row_tiles;
   p.own_rows = (int32_t)std::min<int64_t>(rows, tile_rows);
-  p.split = all < kPagedTarget && tiles > kPagedWhole;
-  p.target = kPagedTarget;
-  // items are at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / target of them
-  const int64_t items = p.split ? std::min(all * tiles, p.target + all) : all;
-  cut.grid = round_up(items, 8) + (p.split ? 8 : 0);
-  const int64_t by = q_rows <= kPagedMergeRows ? 1 : 1024 / c->d, merges = p.split ? (q_rows + by - 1) / by : 0;
+  if (all * tiles > kMost) return fail(who, DBSP_ESHAPE, "the cache is too large for so many sequences, heads and queries");
+  p.whole = tiles <= kPagedWhole;
+  p.runs = paged_runs(rows, c->d);
+  // runs, or parts: at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kPagedParts of them
+  cut.grid = round_up(p.whole ? all : std::max<int64_t>(std::min<int64_t>(p.runs, all * tiles), std::min(all * tiles, (int64_t)kPagedParts + all)), 8);
+  // parts of a row on average, if all sequences are as long; a merge workgroup has 1024 / d of them in hand at a time, eight of a row each
+  int ways = 1;
+  while (ways < 8 && 8 * ways * all < p.runs) ways *= 2;
+  const int64_t by = 1024 / c->d / ways, merges = p.whole ? 0 : (q_rows + by - 1) / by;
   if (std::max(cut.grid, merges) > kMostThreads / 256) return fail(who, DBSP_ESHAPE, "too many queries or sequences");
   p.merge_groups = (int32_t)merges;
-  p.merge_by_row = by == 1;
-  const int64_t part_rows = p.split ? items * p.own_rows : 0;
-  cut.part_o_at = round_up(2 * (int64_t)p.B * 4, 256);
+  p.merge_ways = ways;
+  const int64_t part_rows = p.whole ? 0 : (cut.grid + all) * p.own_rows;
+  cut.part_o_at = round_up((2 + 2 * (int64_t)p.B) * 4, 256);
   cut.part_lse_at = cut.part_o_at + part_rows * c->d * 4;
-  cut.bytes = p.split ? round_up(cut.part_lse_at + part_rows * 4, 256) : 0;
+  cut.bytes = p.whole ? 0 : round_up(cut.part_lse_at + part_rows * 4, 256);
   return DBSP_OK;
 }
 
@@ -64,52 +66,43 @@ int lay_out(const char* who, const dbsp_paged_cache* c, int32_t H, int32_t Nq, C
 
 extern "C" {
 
-int dbsp_paged_append(const dbsp_paged_cache* cache, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token, const void* v,
-                      int64_t v_batch, int64_t v_head, int64_t v_token, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
-                      void* q_out, int64_t q_out_batch, int64_t q_out_head, int64_t q_out_token, int32_t H, int32_t Nn, const int32_t* new_lens,
-                      const dbsp_head_norm* norm, const dbsp_rotary* rotary, const int32_t* positions, int64_t pos_batch, int64_t pos_token,
-                      void* stream) {
+int dbsp_paged_append(const dbsp_paged_cache* cache, const dbsp_qk_rows* rows, const dbsp_heads* v, const int32_t* new_lens,
+                      const dbsp_head_norm* norm, const dbsp_rotary* rotary, void* stream) {
   const char* who = "dbsp_paged_append";
   dbsp_rows_params p = {};
   int kind = 0, rc = check_paged(who, cache);
   bool halves = false;
-  if (rc == DBSP_OK) rc = dbsp_rows_settle(who, norm, rotary, positions, pos_batch, pos_token, cache->B, Nn, cache->d, p, kind, halves);
+  if (rc == DBSP_OK) rc = dbsp_rows_settle(who, rows, norm, rotary, p, kind, halves);
   if (rc != DBSP_OK) return rc;
-  const int32_t B = cache->B, Hk = cache->Hk, d = cache->d;
-  if (q && H <= 0) return fail(who, DBSP_EINVAL, "H must be positive");
+  const int32_t B = cache->B, Hk = cache->Hk, d = cache->d, N = rows->N;
+  if (rows->dtype != cache->dtype || rows->B != B || rows->d != d || rows->Hk != Hk) return fail(who, DBSP_ESHAPE, "type, sequences, head dim and KV heads must be the cache's");
+  if (rows->q.x && rows->H <= 0) return fail(who, DBSP_EINVAL, "H must be positive");
   const int64_t size[3] = {cache->n_pages, Hk, cache->page_size};
   if (!distinct(size, cache->k_stride, d) || !distinct(size, cache->v_stride, d)) return fail(who, DBSP_EINVAL, "elements of the pool's k or v overlap");
+  if (!v) return fail(who, DBSP_EINVAL, "null pointer (v)");
   if (!aligned(new_lens, 4)) return fail(who, DBSP_EINVAL, "new_lens must be 4-byte aligned");
   // queries, keys, values
-  const dbsp_rows_tensor in[3] = {{q, q_batch, q_head, q_token}, {k, k_batch, k_head, k_token}, {v, v_batch, v_head, v_token}};
-  static const char* const names[3] = {"q", "k", "v"};
-  for (int i = q ? 0 : 1; i < 3; ++i) {
+  for (int i = rows->q.x ? 0 : 1; i < 3; ++i) {
     dbsp_rows_part& part = p.part[i];
-    part.heads = i == 0 ? H : Hk;
-    if ((rc = dbsp_rows_check(who, names[i], in[i], false, B, part.heads, Nn, d)) != DBSP_OK) return rc;
-    part.x = static_cast<const uint16_t*>(in[i].x);
-    part.x_sb = step(B, in[i].batch);
-    part.x_sh = step(part.heads, in[i].head);
-    part.x_st = step(Nn, in[i].token);
+    const dbsp_heads& in = i == 0 ? rows->q : i == 1 ? rows->k : *v;
+    const int32_t heads = i == 0 ? rows->H : Hk;
+    if ((rc = dbsp_rows_check(who, i == 0 ? "q" : i == 1 ? "k" : "v", in, false, B, heads, N, d)) != DBSP_OK) return rc;
+    set_in(part, in, B, heads, N);
     part.plain = i == 2 || (kind == DBSP_NORM_NONE && p.turned == 0);
     if (kind != DBSP_NORM_NONE && i < 2) {
       part.gain = i == 0 ? norm->q_gain : norm->k_gain;
       part.bias = i == 0 ? norm->q_bias : norm->k_bias;
     }
-    if (i == 0) continue;
+    if (i == 0) {
+      if ((rc = dbsp_rows_check(who, "q_out", rows->q_out, true, B, heads, N, d)) != DBSP_OK) return rc;
+      set_out(part, rows->q_out, B, heads, N);
+      continue;
+    }
     const int64_t* stride = i == 1 ? cache->k_stride : cache->v_stride;
     part.pool = static_cast<uint16_t*>(i == 1 ? cache->k : cache->v);
     part.page_s = step(size[0], stride[0]);
     part.y_sh = step(size[1], stride[1]);
     part.y_st = step(size[2], stride[2]);
-  }
-  if (q) {
-    const dbsp_rows_tensor out = {q_out, q_out_batch, q_out_head, q_out_token};
-    if ((rc = dbsp_rows_check(who, "q_out", out, true, B, H, Nn, d)) != DBSP_OK) return rc;
-    p.part[0].y = static_cast<uint16_t*>(q_out);
-    p.part[0].y_sb = step(B, q_out_batch);
-    p.part[0].y_sh = step(H, q_out_head);
-    p.part[0].y_st = step(Nn, q_out_token);
   }
   p.lens = cache->lens;
   p.new_lens = new_lens;
@@ -140,8 +133,8 @@ int dbsp_paged_attn_fwd(const dbsp_paged_cache* cache, const void* q, int64_t q_
   Cut cut;
   int rc = lay_out(who, cache, H, Nq, cut);
   if (rc != DBSP_OK) return rc;
-  if ((rc = dbsp_rows_check(who, "q", {q, q_batch, q_head, q_token}, false, cache->B, H, Nq, cache->d)) != DBSP_OK) return rc;
-  if ((rc = dbsp_rows_check(who, "o", {o, o_batch, o_head, o_token}, true, cache->B, H, Nq, cache->d)) != DBSP_OK) return rc;
+  if ((rc = dbsp_rows_check(who, "q", {const_cast<void*>(q), {q_batch, q_head, q_token}}, false, cache->B, H, Nq, cache->d)) != DBSP_OK) return rc;
+  if ((rc = dbsp_rows_check(who, "o", {o, {o_batch, o_head, o_token}}, true, cache->B, H, Nq, cache->d)) != DBSP_OK) return rc;
   if (!aligned(lse, 4) || !aligned(q_lens, 4)) return fail(who, DBSP_EINVAL, "lse and q_lens must be 4-byte aligned");
   if (!workspace && cut.bytes > 0) return fail(who, DBSP_EINVAL, "null pointer (workspace)");
   if (!aligned(workspace, 256)) return fail(who, DBSP_EINVAL, "the workspace must be 256-byte aligned");
@@ -159,8 +152,10 @@ int dbsp_paged_attn_fwd(const dbsp_paged_cache* cache, const void* q, int64_t q_
   p.pages_stride = step(p.B, cache->pages_stride);
   p.q_sb = step(p.B, q_batch); p.q_sh = step(H, q_head); p.q_st = step(Nq, q_token);
   p.o_sb = step(p.B, o_batch); p.o_sh = step(H, o_head); p.o_st = step(Nq, o_token);
-  p.k_sp = step(p.n_pages, cache->k_stride[0]) * 2; p.k_sh = step(p.Hk, cache->k_stride[1]) * 2; p.k_ss = (int32_t)(step(p.page_size, cache->k_stride[2]) * 2);
-  p.v_sp = step(p.n_pages, cache->v_stride[0]) * 2; p.v_sh = step(p.Hk, cache->v_stride[1]) * 2; p.v_ss = (int32_t)(step(p.page_size, cache->v_stride[2]) * 2);
+  auto bytes = [](int64_t size, int64_t stride) { return (uint32_t)(step(size, stride) * 2); };
+  p.k_sp = bytes(p.n_pages, cache->k_stride[0]); p.k_sh = step(p.Hk, cache->k_stride[1]) * 2; p.k_ss = bytes(p.page_size, cache->k_stride[2]);
+  p.v_sp = bytes(p.n_pages, cache->v_stride[0]); p.v_sh = step(p.Hk, cache->v_stride[1]) * 2; p.v_ss = bytes(p.page_size, cache->v_stride[2]);
+  p.page_16 = p.page_size % 16 == 0;
   paged_divisor(p.page_size, p.page_mul, p.page_shift);
   p.causal = causal != 0;
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->d)) * 1.4426950408889634f;

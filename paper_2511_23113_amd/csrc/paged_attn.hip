@@ -4,10 +4,11 @@
 //   s = scale q.k,  LSE = ln sum exp(s),  O = sum exp(s - LSE) v,
 // in one pass with a running max and sum, and O = 0, LSE = -inf without a key.
 //
-// Rows and items.  The G heads of a group read the same keys: a row is a (token, head of the group) pair, and a workgroup has up to 32 of them
-// (d = 64: 64), one token's most often.  An item is a row tile and a range of its tiles of 64 keys; lengths are known on the device only, so every
-// wave works out from them how the launch is cut, about p.target items of equally many tiles.  Parts leave partial results that a second
-// launch joins: LSE = log sum exp LSE_i, O = sum exp(LSE_i - LSE) O_i.
+// Rows and runs.  The G heads of a group read the same keys: a row is a (token, head of the group) pair, and a row tile has up to 32 of them
+// (d = 64: 64), one token's most often.  The tiles of 64 keys of all row tiles, one sequence and KV head behind the other, are one list, of which
+// every workgroup has a run of equally many: as many workgroups as the chip holds at a time begin and end together, whatever the
+// lengths, which are known on the device only.  A row tile that lies in one run is written as it is; the others leave a partial result for
+// every run, which a second launch joins: LSE = log sum exp LSE_i, O = sum exp(LSE_i - LSE) O_i.
 //
 // A workgroup is four waves, which share the rows and have 16 keys of a tile each: a wave copies them into the LDS directly and reads nothing that
 // another has copied, so no barrier couples the waves; their statistics are joined through the LDS at the end.  The pages of a tile's
@@ -34,72 +35,133 @@ __device__ __forceinline__ void copy_lane4(uint64_t from, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(dst) : "memory");
 }
 
-__device__ __forceinline__ int paged_len(const dbsp_paged_attn_params& p, int b) { return max(0, min(p.lens[b], p.cap)); }
-__device__ __forceinline__ int paged_q_len(const dbsp_paged_attn_params& p, int b) { return p.q_lens ? max(0, min(p.q_lens[b], p.Nq)) : p.Nq; }
+// Of a sequence that all lanes ask for, by way of the scalar cache: a vector load would be waited for with the copies that are under way.
+__device__ __forceinline__ int scalar_load(const int32_t* from, int i) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(from + __builtin_amdgcn_readfirstlane(i)));
+}
+__device__ __forceinline__ int paged_len(const dbsp_paged_attn_params& p, int b) { return max(0, min(scalar_load(p.lens, b), p.cap)); }
+__device__ __forceinline__ int paged_q_len(const dbsp_paged_attn_params& p, int b) { return p.q_lens ? max(0, min(scalar_load(p.q_lens, b), p.Nq)) : p.Nq; }
 __device__ __forceinline__ int page_of(const dbsp_paged_attn_params& p, int slot) { return paged_quotient(slot, p.page_mul, p.page_shift); }
 
-struct PagedItem {
-  int b, hk, rt;         // sequence, KV head, row tile
-  int c, n;              // part c of n
-  int64_t slot;          // of its partial result, -1: none
+// Tiles that sequence b's row tiles have in the list: one where there is nothing to read, in which zeros are written.
+__device__ __forceinline__ int listed_tiles(int len, int q_len) { return q_len > 0 ? max(1, tiles_of(len)) : 1; }
+
+// A workgroup's run of the list: where it begins, and its length (0: it has none).
+struct Run {
+  int b, pair;           // sequence, and of its row tiles (KV head by KV head) which
+  int t, left;           // tile of the row tile, tiles of the run
+  int n;                 // number of the run
+  int len, q_len;        // of the sequence
 };
 
-// Which item this workgroup has; false: none.  Every wave works it out for itself, 64 sequences at a time.
-__device__ __forceinline__ bool find_paged_item(const dbsp_paged_attn_params& p, PagedItem& it) {
-  const int unit = p.Hk * p.row_tiles, die = blockIdx.x & 7, i = blockIdx.x >> 3, l = threadIdx.x & 63;
-  if (!p.split) {
-    const int n = p.B * unit, per = (n + 7) / 8, x = die * per + i;
-    if (i >= per || x >= n) return false;
-    it.rt = x % p.row_tiles;
-    it.hk = x / p.row_tiles % p.Hk;
-    it.b = x / p.row_tiles / p.Hk;
-    it.c = 0;
-    it.n = 1;
-    it.slot = -1;
-    return true;
+// Every wave works it out for itself, 64 sequences at a time, a sequence a lane.
+__device__ __forceinline__ Run find_run(const dbsp_paged_attn_params& p) {
+  const int l = threadIdx.x & 63, unit = p.Hk * p.row_tiles;
+  Run run;
+  run.t = run.left = 0;
+  // number of the run that this workgroup has of so many: neighbouring ones on one die (workgroup number mod 8); false: it has none
+  auto take = [&](unsigned count) {
+    const unsigned per = (count + 7) / 8, i = blockIdx.x >> 3;
+    run.n = (int)((blockIdx.x & 7) * per + i);
+    return i < per && (unsigned)run.n < count;
+  };
+  if (p.whole) {         // a row tile a workgroup
+    if (!take((unsigned)p.B * (unsigned)unit)) return run;
+    run.b = (int)((unsigned)run.n / (unsigned)unit);
+    run.pair = run.n - run.b * unit;
+    run.len = paged_len(p, run.b);
+    run.q_len = paged_q_len(p, run.b);
+    run.left = listed_tiles(run.len, run.q_len);
+    return run;
   }
-  auto tiles = [&](int b) { return b < p.B ? tiles_of(paged_len(p, b)) : 0; };
-  const int first_tiles = tiles(l);
-  int64_t total = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) total += __builtin_amdgcn_readlane(scan_wave(b0 == 0 ? first_tiles : tiles(b0 + l)), 63);
-  total *= unit;
-  // (of few tiles up to four an item as long as there are 256 of them, as every part costs the merge)
-  const int chunk = (int)max(max((int64_t)1, min((int64_t)4, total / 256)), min((int64_t)(1 << 30), (total + p.target - 1) / p.target));
-  auto parts = [&](int b, int tiles) { return b < p.B ? max(1, (tiles + chunk - 1) / chunk) : 0; };
-  // parts of all sequences, and where those of each begin
+  // (lengths and new tokens are asked for at once: lanes without a sequence ask for the last one's, so that no branch stands between)
+  const int32_t* const q_lens = p.q_lens ? p.q_lens : p.lens;
+  auto get = [&](int b, int& len, int& q_len) __attribute__((always_inline)) {
+    const int at = min(b, p.B - 1), as_given = p.lens[at], q_as_given = q_lens[at];
+    len = max(0, min(as_given, p.cap));
+    q_len = p.q_lens ? max(0, min(q_as_given, p.Nq)) : p.Nq;
+    return b < p.B ? listed_tiles(len, q_len) : 0;
+  };
+  int len0, q_len0;
+  const int tiles0 = get(l, len0, q_len0), upto0 = scan_wave(tiles0);
+  int all = __builtin_amdgcn_readlane(upto0, 63);
+  for (int b0 = 64; b0 < p.B; b0 += 64) {
+    int len, q_len;
+    all += __builtin_amdgcn_readlane(scan_wave(get(b0 + l, len, q_len)), 63);
+  }
+  const unsigned total = (unsigned)all * (unsigned)unit;
+  const bool parts = total < kPagedLong * max(p.runs, (unsigned)p.B * (unsigned)unit);
+  // (of few tiles up to four a part as long as there are 256 of them, as every part costs the merge)
+  const unsigned chunk = parts ? max(max(1u, min(4u, total / 256)), (total + kPagedParts - 1) / kPagedParts) : (total + p.runs - 1) / p.runs;
+  auto parts_of = [&](int tiles) { return (int)((tiles + chunk - 1) / chunk); };
+  const int mine0 = parts ? parts_of(tiles0) : tiles0, mine_upto0 = parts ? scan_wave(mine0) : upto0;
+  unsigned count = (unsigned)__builtin_amdgcn_readlane(mine_upto0, 63);
+  if (parts) {
+    for (int b0 = 64; b0 < p.B; b0 += 64) {
+      int len, q_len;
+      count += (unsigned)__builtin_amdgcn_readlane(scan_wave(parts_of(get(b0 + l, len, q_len))), 63);
+    }
+    count *= (unsigned)unit;
+  } else {
+    count = (total + chunk - 1) / chunk;
+  }
+  if (!take(count)) return run;
+  // Runs: where in one KV head's tiles this one begins.  Parts: which it is, counted alike.
+  const unsigned from = parts ? (unsigned)run.n : run.n * chunk, where = from / (unsigned)unit;
   const bool writes = blockIdx.x == 0 && threadIdx.x < 64;
-  int all = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const int b = b0 + l, n = parts(b, b0 == 0 ? first_tiles : tiles(b)), upto = scan_wave(n);
-    if (writes && b < p.B) {
-      p.table[2 * b] = all + upto - n;
-      p.table[2 * b + 1] = n;
-    }
-    all += __builtin_amdgcn_readlane(upto, 63);
+  if (writes && l == 0) {
+    p.table[0] = (int)chunk;
+    p.table[1] = parts;
   }
-  // a run of the items for every die
-  const int64_t items = (int64_t)unit * all, from = items * die / 8;
-  if (from + i >= items * (die + 1) / 8) return false;
-  const int64_t y = from + i;
-  const int part = (int)(y / unit);
-  int before = 0;
+  unsigned before = 0;
+  bool found = false;
   for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const int n = parts(b0 + l, b0 == 0 ? first_tiles : tiles(b0 + l)), upto = scan_wave(n), here = __builtin_amdgcn_readlane(upto, 63);
-    if (part < before + here) {
-      const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(part < before + upto));
-      it.b = b0 + at;
-      it.n = __builtin_amdgcn_readlane(n, at);
-      const int first = before + __builtin_amdgcn_readlane(upto, at) - it.n;
-      const int z = (int)(y - (int64_t)first * unit);
-      it.rt = z % p.row_tiles;
-      it.c = z / p.row_tiles % it.n;
-      it.hk = z / p.row_tiles / it.n;
-      it.slot = it.n == 1 ? -1 : (int64_t)first * unit + ((int64_t)it.hk * it.n + it.c) * p.row_tiles + it.rt;
-      return true;
+    int len = len0, q_len = q_len0, tiles = tiles0, mine = mine0, upto = mine_upto0;
+    if (b0 > 0) {
+      tiles = get(b0 + l, len, q_len);
+      mine = parts ? parts_of(tiles) : tiles;
+      upto = scan_wave(mine);
     }
-    before += here;
+    if (writes && b0 + l < p.B) {          // for the merge
+      p.table[2 + 2 * (b0 + l)] = (int)before + upto - mine;
+      p.table[3 + 2 * (b0 + l)] = tiles;
+    }
+    const uint64_t behind = __builtin_amdgcn_ballot_w64(where < before + upto);
+    if (!found && behind) {
+      const int at = __builtin_ctzll(behind), n = __builtin_amdgcn_readlane(mine, at), of = __builtin_amdgcn_readlane(tiles, at);
+      const unsigned in = from - (before + (unsigned)(__builtin_amdgcn_readlane(upto, at) - n)) * unit;
+      found = true;
+      run.b = b0 + at;
+      run.pair = (int)(in / (unsigned)n);
+      run.t = (int)(in - run.pair * n);
+      run.left = (int)min(chunk, total - from);
+      if (parts) {         // part run.t of n, of equally many tiles
+        const int per = (int)((unsigned)(of + n - 1) / (unsigned)n);
+        run.t = min(run.t * per, of);
+        run.left = min(per, of - run.t);
+      }
+      run.len = __builtin_amdgcn_readlane(len, at);
+      run.q_len = __builtin_amdgcn_readlane(q_len, at);
+    }
+    if (found && !writes) break;
+    before += __builtin_amdgcn_readlane(upto, 63);
   }
-  return false;          // (not reached: part < all)
+  return run;
+}
+
+// A tile of the list: sequence, row tile of it, tile of that; and what goes with the sequence.
+struct At {
+  int b, pair, t;
+  int len, listed;       // used slots, tiles of its row tiles in the list
+};
+__device__ __forceinline__ void to_next(const dbsp_paged_attn_params& p, int unit, At& x) {
+  if (++x.t < x.listed) return;
+  x.t = 0;
+  if (++x.pair < unit) return;
+  x.pair = 0;
+  if (++x.b >= p.B) return;                // (past the end: not looked at)
+  x.len = paged_len(p, x.b);
+  x.listed = listed_tiles(x.len, paged_q_len(p, x.b));
 }
 
 template <class T, int D, int NR>
@@ -109,69 +171,32 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
   constexpr int KS = D / 32, DT = D / 16, CH = D / 4, ROWS = 16 * NR;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * L::TILE];      // [buffer][K, V]
   __shared__ int page_ids[4][2][64];
-  PagedItem it;
-  if (!find_paged_item(p, it)) return;
-  const int b = __builtin_amdgcn_readfirstlane(it.b), hk = __builtin_amdgcn_readfirstlane(it.hk), rt = __builtin_amdgcn_readfirstlane(it.rt);
+  __shared__ float mcs[4][16], sums[4][16], rounds[4][16];
+  const Run run = find_run(p);
+  const int left = __builtin_amdgcn_readfirstlane(run.left), run_n = __builtin_amdgcn_readfirstlane(run.n), unit = p.Hk * p.row_tiles;
+  if (left == 0) return;
+  At at;
+  at.b = __builtin_amdgcn_readfirstlane(run.b);
+  at.pair = __builtin_amdgcn_readfirstlane(run.pair);
+  at.t = __builtin_amdgcn_readfirstlane(run.t);
+  at.len = __builtin_amdgcn_readfirstlane(run.len);
+  int q_len = __builtin_amdgcn_readfirstlane(run.q_len);
+  at.listed = listed_tiles(at.len, q_len);
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 15, g = l >> 4;
-  const int len = paged_len(p, b), q_len = paged_q_len(p, b), rows = p.Nq * p.G, row0 = rt * ROWS, base = len - q_len + 1;
-  if (row0 / p.G >= q_len) return;         // no query here: its rows stay as they are
-  const int tiles = tiles_of(len), per = (tiles + it.n - 1) / it.n;
-  const int t0 = __builtin_amdgcn_readfirstlane(min(it.c * per, tiles)), t1 = __builtin_amdgcn_readfirstlane(min((it.c + 1) * per, tiles));
-
+  const int rows = p.Nq * p.G;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(LDS_PTR(unsigned char))lds;
   const uint32_t ids_base = (uint32_t)(uintptr_t)(LDS_PTR(int))&page_ids[w][0][0];
-  const int32_t* const row_pages = p.pages + b * p.pages_stride;
-  // lane l asks for the page of the wave's key l % 16 of tile t (past the end of the table: its last entry, which is not looked at)
-  auto copy_ids = [&](int t) __attribute__((always_inline)) {
-    const int slot = min(t, t1 - 1) * kPagedKeys + 16 * w + n;
-    copy_lane4((uint64_t)(uintptr_t)(row_pages + min(page_of(p, slot), p.max_pages - 1)), ids_base + (t & 1) * 256);
+  // lane l asks for the page of the wave's key l % 16 of a tile (past the end of the table: its last entry, which is not looked at)
+  auto copy_ids = [&](const At& x, int parity) __attribute__((always_inline)) {
+    const int slot = x.t * kPagedKeys + 16 * w + n;
+    copy_lane4((uint64_t)(uintptr_t)(p.pages + x.b * p.pages_stride + min(page_of(p, slot), p.max_pages - 1)), ids_base + parity * 256);
   };
-  if (t0 < t1) {
-    copy_ids(t0);
-    copy_ids(t0 + 1);
-  }
+  At next = at, after;
+  copy_ids(at, 0);
+  if (left > 1) to_next(p, unit, next);
+  copy_ids(next, 1);
+  after = next;
 
-  int limit[NR], all_see = INT_MAX;
-  bool valid[NR];
-  u32x4 q[NR][KS];
-#pragma unroll
-  for (int y = 0; y < NR; ++y) {
-    const int row = row0 + 16 * y + n, in = min(row, rows - 1), tok = in / p.G, gh = in % p.G;
-    valid[y] = row < rows && tok < q_len;
-    limit[y] = p.causal ? max(0, min(len, base + tok)) : len;
-    all_see = min(all_see, valid[y] ? limit[y] : INT_MAX);
-    const uint16_t* src = p.q + b * p.q_sb + (hk * p.G + gh) * p.q_sh + tok * p.q_st;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) q[y][ks] = *reinterpret_cast<const u32x4*>(src + 32 * ks + 8 * g);
-  }
-  all_see = over_row(all_see, [](int x, int y) { return min(x, y); });
-  all_see = __builtin_amdgcn_readfirstlane(all_see);
-  // the queries are waited for here, in front of the copies, which the compiler does not count
-#pragma unroll
-  for (int y = 0; y < NR; ++y)
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[y][ks]));
-
-  const int row_in = l / L::NCH, pch = l % L::NCH;
-  const uint64_t k_head = (uint64_t)(uintptr_t)(p.k + hk * p.k_sh), v_head = (uint64_t)(uintptr_t)(p.v + hk * p.v_sh);
-  const uint64_t zeros = (uint64_t)(uintptr_t)kZeros + (pch << 4);
-  // copies this wave's keys of tile t; which of them are there, a bit each
-  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
-    const uint32_t dst = lds_base + buf * 2 * L::TILE + 16 * w * L::ROWB, ids = ids_base + (t & 1) * 256;
-    const int slot0 = t * kPagedKeys + 16 * w;
-#pragma unroll
-    for (int x = 0; x < L::COPIES; ++x) {
-      const int in = x * L::RPC + row_in, slot = slot0 + in;
-      const int page = *(LDS_PTR(int))(uintptr_t)(ids + 4 * in), at = slot - page_of(p, slot) * p.page_size;
-      const bool there = slot < len && (unsigned)page < (unsigned)p.n_pages;
-      const uint64_t k_at = k_head + (int64_t)page * p.k_sp + (int64_t)at * p.k_ss + ((pch ^ L::k_swz(in)) << 4);
-      const uint64_t v_at = v_head + (int64_t)page * p.v_sp + (int64_t)at * p.v_ss + ((pch ^ L::v_swz(in)) << 4);
-      copy_lane16(there ? k_at : zeros, dst + x * 1024);
-      copy_lane16(there ? v_at : zeros, dst + L::TILE + x * 1024);
-    }
-    const int page = *(LDS_PTR(int))(uintptr_t)(ids + 4 * n);
-    return (uint32_t)__builtin_amdgcn_ballot_w64(slot0 + n < len && (unsigned)page < (unsigned)p.n_pages) & 0xffffu;
-  };
   // operand reads: K rows n with 16-byte chunk 4 ks + g; of V^T, lane 4 j + a of 16 has the address of four values of key j
   const uint32_t mine = lds_base + 16 * w * L::ROWB;
   uint32_t k_rd[KS], v_rd[DT];
@@ -182,40 +207,102 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) v_rd[dt] = mine + L::TILE + key * L::ROWB + (((2 * dt + (a4 >> 1)) ^ L::v_swz(key)) << 4) + (a4 & 1) * 8;
   }
+  const u32x2 ones = {T::pack(1.f, 1.f), T::pack(1.f, 1.f)};
+  const float c = p.scale_log2;
+  const int row_in = l / L::NCH, pch = l % L::NCH;
+  const uint64_t zeros = (uint64_t)(uintptr_t)kZeros + (pch << 4);
+  // where a lane's 16 bytes of a row lie, behind the wave's first slot, where all its slots are in one page
+  uint32_t k_in[L::COPIES], v_in;
+#pragma unroll
+  for (int i = 0; i < L::COPIES; ++i) k_in[i] = row_in * p.k_ss + ((pch ^ L::k_swz(i * L::RPC + row_in)) << 4);
+  v_in = row_in * p.v_ss + ((pch ^ L::v_swz(row_in)) << 4);
+  static_assert(L::RPC % (L::RPL * L::NCH / 4) == 0, "V's chunks lie alike in all of a wave's copies");
+  // copies this wave's keys of a tile; which of them are there, a bit each
+  auto copy_tile = [&](const At& x, int buf) __attribute__((always_inline)) {
+    const uint32_t dst = lds_base + buf * 2 * L::TILE + 16 * w * L::ROWB, ids = ids_base + buf * 256;
+    const int slot0 = x.t * kPagedKeys + 16 * w, hk = (int)((unsigned)x.pair / (unsigned)p.row_tiles);
+    const uint64_t k_head = (uint64_t)(uintptr_t)(p.k + hk * p.k_sh), v_head = (uint64_t)(uintptr_t)(p.v + hk * p.v_sh);
+    const int page_n = *(LDS_PTR(int))(uintptr_t)(ids + 4 * n);
+    const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(slot0 + n < x.len && (unsigned)page_n < (unsigned)p.n_pages) & 0xffffu;
+    if (p.page_16 && there == 0xffffu) {
+      const uint64_t page = (unsigned)__builtin_amdgcn_readfirstlane(page_n), place = (unsigned)__builtin_amdgcn_readfirstlane(slot0 - page_of(p, slot0) * p.page_size);
+      const unsigned char* k_at = reinterpret_cast<const unsigned char*>(k_head + page * p.k_sp + place * p.k_ss);
+      const unsigned char* v_at = reinterpret_cast<const unsigned char*>(v_head + page * p.v_sp + place * p.v_ss);
+#pragma unroll
+      for (int i = 0; i < L::COPIES; ++i) {
+        copy_row16(k_at + (uint64_t)(i * L::RPC) * p.k_ss, k_in[i], dst + i * 1024);
+        copy_row16(v_at + (uint64_t)(i * L::RPC) * p.v_ss, v_in, dst + L::TILE + i * 1024);
+      }
+      return there;
+    }
+#pragma unroll
+    for (int i = 0; i < L::COPIES; ++i) {
+      const int in = i * L::RPC + row_in, slot = slot0 + in;
+      const uint32_t page = *(LDS_PTR(uint32_t))(uintptr_t)(ids + 4 * in), place = slot - page_of(p, slot) * p.page_size;
+      const bool here = slot < x.len && page < (unsigned)p.n_pages;
+      uint64_t k_at = k_head + (uint64_t)page * p.k_sp + (uint64_t)place * p.k_ss + ((pch ^ L::k_swz(in)) << 4);
+      uint64_t v_at = v_head + (uint64_t)page * p.v_sp + (uint64_t)place * p.v_ss + ((pch ^ L::v_swz(in)) << 4);
+      asm("" : "+v"(k_at), "+v"(v_at));      // (formed by all lanes: no branch for the choice)
+      copy_lane16(here ? k_at : zeros, dst + i * 1024);
+      copy_lane16(here ? v_at : zeros, dst + L::TILE + i * 1024);
+    }
+    return there;
+  };
+
+  int limit[NR], all_see, row0, hk;
+  bool valid[NR];
+  u32x4 q[NR][KS];
   // rounded[y]: sums of the rounded probabilities, by one more MFMA against ones, all four alike.  O is divided by them, so that the
   // rounding of a key that has most of its row's attention drops out; LSE is of `sum`.
   f32x4 o[NR][DT], rounded[NR];
   float mc[NR], sum[NR];                   // the max starts at the lowest finite value: scores of -inf then have probability 0
+  // the queries and limits of a row tile, and statistics of nothing yet
+  auto begin = [&](const At& x) __attribute__((always_inline)) {
+    hk = (int)((unsigned)x.pair / (unsigned)p.row_tiles);
+    row0 = (x.pair - hk * p.row_tiles) * ROWS;
+    all_see = INT_MAX;
 #pragma unroll
-  for (int y = 0; y < NR; ++y) {
-    mc[y] = -FLT_MAX;
-    sum[y] = 0.f;
-    rounded[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int y = 0; y < NR; ++y) {
+      const int row = row0 + 16 * y + n, in = min(row, rows - 1), tok = (int)((unsigned)in / (unsigned)p.G), gh = in - tok * p.G;
+      valid[y] = row < rows && tok < q_len;
+      limit[y] = p.causal ? max(0, min(x.len, x.len - q_len + 1 + tok)) : x.len;
+      all_see = min(all_see, valid[y] ? limit[y] : INT_MAX);
+      const uint16_t* src = p.q + x.b * p.q_sb + (hk * p.G + gh) * p.q_sh + tok * p.q_st;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[y][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  const u32x2 ones = {T::pack(1.f, 1.f), T::pack(1.f, 1.f)};
-  const float c = p.scale_log2;
-
-  uint32_t there = 0;
-  if (t0 < t1) {
-    wait_all();                            // the first two tiles' pages
-    there = copy_tile(t0, 0);
-  }
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
+      for (int ks = 0; ks < KS; ++ks) q[y][ks] = *reinterpret_cast<const u32x4*>(src + 32 * ks + 8 * g);
+      mc[y] = -FLT_MAX;
+      sum[y] = 0.f;
+      rounded[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[y][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    all_see = over_row(all_see, [](int x, int y) { return min(x, y); });
+    all_see = __builtin_amdgcn_readfirstlane(all_see);
+    // the queries are waited for here and not between copies, which the compiler does not count
+#pragma unroll
+    for (int y = 0; y < NR; ++y)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[y][ks]));
+  };
+  begin(at);
+  wait_all();                              // the first two tiles' pages
+  uint32_t there = copy_tile(at, 0);
+  int first = at.t;                        // of the row tile's tiles in this run
+  for (int j = 0; j < left; ++j) {
+    const int buf = j & 1;
     uint32_t there_next = 0;
-    if (t + 1 < t1) {
-      // the pages of tile t + 1 have landed (younger are the copies of tile t only), and what was read in its buffer has arrived
+    if (j + 1 < left) {
+      // the pages of the next tile have landed (younger are the copies of this tile only), and what was read in its buffer has arrived
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * L::COPIES) : "memory");
-      copy_ids(t + 2);
-      there_next = copy_tile(t + 1, buf ^ 1);
+      if (j + 2 < left) to_next(p, unit, after);
+      copy_ids(after, buf);
+      there_next = copy_tile(next, buf ^ 1);
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * L::COPIES + 1) : "memory");      // this tile has landed, the next one is under way
     } else {
       wait_all();
     }
     const uint32_t off = buf * 2 * L::TILE;
-    const int key = t * kPagedKeys + 16 * w + 4 * g;
+    const int key = at.t * kPagedKeys + 16 * w + 4 * g;
     u32x4 kf[KS];
     u32x2 vf[DT], pb[NR];
 #pragma unroll
@@ -227,11 +314,11 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) x = T::mfma32(kf[ks], q[y][ks], x);
-      if (there != 0xffffu || (t + 1) * kPagedKeys > all_see) {
-        const int left = limit[y] - key;
+      if (there != 0xffffu || (at.t + 1) * kPagedKeys > all_see) {
+        const int see = limit[y] - key;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (i >= left || !((there >> (4 * g + i)) & 1)) x[i] = -INFINITY;
+          if (i >= see || !((there >> (4 * g + i)) & 1)) x[i] = -INFINITY;
       }
       float pr[4];
 #pragma unroll
@@ -260,83 +347,107 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
 #pragma unroll
     for (int y = 0; y < NR; ++y) rounded[y] = T::mfma16(ones, pb[y], rounded[y]);
     there = there_next;
-  }
+    if (j + 1 < left && next.t != 0) {
+      at = next;
+      next = after;
+      continue;
+    }
 
-  // the waves' results, up to 32 rows at a time: [wave][row][16-byte chunk of the head dim, by row swizzled]
-  constexpr int AT = NR < 2 ? NR : 2;
-  __shared__ float mcs[4][16 * AT], sums[4][16 * AT], rounds[4][16 * AT];
-  f32x4* const os = reinterpret_cast<f32x4*>(lds);
+    // The row tile's last tile, here or at all: the waves' results, 16 rows at a time, by way of the buffer that has been read (the next tile
+    // is under way to the other one): [wave][row][16-byte chunk of the head dim, by row swizzled].
+    const bool part = first != 0 || at.t + 1 != at.listed;
+    const int64_t slot = (int64_t)run_n + (int64_t)at.b * unit + at.pair;      // of a partial result: from each to the next one of the two grows
+    f32x4* const os = reinterpret_cast<f32x4*>(lds + off);
 #pragma unroll
-  for (int y0 = 0; y0 < NR; y0 += AT) {
-    __syncthreads();                       // everybody has read its last tile, or the rows before
-#pragma unroll
-    for (int z = 0; z < AT; ++z) {
-      const int y = y0 + z;
+    for (int y = 0; y < NR; ++y) {
+      __syncthreads();                     // everybody has read the tile, or the rows before
       sum[y] += __shfl_xor(sum[y], 16);
       sum[y] += __shfl_xor(sum[y], 32);
       if (g == 0) {
-        mcs[w][16 * z + n] = mc[y];
-        sums[w][16 * z + n] = sum[y];
-        rounds[w][16 * z + n] = rounded[y][0];
+        mcs[w][n] = mc[y];
+        sums[w][n] = sum[y];
+        rounds[w][n] = rounded[y][0];
       }
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) os[(w * 16 * AT + 16 * z + n) * CH + ((4 * dt + g) ^ n)] = o[y][dt];
+      for (int dt = 0; dt < DT; ++dt) os[(w * 16 + n) * CH + ((4 * dt + g) ^ n)] = o[y][dt];
+      __syncthreads();
+#pragma unroll
+      for (int z = 0; z < 16 * CH / 256; ++z) {
+        const int i = z * 256 + threadIdx.x, in = i / CH, ch = i % CH, row = row0 + 16 * y + in, tok = (int)((unsigned)row / (unsigned)p.G);
+        if (row >= rows || tok >= q_len) continue;
+        float m = mcs[0][in];
+#pragma unroll
+        for (int x = 1; x < 4; ++x) m = fmaxf(m, mcs[x][in]);
+        float all = 0.f, all_rounded = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float f = __builtin_amdgcn_exp2f(mcs[x][in] - m);
+          all += f * sums[x][in];
+          all_rounded += f * rounds[x][in];
+          acc += f * os[(x * 16 + in) * CH + (ch ^ in)];
+        }
+        const bool none = __builtin_bit_cast(uint32_t, all) == 0u;      // (by its bits: NaNs are not regarded in this file)
+        acc *= none ? 0.f : 1.f / all_rounded;
+        const float lse2 = none ? -INFINITY : m + __builtin_amdgcn_logf(all);
+        if (part) {
+          const int64_t pr = slot * p.own_rows + 16 * y + in;
+          *reinterpret_cast<f32x4*>(p.part_o + pr * D + 4 * ch) = acc;
+          if (ch == 0) p.part_lse[pr] = lse2;
+        } else {
+          const int h = hk * p.G + row - tok * p.G;
+          *reinterpret_cast<u32x2*>(p.o + at.b * p.o_sb + h * p.o_sh + tok * p.o_st + 4 * ch) = u32x2{T::pack_o(acc.x, acc.y), T::pack_o(acc.z, acc.w)};
+          if (ch == 0 && p.lse) p.lse[((int64_t)at.b * p.H + h) * p.Nq + tok] = lse2 * 0.69314718055994531f;
+        }
+      }
     }
-    __syncthreads();
-#pragma unroll
-    for (int z = 0; z < 16 * AT * CH / 256; ++z) {
-      const int i = z * 256 + threadIdx.x, in = i / CH, ch = i % CH, row = row0 + 16 * y0 + in, tok = row / p.G;
-      if (row >= rows || tok >= q_len) continue;
-      float m = mcs[0][in];
-#pragma unroll
-      for (int x = 1; x < 4; ++x) m = fmaxf(m, mcs[x][in]);
-      float all = 0.f, all_rounded = 0.f;
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const float f = __builtin_amdgcn_exp2f(mcs[x][in] - m);
-        all += f * sums[x][in];
-        all_rounded += f * rounds[x][in];
-        acc += f * os[(x * 16 * AT + in) * CH + (ch ^ (in & 15))];
-      }
-      const bool none = __builtin_bit_cast(uint32_t, all) == 0u;      // (by its bits: NaNs are not regarded in this file)
-      acc *= none ? 0.f : 1.f / all_rounded;
-      const float lse2 = none ? -INFINITY : m + __builtin_amdgcn_logf(all);
-      if (it.slot >= 0) {
-        const int64_t pr = it.slot * p.own_rows + 16 * y0 + in;
-        *reinterpret_cast<f32x4*>(p.part_o + pr * D + 4 * ch) = acc;
-        if (ch == 0) p.part_lse[pr] = lse2;
-      } else {
-        const int h = hk * p.G + row % p.G;
-        *reinterpret_cast<u32x2*>(p.o + b * p.o_sb + h * p.o_sh + tok * p.o_st + 4 * ch) = u32x2{T::pack_o(acc.x, acc.y), T::pack_o(acc.z, acc.w)};
-        if (ch == 0 && p.lse) p.lse[((int64_t)b * p.H + h) * p.Nq + tok] = lse2 * 0.69314718055994531f;
-      }
-    }
+    if (j + 1 == left) return;
+    __syncthreads();                       // the tile behind the next one goes where the results were
+    if (next.b != at.b) q_len = paged_q_len(p, next.b);
+    at = next;
+    next = after;
+    first = 0;
+    begin(at);
   }
 }
 
 // Joins partial results, D / 4 lanes a part of a row, four values each: WAYS of them a row, which take its parts in turn.
 template <class T, int D, int WAYS>
 __global__ __launch_bounds__(256) void dbsp_paged_merge_kernel(const dbsp_paged_attn_params p, int tile_rows) {
-  constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, U = WAYS > 1 ? 8 : 4;
-  const int unit = threadIdx.x / LANES, way = unit % WAYS, x = 4 * (threadIdx.x % LANES);
-  const int64_t nth = (int64_t)blockIdx.x * ROWS + unit / WAYS;      // [b][h][t]
-  const bool there = nth < (int64_t)p.B * p.H * p.Nq;
-  const int t = there ? (int)(nth % p.Nq) : 0, h = there ? (int)(nth / p.Nq % p.H) : 0, b = there ? (int)(nth / p.Nq / p.H) : 0;
-  const int first = p.table[2 * b], n = p.table[2 * b + 1], row = t * p.G + h % p.G;
-  const bool mine = there && t < paged_q_len(p, b) && n > 1;      // (a part alone has been written as it is)
-  const int64_t step = (int64_t)p.row_tiles * p.own_rows;
-  const int64_t at = ((int64_t)first * p.Hk * p.row_tiles + (int64_t)(h / p.G) * n * p.row_tiles + row / tile_rows) * p.own_rows + row % tile_rows;
+  constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, U = 8;
+  const int lanes = threadIdx.x / LANES, way = lanes % WAYS, x = 4 * (threadIdx.x % LANES);
+  const unsigned nth = blockIdx.x * ROWS + lanes / WAYS, all = (unsigned)p.B * p.H * p.Nq, at_row = min(nth, all - 1);      // [b][h][t]
+  const unsigned bh = at_row / (unsigned)p.Nq;
+  const int t = (int)(at_row - bh * p.Nq), b = (int)(bh / (unsigned)p.H), h = (int)(bh - b * p.H), hk = (int)((unsigned)h / (unsigned)p.G);
+  const int32_t* const q_lens = p.q_lens ? p.q_lens : p.lens;
+  const unsigned chunk = (unsigned)p.table[0], parts = (unsigned)p.table[1], before = (unsigned)p.table[2 + 2 * b], tiles = (unsigned)p.table[3 + 2 * b];
+  const int q_as_given = q_lens[b];
+  const int row = t * p.G + h - hk * p.G, rt = row / tile_rows;
+  // the runs that the row tile lies in, or its parts
+  const unsigned unit = (unsigned)(p.Hk * p.row_tiles), pair = (unsigned)(hk * p.row_tiles + rt);
+  unsigned run0, n;
+  if (parts) {
+    n = (tiles + chunk - 1) / chunk;
+    run0 = before * unit + pair * n;
+    const unsigned per = (tiles + n - 1) / n;
+    n = (tiles + per - 1) / per;           // (the last ones may have none left)
+  } else {
+    const unsigned from = before * unit + pair * tiles;
+    run0 = from / chunk;
+    n = (from + tiles - 1) / chunk - run0 + 1;
+  }
+  const bool mine = nth < all && (!p.q_lens || t < q_as_given) && n > 1;      // (a row tile in one run has been written as it is)
+  const int64_t step = p.own_rows, at = ((int64_t)run0 + (int64_t)b * unit + pair) * p.own_rows + row - rt * tile_rows;
   float m = -FLT_MAX, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = way; mine && i0 < n; i0 += U * WAYS) {
+  for (int i0 = way; mine && i0 < (int)n; i0 += U * WAYS) {
     float ls[U];
     f32x4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * WAYS;
-      const int64_t pr = at + min(i, n - 1) * step;
-      ls[u] = i < n ? p.part_lse[pr] : -INFINITY;
+      const int64_t pr = at + min(i, (int)n - 1) * step;
+      ls[u] = i < (int)n ? p.part_lse[pr] : -INFINITY;
       v[u] = *reinterpret_cast<const f32x4*>(p.part_o + pr * D + x);
     }
     float to = m;
@@ -348,32 +459,31 @@ __global__ __launch_bounds__(256) void dbsp_paged_merge_kernel(const dbsp_paged_
     acc *= f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + u * WAYS >= n) break;
       const float wgt = __builtin_amdgcn_exp2f(ls[u] - m);
       sum += wgt;
-      acc += wgt * v[u];                   // (a part without a key has zeros)
+      acc += wgt * v[u];                   // (a part without a key has zeros; the last part again, past the end, weighs nothing)
     }
   }
   if constexpr (WAYS > 1) {
-    static_assert(ROWS == 1, "a row a workgroup");
-    __shared__ f32x4 accs[WAYS][LANES];
-    __shared__ float ms[WAYS], sums[WAYS];
-    accs[way][threadIdx.x % LANES] = acc;
+    __shared__ f32x4 accs[ROWS][WAYS][LANES];
+    __shared__ float ms[ROWS][WAYS], sums[ROWS][WAYS];
+    const int r = lanes / WAYS, lane = threadIdx.x % LANES;
+    accs[r][way][lane] = acc;
     if (x == 0) {
-      ms[way] = m;
-      sums[way] = sum;
+      ms[r][way] = m;
+      sums[r][way] = sum;
     }
     __syncthreads();
     if (way != 0) return;
 #pragma unroll
-    for (int y = 1; y < WAYS; ++y) m = fmaxf(m, ms[y]);
+    for (int y = 1; y < WAYS; ++y) m = fmaxf(m, ms[r][y]);
     sum = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int y = 0; y < WAYS; ++y) {
-      const float f = __builtin_amdgcn_exp2f(ms[y] - m);
-      sum += f * sums[y];
-      acc += f * accs[y][threadIdx.x % LANES];
+      const float f = __builtin_amdgcn_exp2f(ms[r][y] - m);
+      sum += f * sums[r][y];
+      acc += f * accs[r][y][lane];
     }
   }
   if (!mine) return;
@@ -391,8 +501,10 @@ hipError_t launch(const dbsp_paged_attn_params& p, int grid, hipStream_t stream)
   else if constexpr (D == 64) dbsp_paged_attn_kernel<T, D, 4><<<grid, 256, 0, stream>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.merge_groups == 0) return e;
-  if (p.merge_by_row) dbsp_paged_merge_kernel<T, D, 256 / (D / 4)><<<p.merge_groups, 256, 0, stream>>>(p, tile_rows);
-  else dbsp_paged_merge_kernel<T, D, 1><<<p.merge_groups, 256, 0, stream>>>(p, tile_rows);
+  if (p.merge_ways == 1) dbsp_paged_merge_kernel<T, D, 1><<<p.merge_groups, 256, 0, stream>>>(p, tile_rows);
+  else if (p.merge_ways == 2) dbsp_paged_merge_kernel<T, D, 2><<<p.merge_groups, 256, 0, stream>>>(p, tile_rows);
+  else if (p.merge_ways == 4) dbsp_paged_merge_kernel<T, D, 4><<<p.merge_groups, 256, 0, stream>>>(p, tile_rows);
+  else dbsp_paged_merge_kernel<T, D, 8><<<p.merge_groups, 256, 0, stream>>>(p, tile_rows);
   return hipGetLastError();
 }
 

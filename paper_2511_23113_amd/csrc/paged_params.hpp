@@ -5,12 +5,11 @@
 
 #include <cstdint>
 
+constexpr int64_t kMostSlots = (int64_t)1 << 30;      // of a sequence, and less
 constexpr int kPagedKeys = 64;         // keys of a tile, 16 a wave
 // Rows of a row tile: 16, 32, or at d = 64 64, by how many there are (64 of d = 128 do not fit into the registers of two waves)
 constexpr int paged_tile_rows(int64_t rows, int d) { return rows <= 16 ? 16 : rows <= 32 || d == 128 ? 32 : 64; }
-constexpr int kPagedTarget = 1024;     // items that a launch is cut into where there is enough to cut
-constexpr int kPagedWhole = 10;        // tiles that are not cut
-constexpr int kPagedMergeRows = 2048;  // rows up to which a workgroup joins the parts of one
+constexpr int kPagedWhole = 10;        // tiles that a row tile may have at most where each goes to a workgroup of its own, without a merge
 
 // slot / page_size as slot * mul >> shift, for slots below 2^31: with 2^s >= page_size, mul = 2^(31 + s) / page_size rounded up is too large by
 // less than 1, so the product by less than slot / 2^(31 + s) < 2^-s <= 1 / page_size of the quotient.
@@ -21,6 +20,15 @@ inline void paged_divisor(int page_size, uint32_t& mul, uint32_t& shift) {
 }
 __host__ __device__ inline int paged_quotient(int slot, uint32_t mul, uint32_t shift) { return (int)(((uint64_t)(uint32_t)slot * mul) >> shift); }
 
+// The list of tiles is cut into runs if these and the row tiles have at least kPagedLong tiles each on average, else row tiles are cut into parts
+// for themselves: kPagedParts in all, and one more a row tile at most.  us, runs / parts: 256 (sequence, KV head) pairs of 41 tiles 67.4 / 72,
+// 8 of 1650 tiles 83 / 87, 128 of 18 21.7 / 25; but at d = 64 2048 pairs of 6 tiles 52.4 / 49.7, 240 of 12 with 21 rows each 24.3 / 18
+// (parts: 1024 of them 20.5).
+constexpr unsigned kPagedLong = 8, kPagedParts = 512;
+// Runs: two workgroups a compute unit, or one where it draws as much from memory (single tokens at d = 128).  us, one / two: 256 pairs of 41
+// tiles 67.4 / 68.9, 256 of 58 89.4 / 91.2, 1600 of 23 207 / 210; at d = 64 256 of 83 69.1 / 67.0, and 240 of 12 with 21 rows each 43.4 / 29.2.
+constexpr unsigned paged_runs(int64_t rows, int d) { return d == 128 && rows <= 16 ? 256 : 512; }
+
 struct dbsp_paged_attn_params {
   const uint16_t* q;
   const unsigned char *k, *v;
@@ -28,18 +36,20 @@ struct dbsp_paged_attn_params {
   float* lse;                          // f32 [B,H,Nq] or null
   const int32_t *lens, *q_lens, *pages;
   int64_t q_sb, q_sh, q_st, o_sb, o_sh, o_st;      // strides in elements: batch, head, token
-  int64_t k_sp, k_sh, v_sp, v_sh;                  // in bytes: page, head
-  int32_t k_ss, v_ss;                              // in bytes: slot
+  int64_t k_sh, v_sh;                              // in bytes: head
+  uint32_t k_sp, k_ss, v_sp, v_ss;                 // in bytes: page, slot
   int64_t pages_stride;
   int32_t B, H, Hk, G, Nq, n_pages, page_size, max_pages, cap;
   uint32_t page_mul, page_shift;       // see paged_quotient
-  int32_t causal, split, target;
+  int32_t causal, whole;
+  int32_t page_16;                     // a page's slots are a multiple of a wave's 16
+  uint32_t runs;                       // that the list of tiles is cut into
   int32_t row_tiles, own_rows;         // of a (sequence, KV head); rows of a partial result
   float scale_log2;                    // softmax scale * log2(e)
   // workspace
-  int32_t* table;                      // [2 B] first part and parts of every sequence
-  float *part_o, *part_lse;            // f32 [items][own_rows][d], [items][own_rows] (base 2)
-  int32_t merge_groups, merge_by_row;
+  int32_t* table;                      // [2 + 2 B] tiles of a run; of every sequence tiles before it, and its own
+  float *part_o, *part_lse;            // f32 [parts][own_rows][d], [parts][own_rows] (base 2)
+  int32_t merge_groups, merge_ways;    // workgroups of the merge, and how many of a row's parts it takes at a time, eight each
 };
 
 hipError_t dbsp_launch_paged_attn(const dbsp_paged_attn_params& p, int d, bool fp16, int grid, hipStream_t stream);

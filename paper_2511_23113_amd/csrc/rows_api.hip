@@ -3,8 +3,11 @@
 
 #include <cmath>
 
-int dbsp_rows_settle(const char* who, const dbsp_head_norm* norm, const dbsp_rotary* rotary, const int32_t* positions, int64_t pos_batch,
-                     int64_t pos_token, int32_t B, int32_t N, int32_t d, dbsp_rows_params& p, int& kind, bool& halves) {
+int dbsp_rows_settle(const char* who, const dbsp_qk_rows* rows, const dbsp_head_norm* norm, const dbsp_rotary* rotary, dbsp_rows_params& p, int& kind,
+                     bool& halves) {
+  if (!rows) return fail(who, DBSP_EINVAL, "null pointer (rows)");
+  const int32_t B = rows->B, N = rows->N, d = rows->d;
+  if (rows->dtype != DBSP_BF16 && rows->dtype != DBSP_FP16) return fail(who, DBSP_EINVAL, "dtype must be DBSP_BF16 or DBSP_FP16");
   if (d != 64 && d != 128) return fail(who, DBSP_EINVAL, "head dim must be 64 or 128");
   if (B <= 0 || N <= 0) return fail(who, DBSP_EINVAL, "the numbers of sequences and tokens must be positive");
   if ((int64_t)B * N > kMost) return fail(who, DBSP_ESHAPE, "too many tokens");
@@ -35,24 +38,26 @@ int dbsp_rows_settle(const char* who, const dbsp_head_norm* norm, const dbsp_rot
     if (!std::isfinite(rotary->freqs[i])) return fail(who, DBSP_EINVAL, "freqs must be finite");
     p.turns[i] = rotary->freqs[i] * 0.15915494309189533577;      // 1 / (2 pi)
   }
+  const int32_t* positions = rows->positions;
   if (!positions && axes > 1) return fail(who, DBSP_EINVAL, "a rotation of several axes needs positions");
   if (!aligned(positions, 4)) return fail(who, DBSP_EINVAL, "positions must be 4-byte aligned");
   if (positions && axes > 0) {
-    if ((B > 1 && (pos_batch < 0 || pos_batch > (int64_t)1 << 40)) || (N > 1 && (pos_token < 0 || pos_token > (int64_t)1 << 40)))
-      return fail(who, DBSP_EINVAL, "the strides of positions must not be negative");
+    const int64_t size[2] = {B, N};
+    for (int i = 0; i < 2; ++i)
+      if (size[i] > 1 && (rows->pos_stride[i] < 0 || rows->pos_stride[i] > (int64_t)1 << 40)) return fail(who, DBSP_EINVAL, "the strides of positions must not be negative");
     p.positions = positions;
-    p.pos_sb = step(B, pos_batch);
-    p.pos_st = step(N, pos_token);
+    p.pos_sb = step(B, rows->pos_stride[0]);
+    p.pos_st = step(N, rows->pos_stride[1]);
   }
   return DBSP_OK;
 }
 
-int dbsp_rows_check(const char* who, const char* name, const dbsp_rows_tensor& t, bool written, int32_t B, int32_t heads, int32_t N, int32_t d) {
+int dbsp_rows_check(const char* who, const char* name, const dbsp_heads& t, bool written, int32_t B, int32_t heads, int32_t N, int32_t d) {
   if (!t.x) return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": null pointer (" + name + ")");
-  const int64_t size[3] = {B, heads, N}, stride[3] = {t.batch, t.head, t.token};
-  if (!strides_ok(size, stride, 3) || !aligned(t.x, 16))
+  const int64_t size[3] = {B, heads, N};
+  if (!strides_ok(size, t.stride, 3) || !aligned(t.x, 16))
     return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": " + name + " must be 16-byte aligned, its strides multiples of 8 and a token's at most 2^24");
-  if (written && !distinct(size, stride, d)) return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": elements of " + name + " overlap");
+  if (written && !distinct(size, t.stride, d)) return dbsp_set_error(DBSP_EINVAL, std::string(who) + ": elements of " + name + " overlap");
   return DBSP_OK;
 }
 
@@ -80,56 +85,40 @@ int dbsp_rows_deal(const char* who, dbsp_rows_params& p, int d, int64_t most) {
 
 namespace {
 
-int check_dtype(const char* who, int32_t dtype) { return dtype == DBSP_BF16 || dtype == DBSP_FP16 ? DBSP_OK : fail(who, DBSP_EINVAL, "dtype must be DBSP_BF16 or DBSP_FP16"); }
-
-void set_in(dbsp_rows_part& part, const dbsp_rows_tensor& t, int32_t B, int32_t heads, int32_t N) {
-  part.x = static_cast<const uint16_t*>(t.x);
-  part.x_sb = step(B, t.batch);
-  part.x_sh = step(heads, t.head);
-  part.x_st = step(N, t.token);
-  part.heads = heads;
-}
-void set_out(dbsp_rows_part& part, const dbsp_rows_tensor& t, int32_t B, int32_t heads, int32_t N) {
-  part.y = static_cast<uint16_t*>(const_cast<void*>(t.x));
-  part.y_sb = step(B, t.batch);
-  part.y_sh = step(heads, t.head);
-  part.y_st = step(N, t.token);
-}
-
 int64_t grad_bytes(const dbsp_rows_params& p, int d) { return round_up((int64_t)p.groups * p.walkers * 2 * d * 4, 256); }
+
+// Heads of the queries (0) or keys (1) of a call; 0: it has no such.
+int heads_of(const char* who, const dbsp_qk_rows* rows, int i, int32_t& heads) {
+  heads = i == 0 ? rows->H : rows->k.x ? rows->Hk : 0;
+  return heads > 0 || (i == 1 && !rows->k.x) ? DBSP_OK : fail(who, DBSP_EINVAL, "the numbers of heads must be positive");
+}
 
 }  // namespace
 
 extern "C" {
 
-int dbsp_qk_norm_rope_fwd(int32_t dtype, int32_t B, int32_t N, int32_t d, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
-                          void* q_out, int64_t q_out_batch, int64_t q_out_head, int64_t q_out_token, int32_t H, const void* k, int64_t k_batch,
-                          int64_t k_head, int64_t k_token, void* k_out, int64_t k_out_batch, int64_t k_out_head, int64_t k_out_token, int32_t Hk,
-                          const dbsp_head_norm* norm, const dbsp_rotary* rotary, const int32_t* positions, int64_t pos_batch, int64_t pos_token,
-                          void* stream) {
+int dbsp_qk_norm_rope_fwd(const dbsp_qk_rows* rows, const dbsp_head_norm* norm, const dbsp_rotary* rotary, void* stream) {
   const char* who = "dbsp_qk_norm_rope_fwd";
   dbsp_rows_params p = {};
-  int kind = 0, rc = check_dtype(who, dtype);
+  int kind = 0, rc;
   bool halves = false;
-  if (rc == DBSP_OK) rc = dbsp_rows_settle(who, norm, rotary, positions, pos_batch, pos_token, B, N, d, p, kind, halves);
-  if (rc != DBSP_OK) return rc;
-  if (H <= 0 || (k && Hk <= 0)) return fail(who, DBSP_EINVAL, "the numbers of heads must be positive");
-  const dbsp_rows_tensor in[2] = {{q, q_batch, q_head, q_token}, {k, k_batch, k_head, k_token}};
-  const dbsp_rows_tensor out[2] = {{q_out, q_out_batch, q_out_head, q_out_token}, {k_out, k_out_batch, k_out_head, k_out_token}};
-  static const char* const names[2][2] = {{"q", "q_out"}, {"k", "k_out"}};
-  for (int i = 0; i < (k ? 2 : 1); ++i) {
-    const int32_t heads = i == 0 ? H : Hk;
-    if ((rc = dbsp_rows_check(who, names[i][0], in[i], false, B, heads, N, d)) != DBSP_OK) return rc;
-    if ((rc = dbsp_rows_check(who, names[i][1], out[i], true, B, heads, N, d)) != DBSP_OK) return rc;
-    set_in(p.part[i], in[i], B, heads, N);
-    set_out(p.part[i], out[i], B, heads, N);
+  if ((rc = dbsp_rows_settle(who, rows, norm, rotary, p, kind, halves)) != DBSP_OK) return rc;
+  for (int i = 0; i < 2; ++i) {
+    int32_t heads;
+    if ((rc = heads_of(who, rows, i, heads)) != DBSP_OK) return rc;
+    if (heads == 0) continue;
+    const dbsp_heads &in = i == 0 ? rows->q : rows->k, &out = i == 0 ? rows->q_out : rows->k_out;
+    if ((rc = dbsp_rows_check(who, i == 0 ? "q" : "k", in, false, p.B, heads, p.N, rows->d)) != DBSP_OK) return rc;
+    if ((rc = dbsp_rows_check(who, i == 0 ? "q_out" : "k_out", out, true, p.B, heads, p.N, rows->d)) != DBSP_OK) return rc;
+    set_in(p.part[i], in, p.B, heads, p.N);
+    set_out(p.part[i], out, p.B, heads, p.N);
     if (kind != DBSP_NORM_NONE) {
       p.part[i].gain = i == 0 ? norm->q_gain : norm->k_gain;
       p.part[i].bias = i == 0 ? norm->q_bias : norm->k_bias;
     }
   }
-  if ((rc = dbsp_rows_deal(who, p, d, kRowGroups)) != DBSP_OK) return rc;
-  return done(who, dbsp_launch_rows(p, d, dtype == DBSP_FP16, kind, halves, false, static_cast<hipStream_t>(stream)));
+  if ((rc = dbsp_rows_deal(who, p, rows->d, kRowGroups)) != DBSP_OK) return rc;
+  return done(who, dbsp_launch_rows(p, rows->d, rows->dtype == DBSP_FP16, kind, halves, false, static_cast<hipStream_t>(stream)));
 }
 
 int dbsp_qk_norm_rope_bwd_workspace(int32_t B, int32_t N, int32_t d, int32_t H, int32_t Hk, int64_t* bytes) {
@@ -137,11 +126,14 @@ int dbsp_qk_norm_rope_bwd_workspace(int32_t B, int32_t N, int32_t d, int32_t H, 
   if (!bytes) return fail(who, DBSP_EINVAL, "null pointer");
   *bytes = 0;
   if (H <= 0 || Hk < 0) return fail(who, DBSP_EINVAL, "the numbers of heads must be positive");
+  dbsp_qk_rows rows = {};
+  rows.B = B;
+  rows.N = N;
+  rows.d = d;
   dbsp_rows_params p = {};
-  int kind;
+  int kind, rc;
   bool halves;
-  int rc = dbsp_rows_settle(who, nullptr, nullptr, nullptr, 0, 0, B, N, d, p, kind, halves);
-  if (rc != DBSP_OK) return rc;
+  if ((rc = dbsp_rows_settle(who, &rows, nullptr, nullptr, p, kind, halves)) != DBSP_OK) return rc;
   p.part[0].heads = H;
   p.part[1].heads = Hk;
   if ((rc = dbsp_rows_deal(who, p, d, kGradGroups)) != DBSP_OK) return rc;
@@ -149,43 +141,36 @@ int dbsp_qk_norm_rope_bwd_workspace(int32_t B, int32_t N, int32_t d, int32_t H, 
   return DBSP_OK;
 }
 
-int dbsp_qk_norm_rope_bwd(int32_t dtype, int32_t B, int32_t N, int32_t d, const void* q, int64_t q_batch, int64_t q_head, int64_t q_token,
-                          const void* dq_out, int64_t dq_out_batch, int64_t dq_out_head, int64_t dq_out_token, void* dq, int64_t dq_batch,
-                          int64_t dq_head, int64_t dq_token, int32_t H, const void* k, int64_t k_batch, int64_t k_head, int64_t k_token,
-                          const void* dk_out, int64_t dk_out_batch, int64_t dk_out_head, int64_t dk_out_token, void* dk, int64_t dk_batch,
-                          int64_t dk_head, int64_t dk_token, int32_t Hk, const dbsp_head_norm* norm, const dbsp_rotary* rotary,
-                          const int32_t* positions, int64_t pos_batch, int64_t pos_token, float* grads, void* workspace, int64_t workspace_bytes,
-                          void* stream) {
+int dbsp_qk_norm_rope_bwd(const dbsp_qk_rows* rows, const dbsp_heads* dq, const dbsp_heads* dk, const dbsp_head_norm* norm,
+                          const dbsp_rotary* rotary, float* grads, void* workspace, int64_t workspace_bytes, void* stream) {
   const char* who = "dbsp_qk_norm_rope_bwd";
   dbsp_rows_params p = {};
-  int kind = 0, rc = check_dtype(who, dtype);
+  int kind = 0, rc;
   bool halves = false;
-  if (rc == DBSP_OK) rc = dbsp_rows_settle(who, norm, rotary, positions, pos_batch, pos_token, B, N, d, p, kind, halves);
-  if (rc != DBSP_OK) return rc;
-  if (H <= 0 || (k && Hk <= 0)) return fail(who, DBSP_EINVAL, "the numbers of heads must be positive");
-  const dbsp_rows_tensor in[2] = {{q, q_batch, q_head, q_token}, {k, k_batch, k_head, k_token}};
-  const dbsp_rows_tensor dy[2] = {{dq_out, dq_out_batch, dq_out_head, dq_out_token}, {dk_out, dk_out_batch, dk_out_head, dk_out_token}};
-  const dbsp_rows_tensor dx[2] = {{dq, dq_batch, dq_head, dq_token}, {dk, dk_batch, dk_head, dk_token}};
-  static const char* const names[2][3] = {{"q", "dq_out", "dq"}, {"k", "dk_out", "dk"}};
-  for (int i = 0; i < (k ? 2 : 1); ++i) {
-    const int32_t heads = i == 0 ? H : Hk;
-    if ((rc = dbsp_rows_check(who, names[i][0], in[i], false, B, heads, N, d)) != DBSP_OK) return rc;
-    if ((rc = dbsp_rows_check(who, names[i][1], dy[i], false, B, heads, N, d)) != DBSP_OK) return rc;
-    if ((rc = dbsp_rows_check(who, names[i][2], dx[i], true, B, heads, N, d)) != DBSP_OK) return rc;
+  if ((rc = dbsp_rows_settle(who, rows, norm, rotary, p, kind, halves)) != DBSP_OK) return rc;
+  for (int i = 0; i < 2; ++i) {
+    int32_t heads;
+    if ((rc = heads_of(who, rows, i, heads)) != DBSP_OK) return rc;
+    if (heads == 0) continue;
+    const dbsp_heads &in = i == 0 ? rows->q : rows->k, &dy = i == 0 ? rows->q_out : rows->k_out, *dx = i == 0 ? dq : dk;
+    if (!dx) return fail(who, DBSP_EINVAL, i == 0 ? "null pointer (dq)" : "null pointer (dk)");
+    if ((rc = dbsp_rows_check(who, i == 0 ? "q" : "k", in, false, p.B, heads, p.N, rows->d)) != DBSP_OK) return rc;
+    if ((rc = dbsp_rows_check(who, i == 0 ? "q_out" : "k_out", dy, false, p.B, heads, p.N, rows->d)) != DBSP_OK) return rc;
+    if ((rc = dbsp_rows_check(who, i == 0 ? "dq" : "dk", *dx, true, p.B, heads, p.N, rows->d)) != DBSP_OK) return rc;
     dbsp_rows_part& part = p.part[i];
-    set_in(part, in[i], B, heads, N);
-    set_out(part, dx[i], B, heads, N);
-    part.dy = static_cast<const uint16_t*>(dy[i].x);
-    part.dy_sb = step(B, dy[i].batch);
-    part.dy_sh = step(heads, dy[i].head);
-    part.dy_st = step(N, dy[i].token);
+    set_in(part, in, p.B, heads, p.N);
+    set_out(part, *dx, p.B, heads, p.N);
+    part.dy = static_cast<const uint16_t*>(dy.x);
+    part.dy_sb = step(p.B, dy.stride[0]);
+    part.dy_sh = step(heads, dy.stride[1]);
+    part.dy_st = step(p.N, dy.stride[2]);
     if (kind != DBSP_NORM_NONE) part.gain = i == 0 ? norm->q_gain : norm->k_gain;
   }
   if (grads && kind == DBSP_NORM_NONE) return fail(who, DBSP_EINVAL, "without a norm there are no gains to form gradients of");
   if (!aligned(grads, 16)) return fail(who, DBSP_EINVAL, "grads must be 16-byte aligned");
-  if ((rc = dbsp_rows_deal(who, p, d, kGradGroups)) != DBSP_OK) return rc;
+  if ((rc = dbsp_rows_deal(who, p, rows->d, kGradGroups)) != DBSP_OK) return rc;
   if (grads) {
-    const int64_t need = grad_bytes(p, d);
+    const int64_t need = grad_bytes(p, rows->d);
     if (!workspace) return fail(who, DBSP_EINVAL, "null pointer (workspace)");
     if (!aligned(workspace, 256)) return fail(who, DBSP_EINVAL, "the workspace must be 256-byte aligned");
     if (workspace_bytes < need)
@@ -193,7 +178,7 @@ int dbsp_qk_norm_rope_bwd(int32_t dtype, int32_t B, int32_t N, int32_t d, const 
     p.grads = grads;
     p.sums = static_cast<float*>(workspace);
   }
-  return done(who, dbsp_launch_rows_grad(p, d, dtype == DBSP_FP16, kind, halves, static_cast<hipStream_t>(stream)));
+  return done(who, dbsp_launch_rows_grad(p, rows->d, rows->dtype == DBSP_FP16, kind, halves, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -35,15 +35,22 @@ def ref(x):
     return None if x is None else C.byref(x)
 
 
+def packed(dtype, nb, n, d, H, Hk, q, qs, k, ks, qo, qos, ko, kos, pos, pb, pt):
+    return B._QK_ROWS.pack(dtype, nb, n, d, H, Hk, q or 0, *qs, k or 0, *ks, qo or 0, *qos, ko or 0, *kos, pos or 0, pb, pt)
+
+
 def fwd(dtype=0, nb=2, n=8, d=64, q=FAKE, qs=STRIDES, qo=FAKE, qos=STRIDES, H=2, k=FAKE, ks=STRIDES, ko=FAKE, kos=STRIDES, Hk=2, nrm=norm(), rot=rotary(),
         pos=FAKE, pb=24, pt=3):
-    return said(B.load_library().dbsp_qk_norm_rope_fwd(dtype, nb, n, d, q, *qs, qo, *qos, H, k, *ks, ko, *kos, Hk, ref(nrm), ref(rot), pos, pb, pt, None))
+    rows = packed(dtype, nb, n, d, H, Hk, q, qs, k, ks, qo, qos, ko, kos, pos, pb, pt)
+    return said(B.load_library().dbsp_qk_norm_rope_fwd(rows, ref(nrm), ref(rot), None))
 
 
 def bwd(dtype=0, nb=2, n=8, d=64, q=FAKE, qs=STRIDES, qo=FAKE, qos=STRIDES, H=2, k=FAKE, ks=STRIDES, ko=FAKE, kos=STRIDES, Hk=2, nrm=norm(), rot=rotary(),
         pos=FAKE, pb=24, pt=3, dy=FAKE, dys=STRIDES, grads=FAKE, ws=FAKE, size=1 << 40):
-    return said(B.load_library().dbsp_qk_norm_rope_bwd(dtype, nb, n, d, q, *qs, dy, *dys, qo, *qos, H, k, *ks, dy, *dys, ko, *kos, Hk, ref(nrm), ref(rot),
-                                                       pos, pb, pt, grads, ws, size, None))
+    # q_out and k_out of the forward pass: dq and dk here, behind gradients of the results that are all right
+    rows = packed(dtype, nb, n, d, H, Hk, q, qs, k, ks, dy, dys, dy, dys, pos, pb, pt)
+    dx = [B._HEADS.pack(x or 0, *xs) for x, xs in ((qo, qos), (ko, kos))]
+    return said(B.load_library().dbsp_qk_norm_rope_bwd(rows, *dx, ref(nrm), ref(rot), grads, ws, size, None))
 
 
 def cache(**kw):
@@ -57,8 +64,10 @@ def cache(**kw):
     return x
 
 
-def append(c, nrm=norm(), rot=rotary(), k=FAKE, ks=STRIDES, v=FAKE, vs=STRIDES, q=FAKE, qs=STRIDES, qo=FAKE, qos=STRIDES, H=2, n=8, new=None, pos=FAKE, pb=24, pt=3):
-    return said(B.load_library().dbsp_paged_append(ref(c), k, *ks, v, *vs, q, *qs, qo, *qos, H, n, new, ref(nrm), ref(rot), pos, pb, pt, None))
+def append(c, nrm=norm(), rot=rotary(), k=FAKE, ks=STRIDES, v=FAKE, vs=STRIDES, q=FAKE, qs=STRIDES, qo=FAKE, qos=STRIDES, H=2, n=8, new=None, pos=FAKE, pb=24, pt=3, **other):
+    nb, hk, d, dtype = (c.B, c.Hk, c.d, c.dtype) if c is not None else (1, 1, 64, 0)
+    rows = packed(other.get("dtype", dtype), other.get("B", nb), n, other.get("d", d), H, other.get("Hk", hk), q, qs, k, ks, qo, qos, None, STRIDES, pos, pb, pt)
+    return said(B.load_library().dbsp_paged_append(ref(c), rows, B._HEADS.pack(v or 0, *vs), new, ref(nrm), ref(rot), None))
 
 
 def attn(c, q=FAKE, qs=STRIDES, o=FAKE, os_=STRIDES, lse=FAKE, q_lens=None, H=2, n=1, scale=0.0, ws=FAKE, size=1 << 40):
@@ -92,7 +101,7 @@ def test_too_many_tokens_or_heads():
 
 
 BACKWARD = [
-    (dict(dy=None), "dq_out"), (dict(dys=(1024, 4, 64)), "dq_out"), (dict(nrm=None), "no gains"), (dict(nrm=norm(kind=0)), "no gains"), (dict(grads=FAKE + 4), "16-byte"),
+    (dict(dy=None), "q_out"), (dict(dys=(1024, 4, 64)), "q_out"), (dict(nrm=None), "no gains"), (dict(nrm=norm(kind=0)), "no gains"), (dict(grads=FAKE + 4), "16-byte"),
     (dict(ws=None), "workspace"), (dict(ws=FAKE + 16), "256-byte"), (dict(size=100), "holds 100 bytes"),
 ]
 
@@ -117,7 +126,7 @@ PAGED = [
     (dict(dtype=7), "dtype"), (dict(d=80), "head dim"), (dict(B=0), "positive"), (dict(Hk=0), "positive"), (dict(n_pages=0), "positive"), (dict(page_size=0), "positive"),
     (dict(max_pages=-1), "positive"), (dict(k=None), "null"), (dict(v=None), "null"), (dict(pages=None), "null"), (dict(lens=None), "null"), (dict(k=FAKE + 4), "16-byte"),
     (dict(k_stride=(2048, 1024, 60)), "multiples of 8"), (dict(v_stride=(2048, 1024, -64)), "multiples of 8"), (dict(v_stride=(2048, 1024, (1 << 24) + 8)), "2^24"),
-    (dict(pages_stride=3), "pages_stride"), (dict(pages=FAKE + 2), "4-byte"), (dict(lens=FAKE + 1), "4-byte"),
+    (dict(k_stride=((1 << 30) + 8, 1024, 64)), "2^30"), (dict(pages_stride=3), "pages_stride"), (dict(pages=FAKE + 2), "4-byte"), (dict(lens=FAKE + 1), "4-byte"),
 ]
 
 
@@ -147,6 +156,18 @@ APPEND = [
 def test_bad_appends(change, word):
     rc, msg = append(cache(), **change)
     assert rc == B.DBSP_EINVAL and word in msg
+
+
+def test_appended_rows_that_are_not_the_caches():
+    for change in (dict(dtype=1), dict(B=3), dict(d=128), dict(Hk=1)):
+        rc, msg = append(cache(), **change)
+        assert rc == B.DBSP_ESHAPE and "the cache's" in msg
+    lib = B.load_library()
+    assert lib.dbsp_paged_append(C.byref(cache()), None, None, None, None, None, None) == B.DBSP_EINVAL
+    assert lib.dbsp_qk_norm_rope_fwd(None, None, None, None) == B.DBSP_EINVAL
+    rows = packed(0, 2, 8, 64, 2, 2, FAKE, STRIDES, FAKE, STRIDES, FAKE, STRIDES, FAKE, STRIDES, None, 0, 0)
+    assert said(lib.dbsp_qk_norm_rope_bwd(rows, None, None, None, None, None, None, 0, None))[1].endswith("(dq)")
+    assert said(lib.dbsp_paged_append(C.byref(cache()), rows, None, None, None, None, None))[1].endswith("(v)")
 
 
 def test_pools_that_are_written_do_not_overlap():

@@ -20,7 +20,7 @@ def test_m0_is_the_copies_own(lines):
     assert sum(map(names_m0, lines)) == set_here > 0
     for block in asm_blocks(lines):
         if any("_lds_" in line for line in block):      # each copy behind the setting of its destination, in one block
-            assert re.match(r"s_mov_b32 m0, s\d+$", block[0]) and block[1] == "s_nop 0" and re.match(r"global_load_lds_dword(x4)? v\[\d+:\d+\], off", block[2])
+            assert re.match(r"s_mov_b32 m0, s\d+$", block[0]) and block[1] == "s_nop 0" and re.match(r"global_load_lds_dword(x4)? (v\[\d+:\d+\], off|v\d+, s\[\d+:\d+\])$", block[2])
 
 
 def test_the_compiler_waits_for_no_memory_inside_the_loop(lines):
@@ -32,4 +32,5 @@ def test_the_compiler_waits_for_no_memory_inside_the_loop(lines):
     for first, last in zip(waits, ends):
         assert first < last
         assert not [line for line in lines[first + 1:last] if "vmcnt" in line]
-        assert sum("global_load_lds_dwordx4" in line for line in lines[first:last]) == int(re.search(r"vmcnt\((\d+)\)", lines[first])[1])
+        # (by either of two ways: pages of the wave's keys each for itself, or one for all)
+        assert sum("global_load_lds_dwordx4" in line for line in lines[first:last]) == 2 * int(re.search(r"vmcnt\((\d+)\)", lines[first])[1])
