@@ -604,19 +604,21 @@ class _Rows(_OnDevice):
         self.device, self._index, self._at, self._bytes = _torch.device("cuda", index), index, None, {}
 
 
-_rows_on = {}
+_rows_on, _ROW_TYPES = {}, {}
 
 
 def _on_rows(q):
     """What q's calls run on; q is a tensor that they can begin with."""
-    torch = _torch_module()
-    if q.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float16) or not q.is_cuda or q.stride(3) != 1:
-        raise ValueError("q must be [B, H, N, d] in bf16 or fp16 on a GPU, with a dense last dimension")
-    index = q.get_device()
-    here = _rows_on.get(index)
+    here = _rows_on.get(q.get_device())
     if here is None:
+        torch = _torch_module()
+        if not q.is_cuda:
+            raise ValueError("q must be on a GPU")
         load_library()
-        here = _rows_on[index] = _Rows(index)
+        _ROW_TYPES.update({torch.bfloat16: 0, torch.float16: 1})
+        here = _rows_on[q.get_device()] = _Rows(q.get_device())
+    if q.dim() != 4 or q.dtype not in _ROW_TYPES:
+        raise ValueError("q must be [B, H, N, d] in bf16 or fp16")
     return here
 
 
@@ -645,7 +647,7 @@ def qk_norm_rope_fwd(q, k=None, norm: HeadNorm = None, rotary: Rotary = None, po
     (see dbsp.h: dbsp_qk_norm_rope_fwd).  Enqueues on `stream` (default: torch's current stream) and returns (q_out, k_out)."""
     here = _on_rows(q)
     raw, elsewhere = here._on(stream)
-    shape, dtype, index, q_s = q.shape, q.dtype, here._index, q.stride()
+    shape, dtype, index = q.shape, q.dtype, here._index
     B, H, N, d = shape
     if q_out is None:
         q_out = here._empty(shape, dtype, raw, elsewhere)
@@ -660,7 +662,7 @@ def qk_norm_rope_fwd(q, k=None, norm: HeadNorm = None, rotary: Rotary = None, po
         k_out_at = _heads("k_out", k_out, shape_k, dtype, index)
     elif k_out is not None:
         raise ValueError("k_out without k")
-    rows = _QK_ROWS.pack(dtype is _torch.float16, B, N, d, H, Hk, q.data_ptr(), q_s[0], q_s[1], q_s[2], *k_at, *_heads("q_out", q_out, shape, dtype, index),
+    rows = _QK_ROWS.pack(_ROW_TYPES[dtype], B, N, d, H, Hk, *_heads("q", q, shape, dtype, index), *k_at, *_heads("q_out", q_out, shape, dtype, index),
                          *k_out_at, *_positions(positions, rotary, B, N, index))
     rc = _lib.dbsp_qk_norm_rope_fwd(rows, None if norm is None else norm._of(q), None if rotary is None else rotary._at, raw)
     if rc:
@@ -677,7 +679,7 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, norm: HeadNorm = None, rotary: Rotary
     norm has, f32 [d] by name (see dbsp.h: dbsp_qk_norm_rope_bwd).  Enqueues on `stream` and returns (dq, dk, gains)."""
     here = _on_rows(q)
     raw, elsewhere = here._on(stream)
-    shape, dtype, index, q_s = q.shape, q.dtype, here._index, q.stride()
+    shape, dtype, index = q.shape, q.dtype, here._index
     B, H, N, d = shape
     if dq is None:
         dq = here._empty(shape, dtype, raw, elsewhere)
@@ -695,7 +697,7 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, norm: HeadNorm = None, rotary: Rotary
         dk_at = _HEADS.pack(*_heads("dk", dk, shape_k, dtype, index))
     elif dk_out is not None or dk is not None:
         raise ValueError("dk_out or dk without k")
-    rows = _QK_ROWS.pack(dtype is _torch.float16, B, N, d, H, Hk, q.data_ptr(), q_s[0], q_s[1], q_s[2], *k_at, *_heads("dq_out", dq_out, shape, dtype, index),
+    rows = _QK_ROWS.pack(_ROW_TYPES[dtype], B, N, d, H, Hk, *_heads("q", q, shape, dtype, index), *k_at, *_heads("dq_out", dq_out, shape, dtype, index),
                          *k_out_at, *_positions(positions, rotary, B, N, index))
     dq_at = _HEADS.pack(*_heads("dq", dq, shape, dtype, index))
     norm_at, grads, grads_at, at, size, gains = None, None, None, None, 0, {}

@@ -87,6 +87,9 @@ namespace {
 
 int64_t grad_bytes(const dbsp_rows_params& p, int d) { return round_up((int64_t)p.groups * p.walkers * 2 * d * 4, 256); }
 
+// Of queries and keys together.
+int64_t tensor_bytes(const dbsp_rows_params& p, int d) { return (int64_t)p.B * p.N * (p.part[0].heads + p.part[1].heads) * d * 2; }
+
 // Heads of the queries (0) or keys (1) of a call; 0: it has no such.
 int heads_of(const char* who, const dbsp_qk_rows* rows, int i, int32_t& heads) {
   heads = i == 0 ? rows->H : rows->k.x ? rows->Hk : 0;
@@ -112,12 +115,14 @@ int dbsp_qk_norm_rope_fwd(const dbsp_qk_rows* rows, const dbsp_head_norm* norm, 
     if ((rc = dbsp_rows_check(who, i == 0 ? "q_out" : "k_out", out, true, p.B, heads, p.N, rows->d)) != DBSP_OK) return rc;
     set_in(p.part[i], in, p.B, heads, p.N);
     set_out(p.part[i], out, p.B, heads, p.N);
+    p.part[i].plain = kind == DBSP_NORM_NONE && p.turned == 0;
     if (kind != DBSP_NORM_NONE) {
       p.part[i].gain = i == 0 ? norm->q_gain : norm->k_gain;
       p.part[i].bias = i == 0 ? norm->q_bias : norm->k_bias;
     }
   }
   if ((rc = dbsp_rows_deal(who, p, rows->d, kRowGroups)) != DBSP_OK) return rc;
+  p.stream = tensor_bytes(p, rows->d) * 2 >= kRowStream;
   return done(who, dbsp_launch_rows(p, rows->d, rows->dtype == DBSP_FP16, kind, halves, false, static_cast<hipStream_t>(stream)));
 }
 
@@ -169,6 +174,7 @@ int dbsp_qk_norm_rope_bwd(const dbsp_qk_rows* rows, const dbsp_heads* dq, const 
   if (grads && kind == DBSP_NORM_NONE) return fail(who, DBSP_EINVAL, "without a norm there are no gains to form gradients of");
   if (!aligned(grads, 16)) return fail(who, DBSP_EINVAL, "grads must be 16-byte aligned");
   if ((rc = dbsp_rows_deal(who, p, rows->d, kGradGroups)) != DBSP_OK) return rc;
+  p.stream = tensor_bytes(p, rows->d) * 3 >= kRowStream;
   if (grads) {
     const int64_t need = grad_bytes(p, rows->d);
     if (!workspace) return fail(who, DBSP_EINVAL, "null pointer (workspace)");

@@ -9,6 +9,11 @@ constexpr int kRowThreads = 256;       // of a workgroup: d / 8 lanes a row, eac
 constexpr int kRowGroups = 2048;       // workgroups that a launch is cut into where there is enough to cut: eight a compute unit
 constexpr int kGradGroups = 1024;      // those of the backward pass, which leave a partial sum each
 
+// Bytes that a launch reads and writes from which it goes past the caches, which hold 256 MB: what it leaves there does not live until it is
+// read.  us, through / past them, and with a reader of the results behind it: 32,760 tokens of 40 + 40 heads of 128 (1342 MB) 265 / 253,
+// 483 / 474, 8000 tokens 68 / 63, 115 / 116, but 12,303 tokens of 30 + 10 heads of 64 (126 MB) 30.5 / 33.3, 52.6 / 59.7.
+constexpr int64_t kRowStream = (int64_t)512 << 20;
+
 // One of a launch's tensors: queries, keys, or (appended) values, whose heads are dealt to `groups` workgroups, `per` each.
 struct dbsp_rows_part {
   const uint16_t* x;                   // [B, heads, N, d], strides in elements
@@ -28,6 +33,7 @@ struct dbsp_rows_params {
   int32_t tiles;                       // of tokens, those of a workgroup each
   int32_t groups;                      // of heads, over all parts
   int32_t gains_f32;
+  int32_t stream;                      // see kRowStream
   float eps;
   const int32_t* positions;            // [B, N, axes], or null: the token's place, or its slot
   int64_t pos_sb, pos_st;
