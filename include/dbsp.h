@@ -388,7 +388,7 @@ typedef struct dbsp_paged_cache {
   /* strides in elements, of page, head and slot; d has stride 1.  Multiples of 8, at least 0, a slot's at most 2^24, a page's at most 2^30 (that of
    * a dimension of one is not looked at).  dbsp_paged_append writes k and v: no two of their elements may share a place */
   int64_t k_stride[3], v_stride[3];
-  const int32_t* pages;       /* device, int32 [B, max_pages], the sequences pages_stride elements apart (at least max_pages) */
+  const int32_t* pages;       /* device, int32 [B, max_pages], the sequences pages_stride elements apart (at least 0) */
   int64_t pages_stride;
   const int32_t* lens;        /* device, int32 [B]: used slots; taken as 0 below 0 and as max_pages * page_size above it */
 } dbsp_paged_cache;

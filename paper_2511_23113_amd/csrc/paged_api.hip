@@ -18,7 +18,7 @@ int check_paged(const char* who, const dbsp_paged_cache* c) {
   if (!strides_ok(size, c->k_stride, 3) || !strides_ok(size, c->v_stride, 3) || !aligned(c->k, 16) || !aligned(c->v, 16))
     return fail(who, DBSP_EINVAL, "k and v must be 16-byte aligned, their strides multiples of 8 and a slot's at most 2^24");
   if (c->n_pages > 1 && (c->k_stride[0] > (int64_t)1 << 30 || c->v_stride[0] > (int64_t)1 << 30)) return fail(who, DBSP_EINVAL, "the pages of k and v must be at most 2^30 elements apart");
-  if (c->B > 1 && (c->pages_stride < c->max_pages || c->pages_stride > (int64_t)1 << 40)) return fail(who, DBSP_EINVAL, "pages_stride must be at least max_pages");
+  if (c->B > 1 && (c->pages_stride < 0 || c->pages_stride > (int64_t)1 << 40)) return fail(who, DBSP_EINVAL, "pages_stride must not be negative");
   if (!aligned(c->pages, 4) || !aligned(c->lens, 4)) return fail(who, DBSP_EINVAL, "pages and lens must be 4-byte aligned");
   return DBSP_OK;
 }

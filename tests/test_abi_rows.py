@@ -126,7 +126,7 @@ PAGED = [
     (dict(dtype=7), "dtype"), (dict(d=80), "head dim"), (dict(B=0), "positive"), (dict(Hk=0), "positive"), (dict(n_pages=0), "positive"), (dict(page_size=0), "positive"),
     (dict(max_pages=-1), "positive"), (dict(k=None), "null"), (dict(v=None), "null"), (dict(pages=None), "null"), (dict(lens=None), "null"), (dict(k=FAKE + 4), "16-byte"),
     (dict(k_stride=(2048, 1024, 60)), "multiples of 8"), (dict(v_stride=(2048, 1024, -64)), "multiples of 8"), (dict(v_stride=(2048, 1024, (1 << 24) + 8)), "2^24"),
-    (dict(k_stride=((1 << 30) + 8, 1024, 64)), "2^30"), (dict(pages_stride=3), "pages_stride"), (dict(pages=FAKE + 2), "4-byte"), (dict(lens=FAKE + 1), "4-byte"),
+    (dict(k_stride=((1 << 30) + 8, 1024, 64)), "2^30"), (dict(pages_stride=-4), "pages_stride"), (dict(pages=FAKE + 2), "4-byte"), (dict(lens=FAKE + 1), "4-byte"),
 ]
 
 

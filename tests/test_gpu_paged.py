@@ -103,6 +103,11 @@ ATTN = {
     "many_sequences": (130, 2, 1, 1, 64, 16, [i * 37 % 1100 for i in range(130)], None, True, "bf16", "heads", []),
     "whole_batch_uncut": (70, 32, 16, 1, 64, 32, [i * 11 % 200 for i in range(70)], None, True, "fp16", "heads", []),
     "cut_into_many_parts": (1, 2, 1, 1, 64, 64, [20000], None, True, "fp16", "heads", [(0, 100)]),
+    # long enough for runs over several row tiles: more than 64 sequences, some without new tokens or keys; several row tiles a KV head
+    "runs": (70, 4, 2, 2, 128, 16, [(i * 613) % 2900 for i in range(70)], [i % 3 for i in range(70)], True, "bf16", "slots", [(1, 5), (9, 0), (33, 60)]),
+    "runs_64": (70, 2, 2, 1, 64, 24, [(i * 1013) % 5000 for i in range(70)], None, True, "fp16", "heads", [(2, 3), (69, 0)]),
+    "runs_row_tiles": (2, 80, 1, 1, 128, 64, [26000, 23000], None, True, "bf16", "heads", [(0, 100), (1, 0)]),
+    "runs_row_tiles_64": (2, 75, 1, 2, 64, 64, [30000, 26001], [1, 2], True, "fp16", "slots", [(0, 100)]),
     "exact_tiles": (2, 4, 4, 1, 128, 64, [1024, 640], None, True, "bf16", "heads", []),
 }
 
@@ -413,6 +418,30 @@ def test_two_graphs_and_an_eager_call_each_have_their_workspace():
         for (o, lse), (wo, wl) in zip([*outs, got], want):
             assert torch.equal(o, wo) and torch.equal(lse, wl)
     assert isinstance(s[0]["cache"], dbsp.PagedKVCache)
+
+
+def test_a_table_that_all_sequences_share():
+    import torch
+    import paper_2511_23113_amd as dbsp
+    rng = np.random.default_rng(11)
+    k, v = pool_of(6, 2, 16, 64, "bf16", rng, "heads")
+    t, table = table_of(1, 5, 6, [75], 16, rng)
+    filled(k, v, t, [75], rng)
+    q = torch.from_numpy(rng.normal(size=(3, 4, 1, 64))).bfloat16().cuda()
+    lens = [75, 20, 60]
+    o, lse = dbsp.paged_attn_fwd(dbsp.PagedKVCache(k, v, table.expand(3, -1), torch.tensor(lens, dtype=torch.int32, device="cuda")), q)
+    check_attn(host(o), host(lse), q, k, v, np.repeat(t, 3, 0), lens, [1, 1, 1], True, "bf16", 64 ** -0.5)
+
+
+def test_tensors_of_another_device_than_the_current_one(monkeypatch):
+    import torch
+    import paper_2511_23113_amd as dbsp
+    s = generator(2, 4, 2, 64, 16, 4)
+    q = s["rand"](2, 4, 1, 64)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    for call in (lambda: s["step"](), lambda: dbsp.paged_attn_fwd(s["cache"], q), lambda: dbsp.qk_norm_rope_fwd(q), lambda: dbsp.qk_norm_rope_bwd(q, None, q, None)):
+        with pytest.raises(ValueError, match="another device"):
+            call()
 
 
 def test_other_streams():

@@ -306,6 +306,36 @@ def test_zero_rows_and_large_ones():
     np.testing.assert_allclose((host(got)[0, 0, 1] ** 2).sum(), 64, rtol=64 * 2.0 ** -11)
 
 
+def test_large_tensors_are_their_pieces():
+    # 40 + 40 heads of 14,001 tokens (573 MB in and out, past the caches) against thirds of them, which go through the caches: the same bits
+    import torch
+    import paper_2511_23113_amd as dbsp
+    N, d = 14001, 128
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(1, N, 80, d, device="cuda", generator=g).bfloat16()
+    dy = torch.randn(1, 80, N, d, device="cuda", generator=g).bfloat16()
+    norm = dbsp.HeadNorm(*(1 + 0.1 * torch.randn(2, d, device="cuda", generator=g)))
+    rotary = dbsp.Rotary((22, 21, 21))
+    pos = torch.randint(0, 100, (N, 3), device="cuda", generator=g, dtype=torch.int32)
+
+    def both(a, b):
+        q, k = x[:, a:b, :40].transpose(1, 2), x[:, a:b, 40:].transpose(1, 2)
+        more = dict(norm=norm, rotary=rotary, positions=pos[a:b])
+        return (*dbsp.qk_norm_rope_fwd(q, k, **more), *dbsp.qk_norm_rope_bwd(q, k, dy[:, :40, a:b], dy[:, 40:, a:b], **more))
+    whole, third = both(0, N), N // 3
+    sums = {"q_gain": 0, "k_gain": 0}
+    for a in range(0, N, third):
+        part = both(a, a + third)
+        for i in range(4):
+            assert torch.equal(whole[i][:, :, a:a + third], part[i])
+        for name in sums:
+            sums[name] = sums[name] + part[4][name].double()
+    # sums of 560,040 terms |dn xh| of 0.64 on average: two tiles of 40 heads a lane, 2 + 4 additions of lanes and waves, 8 + 6 of the 512
+    # workgroups' sums, less than 128 in all for a term on either side
+    for name in sums:
+        assert float((whole[4][name].double() - sums[name]).abs().max()) <= 2 * 128 * U * 560040 * 0.8
+
+
 def test_strides_past_32_bits():
     import torch
     import paper_2511_23113_amd as dbsp
