@@ -54,7 +54,8 @@ struct Run {
   int len, q_len;        // of the sequence
 };
 
-// Every wave works it out for itself, 64 sequences at a time, a sequence a lane.
+// Every wave works it out for itself: sums over blocks of 64 sequences, a block a lane (of more than 4096 sequences some multiple of 64), and then
+// the sequences of the block that has the run, a sequence a lane.
 __device__ __forceinline__ Run find_run(const dbsp_paged_attn_params& p) {
   const int l = threadIdx.x & 63, unit = p.Hk * p.row_tiles;
   Run run;
@@ -65,13 +66,15 @@ __device__ __forceinline__ Run find_run(const dbsp_paged_attn_params& p) {
     run.n = (int)((blockIdx.x & 7) * per + i);
     return i < per && (unsigned)run.n < count;
   };
-  if (p.whole) {         // a row tile a workgroup
-    if (!take((unsigned)p.B * (unsigned)unit)) return run;
+  auto alone = [&] {       // a row tile a workgroup
     run.b = (int)((unsigned)run.n / (unsigned)unit);
     run.pair = run.n - run.b * unit;
     run.len = paged_len(p, run.b);
     run.q_len = paged_q_len(p, run.b);
     run.left = listed_tiles(run.len, run.q_len);
+  };
+  if (p.whole) {
+    if (take((unsigned)p.B * (unsigned)unit)) alone();
     return run;
   }
   // (lengths and new tokens are asked for at once: lanes without a sequence ask for the last one's, so that no branch stands between)
@@ -82,70 +85,92 @@ __device__ __forceinline__ Run find_run(const dbsp_paged_attn_params& p) {
     q_len = p.q_lens ? max(0, min(q_as_given, p.Nq)) : p.Nq;
     return b < p.B ? listed_tiles(len, q_len) : 0;
   };
-  int len0, q_len0;
-  const int tiles0 = get(l, len0, q_len0), upto0 = scan_wave(tiles0);
-  int all = __builtin_amdgcn_readlane(upto0, 63);
-  for (int b0 = 64; b0 < p.B; b0 += 64) {
-    int len, q_len;
-    all += __builtin_amdgcn_readlane(scan_wave(get(b0 + l, len, q_len)), 63);
-  }
-  const unsigned total = (unsigned)all * (unsigned)unit;
-  const bool parts = total < kPagedLong * max(p.runs, (unsigned)p.B * (unsigned)unit);
+  const int chunks = (p.B + 63) / 64, per_block = (chunks + 63) / 64;
+  int len, q_len, tiles = get(l, len, q_len);
+  // f(first sequence of 64, this lane's tiles), eight loads under way at a time
+  auto over_chunks = [&](auto f) __attribute__((always_inline)) {
+    f(0, tiles);
+    for (int c0 = 1; c0 < chunks; c0 += 8) {
+      int x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        int no_len, no_q_len;
+        x[u] = get((c0 + u) * 64 + l, no_len, no_q_len);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) f(c0 + u, x[u]);
+    }
+  };
+  int sum = 0, longest = 0;
+  over_chunks([&](int, int tiles) {
+    sum += tiles;
+    longest = max(longest, tiles);
+  });
+  const unsigned total = (unsigned)__builtin_amdgcn_readlane(scan_wave(sum), 63) * (unsigned)unit, row_tiles = (unsigned)p.B * (unsigned)unit;
+  const bool parts = total < kPagedLong * max(p.runs, row_tiles);
   // (of few tiles up to four a part as long as there are 256 of them, as every part costs the merge)
   const unsigned chunk = parts ? max(max(1u, min(4u, total / 256)), (total + kPagedParts - 1) / kPagedParts) : (total + p.runs - 1) / p.runs;
-  auto parts_of = [&](int tiles) { return (int)((tiles + chunk - 1) / chunk); };
-  const int mine0 = parts ? parts_of(tiles0) : tiles0, mine_upto0 = parts ? scan_wave(mine0) : upto0;
-  unsigned count = (unsigned)__builtin_amdgcn_readlane(mine_upto0, 63);
-  if (parts) {
-    for (int b0 = 64; b0 < p.B; b0 += 64) {
-      int len, q_len;
-      count += (unsigned)__builtin_amdgcn_readlane(scan_wave(parts_of(get(b0 + l, len, q_len))), 63);
-    }
-    count *= (unsigned)unit;
-  } else {
-    count = (total + chunk - 1) / chunk;
+  // no row tile is cut where that leaves a workgroup four tiles more than a part at most, or ten in all: 512 pairs of 4 to 9 tiles 33.4 us cut
+  // down to 7, 23.8 uncut
+  if (parts && __builtin_amdgcn_ballot_w64(longest > max(kPagedWhole, (int)chunk + 4)) == 0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.table[1] = 2;
+    if (take(row_tiles)) alone();
+    return run;
   }
-  if (!take(count)) return run;
-  // Runs: where in one KV head's tiles this one begins.  Parts: which it is, counted alike.
-  const unsigned from = parts ? (unsigned)run.n : run.n * chunk, where = from / (unsigned)unit;
-  const bool writes = blockIdx.x == 0 && threadIdx.x < 64;
-  if (writes && l == 0) {
-    p.table[0] = (int)chunk;
-    p.table[1] = parts;
-  }
-  unsigned before = 0;
-  bool found = false;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    int len = len0, q_len = q_len0, tiles = tiles0, mine = mine0, upto = mine_upto0;
-    if (b0 > 0) {
-      tiles = get(b0 + l, len, q_len);
-      mine = parts ? parts_of(tiles) : tiles;
-      upto = scan_wave(mine);
+  // what is counted: parts, or tiles of one KV head
+  auto counted = [&](int tiles) { return parts ? (int)((tiles + chunk - 1) / chunk) : tiles; };
+  int mine = 0;            // of block l
+  over_chunks([&](int c, int tiles) {
+    const int sum = __builtin_amdgcn_readlane(scan_wave(counted(tiles)), 63);
+    mine += l == c / per_block ? sum : 0;
+  });
+  int upto = scan_wave(mine);
+  if (!take(parts ? (unsigned)__builtin_amdgcn_readlane(upto, 63) * (unsigned)unit : (total + chunk - 1) / chunk)) return run;
+  if (blockIdx.x == 0 && threadIdx.x < 64) {      // for the merge
+    if (l == 0) {
+      p.table[0] = (int)chunk;
+      p.table[1] = parts;
     }
-    if (writes && b0 + l < p.B) {          // for the merge
-      p.table[2 + 2 * (b0 + l)] = (int)before + upto - mine;
-      p.table[3 + 2 * (b0 + l)] = tiles;
-    }
-    const uint64_t behind = __builtin_amdgcn_ballot_w64(where < before + upto);
-    if (!found && behind) {
-      const int at = __builtin_ctzll(behind), n = __builtin_amdgcn_readlane(mine, at), of = __builtin_amdgcn_readlane(tiles, at);
-      const unsigned in = from - (before + (unsigned)(__builtin_amdgcn_readlane(upto, at) - n)) * unit;
-      found = true;
-      run.b = b0 + at;
-      run.pair = (int)(in / (unsigned)n);
-      run.t = (int)(in - run.pair * n);
-      run.left = (int)min(chunk, total - from);
-      if (parts) {         // part run.t of n, of equally many tiles
-        const int per = (int)((unsigned)(of + n - 1) / (unsigned)n);
-        run.t = min(run.t * per, of);
-        run.left = min(per, of - run.t);
+    int before = 0;
+    for (int c = 0; c < chunks; ++c) {
+      int x, y;
+      const int b = c * 64 + l, n = c == 0 ? tiles : get(b, x, y), here = counted(n), here_upto = scan_wave(here);
+      if (b < p.B) {
+        p.table[2 + 2 * b] = before + here_upto - here;
+        p.table[3 + 2 * b] = n;
       }
-      run.len = __builtin_amdgcn_readlane(len, at);
-      run.q_len = __builtin_amdgcn_readlane(q_len, at);
+      before += __builtin_amdgcn_readlane(here_upto, 63);
     }
-    if (found && !writes) break;
-    before += __builtin_amdgcn_readlane(upto, 63);
   }
+  const unsigned from = parts ? (unsigned)run.n : run.n * chunk, where = from / (unsigned)unit;
+  int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(where < (unsigned)upto));
+  unsigned before = (unsigned)(__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
+  const int b0 = at * per_block * 64;
+  for (int i0 = 0; i0 < per_block * 64; i0 += 64) {
+    if (b0 + i0 > 0) tiles = get(b0 + i0 + l, len, q_len);
+    mine = counted(tiles);
+    upto = scan_wave(mine);
+    const uint64_t behind = __builtin_amdgcn_ballot_w64(where < before + upto);
+    if (behind) {
+      at = __builtin_ctzll(behind);
+      run.b = b0 + i0 + at;
+      before += (unsigned)(__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
+      break;
+    }
+    before += (unsigned)__builtin_amdgcn_readlane(upto, 63);
+  }
+  const int n = __builtin_amdgcn_readlane(mine, at), of = __builtin_amdgcn_readlane(tiles, at);
+  const unsigned in = from - before * unit;
+  run.pair = (int)(in / (unsigned)n);
+  run.t = (int)(in - run.pair * n);
+  run.left = (int)min(chunk, total - from);
+  if (parts) {             // part run.t of n, of equally many tiles
+    const int per = (int)((unsigned)(of + n - 1) / (unsigned)n);
+    run.t = min(run.t * per, of);
+    run.left = min(per, of - run.t);
+  }
+  run.len = __builtin_amdgcn_readlane(len, at);
+  run.q_len = __builtin_amdgcn_readlane(q_len, at);
   return run;
 }
 
@@ -422,6 +447,7 @@ __global__ __launch_bounds__(256) void dbsp_paged_merge_kernel(const dbsp_paged_
   const int32_t* const q_lens = p.q_lens ? p.q_lens : p.lens;
   const unsigned chunk = (unsigned)p.table[0], parts = (unsigned)p.table[1], before = (unsigned)p.table[2 + 2 * b], tiles = (unsigned)p.table[3 + 2 * b];
   const int q_as_given = q_lens[b];
+  if (parts == 2) return;                  // no row tile was cut
   const int row = t * p.G + h - hk * p.G, rt = row / tile_rows;
   // the runs that the row tile lies in, or its parts
   const unsigned unit = (unsigned)(p.Hk * p.row_tiles), pair = (unsigned)(hk * p.row_tiles + rt);

@@ -47,7 +47,7 @@ struct dbsp_paged_attn_params {
   int32_t row_tiles, own_rows;         // of a (sequence, KV head); rows of a partial result
   float scale_log2;                    // softmax scale * log2(e)
   // workspace
-  int32_t* table;                      // [2 + 2 B] tiles of a run; of every sequence tiles before it, and its own
+  int32_t* table;                      // [2 + 2 B] tiles of a run or part, and which (1: parts, 2: nothing is cut); of every sequence what is before it, and its tiles
   float *part_o, *part_lse;            // f32 [parts][own_rows][d], [parts][own_rows] (base 2)
   int32_t merge_groups, merge_ways;    // workgroups of the merge, and how many of a row's parts it takes at a time, eight each
 };
