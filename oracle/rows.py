@@ -86,14 +86,16 @@ def paged_attention(q, pool_k, pool_v, pages, lens, q_lens, causal, scale):
     seen = np.zeros((B, H, Nq), dtype=np.int64)
     for b in range(B):
         n, new = int(lens[b]), int(q_lens[b])
-        places = [slot_place(pages[b], slot, page_size, n_pages) for slot in range(n)]
+        slots = np.arange(n)
+        page = np.asarray(pages[b], dtype=np.int64)[slots // page_size]
+        there = (page >= 0) & (page < n_pages)
         for t in range(new):
-            here = [at for at in places[:seen_slots(n, new, t, causal)] if at is not None]
-            at, off = np.array([x[0] for x in here], dtype=int), np.array([x[1] for x in here], dtype=int)
+            here = slots[there & (slots < seen_slots(n, new, t, causal))]
+            at, off = page[here], here % page_size
             for h in range(H):
                 hk = h // (H // Hk)
                 seen[b, h, t] = len(here)
-                if not here:
+                if not len(here):
                     O[b, h, t], A[b, h, t], LSE[b, h, t] = 0.0, 0.0, -np.inf
                     continue
                 K, V = pool_k[at, hk, off].astype(np.float64), pool_v[at, hk, off].astype(np.float64)

@@ -142,6 +142,23 @@ def test_attention(name):
         check_attn(host(o), host(lse), q, k, v, t, lens, [Nq] * B, causal, dtype, 0.03)
 
 
+@pytest.mark.parametrize("lo, hi", [(0, 40), (500, 700)])
+def test_thousands_of_sequences(lo, hi):
+    # more than 64 blocks of 64 sequences: short ones with a few long ones among them, whose row tiles are cut into parts, and longer ones, in runs
+    import torch
+    import paper_2511_23113_amd as dbsp
+    rng = np.random.default_rng(12)
+    B, H, d, page, n_pages, per = 4230, 2, 64, 16, 200, 100
+    k, v = (torch.from_numpy(rng.normal(size=(n_pages, 1, page, d))).half().cuda() for _ in range(2))
+    table = rng.integers(-1, n_pages, size=(B, per)).astype(np.int32)
+    lens = rng.integers(lo, hi, size=B)
+    lens[rng.integers(0, B, 20)] = 1600
+    q = torch.from_numpy(rng.normal(size=(B, H, 1, d))).half().cuda()
+    cache = dbsp.PagedKVCache(k, v, torch.from_numpy(table).cuda(), torch.from_numpy(lens.astype(np.int32)).cuda())
+    o, lse = dbsp.paged_attn_fwd(cache, q)
+    check_attn(host(o), host(lse), q, k, v, table, lens, [1] * B, True, "fp16", d ** -0.5)
+
+
 def test_the_order_of_pages_changes_no_bit():
     import torch
     import paper_2511_23113_amd as dbsp
