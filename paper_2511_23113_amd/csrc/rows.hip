@@ -8,6 +8,11 @@
 // row are data-parallel primitives inside 16 lanes.  A workgroup takes 16 (d = 64: 32) tokens and goes over its heads, so an
 // angle's cosine and sine are formed once for all of them.  Angles are formed in 64 bits, in turns, and only what is left of whole
 // turns is rounded to f32.
+//
+// Bound by reading and writing once: 40 + 40 heads of 128 of 32,760 tokens (1342 MB) 263 us, 5.1 TB/s, where a large copy reaches 5.0; their
+// gradients at 17,550 tokens (1078 MB) 209 us and 4.7 for the sums of gains.  Smaller ones by a workgroup's first loads (lengths and
+// positions, then rows) and by what comes before its first row, some 200 instructions: 12,303 tokens of 30 + 10 heads of 64 (126 MB) 30 us,
+// 4.2 TB/s, where one head a workgroup takes 57.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
