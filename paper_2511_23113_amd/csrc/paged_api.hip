@@ -46,8 +46,8 @@ int lay_out(const char* who, const dbsp_paged_cache* c, int32_t H, int32_t Nq, C
   if (all * tiles > kMost) return fail(who, DBSP_ESHAPE, "the cache is too large for so many sequences, heads and queries");
   p.whole = tiles <= kPagedWhole;
   p.runs = paged_runs(rows, c->d);
-  // runs, or parts: at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kPagedParts of them
-  cut.grid = round_up(p.whole ? all : std::max<int64_t>(std::min<int64_t>(p.runs, all * tiles), std::min(all * tiles, (int64_t)kPagedParts + all)), 8);
+  // runs, or parts: at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kPagedRuns of them
+  cut.grid = round_up(p.whole ? all : std::min(all * tiles, (int64_t)kPagedRuns + all), 8);
   // parts of a row on average, if all sequences are as long; a merge workgroup has 1024 / d of them in hand at a time, eight of a row each
   int ways = 1;
   while (ways < 8 && 8 * ways * all < p.runs) ways *= 2;

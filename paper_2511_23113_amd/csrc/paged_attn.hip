@@ -111,9 +111,12 @@ __device__ __forceinline__ Run find_run(const dbsp_paged_attn_params& p) {
     longest = max(longest, tiles);
   });
   const unsigned total = (unsigned)__builtin_amdgcn_readlane(scan_wave(sum), 63) * (unsigned)unit, row_tiles = (unsigned)p.B * (unsigned)unit;
-  const bool parts = total < kPagedLong * max(p.runs, row_tiles);
-  // (of few tiles up to four a part as long as there are 256 of them, as every part costs the merge)
-  const unsigned chunk = parts ? max(max(1u, min(4u, total / 256)), (total + kPagedParts - 1) / kPagedParts) : (total + p.runs - 1) / p.runs;
+  const bool parts = total < max(8 * kPagedRuns, kPagedLong * row_tiles);
+  const unsigned runs = total < kPagedEnds * row_tiles ? kPagedRuns : p.runs;
+  // (of few tiles up to four a part as long as there are 256 of them, as every part costs the merge; of many row tiles fewer parts, as each
+  // has one that is not full: 128 pairs of 9 to 18 tiles 19.3 / 17.7 us)
+  const unsigned full = kPagedRuns - min(row_tiles / 2, kPagedRuns / 2);
+  const unsigned chunk = parts ? max(max(1u, min(4u, total / 256)), (total + full - 1) / full) : (total + runs - 1) / runs;
   // no row tile is cut where that leaves a workgroup four tiles more than a part at most, or ten in all: 512 pairs of 4 to 9 tiles 33.4 us cut
   // down to 7, 23.8 uncut
   if (parts && __builtin_amdgcn_ballot_w64(longest > max(kPagedWhole, (int)chunk + 4)) == 0) {

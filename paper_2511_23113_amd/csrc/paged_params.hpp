@@ -20,14 +20,16 @@ inline void paged_divisor(int page_size, uint32_t& mul, uint32_t& shift) {
 }
 __host__ __device__ inline int paged_quotient(int slot, uint32_t mul, uint32_t shift) { return (int)(((uint64_t)(uint32_t)slot * mul) >> shift); }
 
-// The list of tiles is cut into runs if these and the row tiles have at least kPagedLong tiles each on average, else row tiles are cut into parts
-// for themselves: kPagedParts in all, and one more a row tile at most.  us, runs / parts: 256 (sequence, KV head) pairs of 41 tiles 67.4 / 72,
-// 8 of 1650 tiles 83 / 87, 128 of 18 21.7 / 25; but at d = 64 2048 pairs of 6 tiles 52.4 / 49.7, 240 of 12 with 21 rows each 24.3 / 18
-// (parts: 1024 of them 20.5).
-constexpr unsigned kPagedLong = 8, kPagedParts = 512;
-// Runs: two workgroups a compute unit, or one where it draws as much from memory (single tokens at d = 128).  us, one / two: 256 pairs of 41
-// tiles 67.4 / 68.9, 256 of 58 89.4 / 91.2, 1600 of 23 207 / 210; at d = 64 256 of 83 69.1 / 67.0, and 240 of 12 with 21 rows each 43.4 / 29.2.
-constexpr unsigned paged_runs(int64_t rows, int d) { return d == 128 && rows <= 16 ? 256 : 512; }
+// The list of tiles is cut into runs if row tiles have at least kPagedLong tiles each on average and 512 runs would have eight, else row tiles are
+// cut into parts for themselves, kPagedRuns in all, and one more a row tile at most.  us, runs / parts: 256 (sequence, KV head) pairs of 41 tiles 67.4 / 72,
+// 8 of 1650 83 / 87, 400 of 13 42.4 / 45; but 512 of 9 37.5 / 35.1, and at d = 64 2048 of 6 52.4 / 45.7, 240 of 12 with 21 rows each 24.3 / 18.
+constexpr unsigned kPagedLong = 12, kPagedRuns = 512;
+// Runs: two workgroups a compute unit, or one where it draws as much from memory, that is for single tokens at d = 128 over row tiles of
+// kPagedEnds tiles and more on average (at a row tile's end nothing else runs on the compute unit).  us, one / two: 256 pairs of 41 tiles
+// 67.4 / 68.9, 64 of 258 89.4 / 91.2, 64 of 62 31.1 / 32.1, 1024 of 20 134.5 / 137; but 512 of 14 54.3 / 51.9, 240 of 13 30.4 / 27.6, 400 of 13
+// 43.3 / 42.4; at d = 64 256 of 83 69.1 / 67.0, and 240 of 12 with 21 rows each 43.4 / 29.2.
+constexpr unsigned kPagedEnds = 20;
+constexpr unsigned paged_runs(int64_t rows, int d) { return d == 128 && rows <= 16 ? kPagedRuns / 2 : kPagedRuns; }
 
 struct dbsp_paged_attn_params {
   const uint16_t* q;
