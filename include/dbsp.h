@@ -308,7 +308,7 @@ int dbsp_cache_evict_workspace(const dbsp_cache* cache, int32_t budget, int64_t*
  *   rotation:  pair p (of R = sum of pairs[]; the first pairs[0] belong to axis 0, and so on) has the angle
  *              a = position[its axis] * freqs[p], and (n1, n2) becomes (n1 cos a - n2 sin a, n1 sin a + n2 cos a).  Its places are
  *              (2p, 2p + 1), or with `halves` (p, p + R).  Places from 2R on keep n.
- * Norms and rotations are f32, angles 64 bits (off by 2^-51 |position freq| and 2^-22 at most); the result is rounded once.
+ * Norms and rotations are f32, angles 64 bits (off by 2^-51 |position freq| and, with sine and cosine, 2^-21 at most); the result is rounded once.
  */
 enum { DBSP_NORM_NONE = 0, DBSP_NORM_RMS = 1, DBSP_NORM_LAYER = 2 };
 typedef struct dbsp_head_norm {

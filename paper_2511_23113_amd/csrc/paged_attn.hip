@@ -8,7 +8,8 @@
 // (d = 64: 64), one token's most often.  The tiles of 64 keys of all row tiles, one sequence and KV head behind the other, are one list, of which
 // every workgroup has a run of equally many: as many workgroups as the chip holds at a time begin and end together, whatever the
 // lengths, which are known on the device only.  A row tile that lies in one run is written as it is; the others leave a partial result for
-// every run, which a second launch joins: LSE = log sum exp LSE_i, O = sum exp(LSE_i - LSE) O_i.
+// every run, which a second launch joins: LSE = log sum exp LSE_i, O = sum exp(LSE_i - LSE) O_i.  Where there is little to read, or row tiles are
+// short, they are cut into parts for themselves or not at all (see kPagedLong).
 //
 // A workgroup is four waves, which share the rows and have 16 keys of a tile each: a wave copies them into the LDS directly and reads nothing that
 // another has copied, so no barrier couples the waves; their statistics are joined through the LDS at the end.  The pages of a tile's

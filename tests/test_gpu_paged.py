@@ -331,6 +331,22 @@ def test_shared_pages_and_the_same_page_twice():
         assert any(torch.equal(k[4, h, 8], x[b, h, 0]) for b in range(2)) and any(torch.equal(v[4, h, 8], x[b, h, 0]) for b in range(2))
 
 
+@pytest.mark.parametrize("halves", [False, True])
+def test_queries_in_place(halves):
+    import torch
+    import paper_2511_23113_amd as dbsp
+    s = generator(3, 7, 2, 128, 16, 8)
+    s["lens"].copy_(torch.tensor([100, 5, 30]))
+    x = s["rand"](3, 5, 11, 128)
+    q, k, v = (x[:, :, a:b].transpose(1, 2) for a, b in ((0, 7), (7, 9), (9, 11)))
+    new = torch.tensor([5, 2, 0], dtype=torch.int32, device="cuda")
+    more = dict(new_lens=new, norm=s["norm"], rotary=dbsp.Rotary((20, 12), halves=halves), positions=torch.randint(0, 99, (3, 5, 2), device="cuda", dtype=torch.int32))
+    want = dbsp.paged_append(s["cache"], k, v, q=q, q_out=q.clone(), **more)
+    pools = s["k"].clone(), s["v"].clone()
+    assert dbsp.paged_append(s["cache"], k, v, q=q, q_out=q, **more) is q
+    assert torch.equal(q, want) and torch.equal(s["k"], pools[0]) and torch.equal(s["v"], pools[1])
+
+
 def generator(B, H, Hk, d, page, per, seed=10):
     """A program that generates token by token: what it has in hand, and a step."""
     import torch
