@@ -415,7 +415,7 @@ int dbsp_paged_append(const dbsp_paged_cache* cache, const dbsp_qk_rows* rows, c
  * dbsp_paged_attn_fwd -- attention of each sequence's Nq newest tokens over its pages:
  *   s = softmax_scale q.k,  LSE = ln(sum exp(s)),  O = sum exp(s - LSE) v,
  * the sums over the slots j < lens[b] whose page is there, and with `causal` for query t only j <= lens[b] - q_lens[b] + t.  Made for one token or
- * a few: K and V are read once for every 32 rows Nq G of a KV head (64 at d = 64).
+ * a few: K and V are read once for every 64 rows Nq G of a KV head.
  *
  * q, o, lse, q_lens, H, Nq, causal, softmax_scale, stream: as for dbsp_cache_attn_fwd, with the same limits: K and V are finite in
  *      every used slot whose page is there; nothing else of the pool is read.

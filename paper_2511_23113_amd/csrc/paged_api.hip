@@ -45,6 +45,7 @@ int lay_out(const char* who, const dbsp_paged_cache* c, int32_t H, int32_t Nq, C
   p.own_rows = (int32_t)std::min<int64_t>(rows, tile_rows);
   if (all * tiles > kMost) return fail(who, DBSP_ESHAPE, "the cache is too large for so many sequences, heads and queries");
   p.whole = tiles <= kPagedWhole;
+  p.slots = paged_slots(rows, c->d);
   p.runs = paged_runs(rows, c->d);
   // runs, or parts: at most 1 / chunk of the tiles and one a row tile, with chunk at least 1 and 1 / kPagedRuns of them
   cut.grid = round_up(p.whole ? all : std::min(all * tiles, (int64_t)kPagedRuns + all), 8);

@@ -4,8 +4,8 @@
 //   s = scale q.k,  LSE = ln sum exp(s),  O = sum exp(s - LSE) v,
 // in one pass with a running max and sum, and O = 0, LSE = -inf without a key.
 //
-// Rows and runs.  The G heads of a group read the same keys: a row is a (token, head of the group) pair, and a row tile has up to 32 of them
-// (d = 64: 64), one token's most often.  The tiles of 64 keys of all row tiles, one sequence and KV head behind the other, are one list, of which
+// Rows and runs.  The G heads of a group read the same keys: a row is a (token, head of the group) pair, and a row tile has up to 64 of them,
+// one token's most often.  The tiles of 64 keys of all row tiles, one sequence and KV head behind the other, are one list, of which
 // every workgroup has a run of equally many: as many workgroups as the chip holds at a time begin and end together, whatever the
 // lengths, which are known on the device only.  A row tile that lies in one run is written as it is; the others leave a partial result for
 // every run, which a second launch joins: LSE = log sum exp LSE_i, O = sum exp(LSE_i - LSE) O_i.  Where there is little to read, or row tiles are
@@ -112,11 +112,11 @@ __device__ __forceinline__ Run find_run(const dbsp_paged_attn_params& p) {
     longest = max(longest, tiles);
   });
   const unsigned total = (unsigned)__builtin_amdgcn_readlane(scan_wave(sum), 63) * (unsigned)unit, row_tiles = (unsigned)p.B * (unsigned)unit;
-  const bool parts = total < max(8 * kPagedRuns, kPagedLong * row_tiles);
-  const unsigned runs = total < kPagedEnds * row_tiles ? kPagedRuns : p.runs;
+  const bool parts = total < max(8 * p.slots, kPagedLong * row_tiles);
+  const unsigned runs = total < kPagedEnds * row_tiles ? p.slots : p.runs;
   // (of few tiles up to four a part as long as there are 256 of them, as every part costs the merge; of many row tiles fewer parts, as each
   // has one that is not full: 128 pairs of 9 to 18 tiles 19.3 / 17.7 us)
-  const unsigned full = kPagedRuns - min(row_tiles / 2, kPagedRuns / 2);
+  const unsigned full = p.slots - min(row_tiles / 2, p.slots / 2);
   const unsigned chunk = parts ? max(max(1u, min(4u, total / 256)), (total + full - 1) / full) : (total + runs - 1) / runs;
   // no row tile is cut where that leaves a workgroup four tiles more than a part at most, or ten in all: 512 pairs of 4 to 9 tiles 33.4 us cut
   // down to 7, 23.8 uncut
@@ -198,7 +198,7 @@ __device__ __forceinline__ void to_next(const dbsp_paged_attn_params& p, int uni
 }
 
 template <class T, int D, int NR>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 && NR > 2 ? 1 : 2)))
 void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
   using L = Lay<D>;
   constexpr int KS = D / 32, DT = D / 16, CH = D / 4, ROWS = 16 * NR;
@@ -533,7 +533,8 @@ hipError_t launch(const dbsp_paged_attn_params& p, int grid, hipStream_t stream)
   const int tile_rows = paged_tile_rows((int64_t)p.Nq * p.G, D);
   if (tile_rows == 16) dbsp_paged_attn_kernel<T, D, 1><<<grid, 256, 0, stream>>>(p);
   else if (tile_rows == 32) dbsp_paged_attn_kernel<T, D, 2><<<grid, 256, 0, stream>>>(p);
-  else if constexpr (D == 64) dbsp_paged_attn_kernel<T, D, 4><<<grid, 256, 0, stream>>>(p);
+  else if (tile_rows == 48) dbsp_paged_attn_kernel<T, D, 3><<<grid, 256, 0, stream>>>(p);
+  else dbsp_paged_attn_kernel<T, D, 4><<<grid, 256, 0, stream>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.merge_groups == 0) return e;
   if (p.merge_ways == 1) dbsp_paged_merge_kernel<T, D, 1><<<p.merge_groups, 256, 0, stream>>>(p, tile_rows);

@@ -7,8 +7,9 @@
 
 constexpr int64_t kMostSlots = (int64_t)1 << 30;      // of a sequence, and less
 constexpr int kPagedKeys = 64;         // keys of a tile, 16 a wave
-// Rows of a row tile: 16, 32, or at d = 64 64, by how many there are (64 of d = 128 do not fit into the registers of two waves)
-constexpr int paged_tile_rows(int64_t rows, int d) { return rows <= 16 ? 16 : rows <= 32 || d == 128 ? 32 : 64; }
+// Rows of a row tile, by how many there are.  At d = 128 more than 32 take the registers of one wave a SIMD: 256 (sequence, KV head) pairs of 41 tiles
+// and 40 rows 89.6 us, with two row tiles of 32 116; 128 of them with 48 53.7, 64; 64 of 80 and 100 rows 79.4, 92; 40 of 78 and 64 rows 42.4, 43.2.
+constexpr int paged_tile_rows(int64_t rows, int d) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 ? 48 : 64; }
 constexpr int kPagedWhole = 10;        // tiles that a row tile may have at most where each goes to a workgroup of its own, without a merge
 
 // slot / page_size as slot * mul >> shift, for slots below 2^31: with 2^s >= page_size, mul = 2^(31 + s) / page_size rounded up is too large by
@@ -28,8 +29,10 @@ constexpr unsigned kPagedLong = 12, kPagedRuns = 512;
 // kPagedEnds tiles and more on average (at a row tile's end nothing else runs on the compute unit).  us, one / two: 256 pairs of 41 tiles
 // 67.4 / 68.9, 64 of 258 89.4 / 91.2, 64 of 62 31.1 / 32.1, 1024 of 20 134.5 / 137; but 512 of 14 54.3 / 51.9, 240 of 13 30.4 / 27.6, 400 of 13
 // 43.3 / 42.4; at d = 64 256 of 83 69.1 / 67.0, and 240 of 12 with 21 rows each 43.4 / 29.2.
+// And 256 where only one fits: more than 32 rows at d = 128 (with 512 for two rounds 95.2 us where 256 take 89.6, and 29.3 where they take 21.7).
 constexpr unsigned kPagedEnds = 20;
-constexpr unsigned paged_runs(int64_t rows, int d) { return d == 128 && rows <= 16 ? kPagedRuns / 2 : kPagedRuns; }
+constexpr unsigned paged_slots(int64_t rows, int d) { return d == 128 && rows > 32 ? kPagedRuns / 2 : kPagedRuns; }
+constexpr unsigned paged_runs(int64_t rows, int d) { return d == 128 && rows <= 16 ? kPagedRuns / 2 : paged_slots(rows, d); }
 
 struct dbsp_paged_attn_params {
   const uint16_t* q;
@@ -45,7 +48,7 @@ struct dbsp_paged_attn_params {
   uint32_t page_mul, page_shift;       // see paged_quotient
   int32_t causal, whole;
   int32_t page_16;                     // a page's slots are a multiple of a wave's 16
-  uint32_t runs;                       // that the list of tiles is cut into
+  uint32_t slots, runs;                // parts, or runs over short row tiles, that the list of tiles is cut into, and runs over long ones
   int32_t row_tiles, own_rows;         // of a (sequence, KV head); rows of a partial result
   float scale_log2;                    // softmax scale * log2(e)
   // workspace

@@ -95,6 +95,10 @@ ATTN = {
     "sixty_four_rows": (2, 64, 1, 1, 64, 32, [800, 1500], None, True, "fp16", "slots", []),
     "odd_rows": (1, 71, 1, 1, 64, 16, [1300], None, True, "bf16", "slots", [(0, 3)]),
     "odd_rows_128": (1, 71, 1, 1, 128, 16, [1300], None, True, "bf16", "slots", [(0, 3)]),
+    "forty_rows": (2, 16, 2, 5, 64, 16, [900, 70], [5, 3], True, "bf16", "heads", [(0, 30)]),
+    "forty_rows_128": (2, 16, 2, 5, 128, 24, [900, 70], [5, 3], True, "fp16", "slots", [(0, 30)]),
+    "forty_eight_rows_128": (1, 48, 1, 1, 128, 16, [700], None, True, "bf16", "heads", []),
+    "sixty_four_rows_128": (2, 32, 1, 2, 128, 16, [700, 1300], None, True, "bf16", "beside", [(1, 9)]),
     "drafts": (3, 6, 2, 7, 64, 24, [7, 333, 0], [7, 3, 0], True, "fp16", "heads", [(1, 2)]),
     "drafts_128": (3, 15, 3, 5, 128, 16, [900, 5, 64], [5, 4, 1], True, "bf16", "slots", []),
     "more_queries_than_keys": (2, 4, 2, 9, 64, 16, [4, 100], [9, 9], True, "bf16", "heads", []),
@@ -107,6 +111,7 @@ ATTN = {
     "runs": (70, 4, 2, 2, 128, 16, [(i * 613) % 6900 for i in range(70)], [i % 3 for i in range(70)], True, "bf16", "slots", [(1, 5), (9, 0), (33, 60)]),
     "runs_short_row_tiles": (100, 4, 4, 1, 128, 32, [(i * 371) % 2000 for i in range(100)], None, True, "bf16", "heads", [(7, 1), (50, 0)]),
     "runs_64": (70, 2, 2, 1, 64, 24, [(i * 1013) % 5000 for i in range(70)], None, True, "fp16", "heads", [(2, 3), (69, 0)]),
+    "runs_forty_rows": (3, 8, 1, 5, 128, 64, [46000, 44000, 47001], [5, 5, 4], True, "bf16", "heads", [(0, 100), (1, 0)]),
     "runs_row_tiles": (2, 65, 1, 1, 128, 64, [47000, 43000], None, True, "bf16", "heads", [(0, 100), (1, 0)]),
     "runs_row_tiles_64": (2, 65, 1, 2, 64, 64, [47000, 43001], [1, 2], True, "fp16", "slots", [(0, 100)]),
     "exact_tiles": (2, 4, 4, 1, 128, 64, [1024, 640], None, True, "bf16", "heads", []),
