@@ -123,7 +123,7 @@ int dbsp_qk_norm_rope_fwd(const dbsp_qk_rows* rows, const dbsp_head_norm* norm, 
     }
   }
   if ((rc = dbsp_rows_deal(who, p, rows->d, kRowGroups)) != DBSP_OK) return rc;
-  p.stream = tensor_bytes(p, rows->d) * 2 >= kRowStream;
+  p.stream = tensor_bytes(p, rows->d) * 2 >= kRowStream && row_lines_whole(halves, p.turned);
   return done(who, dbsp_launch_rows(p, rows->d, rows->dtype == DBSP_FP16, kind, halves, false, static_cast<hipStream_t>(stream)));
 }
 
@@ -175,7 +175,7 @@ int dbsp_qk_norm_rope_bwd(const dbsp_qk_rows* rows, const dbsp_heads* dq, const 
   if (grads && kind == DBSP_NORM_NONE) return fail(who, DBSP_EINVAL, "without a norm there are no gains to form gradients of");
   if (!aligned(grads, 16)) return fail(who, DBSP_EINVAL, "grads must be 16-byte aligned");
   if ((rc = dbsp_rows_deal(who, p, rows->d, kGradGroups)) != DBSP_OK) return rc;
-  p.stream = tensor_bytes(p, rows->d) * 3 >= kRowStream;
+  p.stream = tensor_bytes(p, rows->d) * 3 >= kRowStream && row_lines_whole(halves, p.turned);
   if (grads) {
     const int64_t need = grad_bytes(p, rows->d);
     if (!workspace) return fail(who, DBSP_EINVAL, "null pointer (workspace)");

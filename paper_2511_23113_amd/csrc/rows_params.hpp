@@ -13,6 +13,9 @@ constexpr int kGradGroups = 1024;      // those of the backward pass, which leav
 // read.  us, through / past them, and with a reader of the results behind it: 32,760 tokens of 40 + 40 heads of 128 (1342 MB) 265 / 253,
 // 483 / 474, 8000 tokens 68 / 63, 115 / 116, but 12,303 tokens of 30 + 10 heads of 64 (126 MB) 30.5 / 33.3, 52.6 / 59.7.
 constexpr int64_t kRowStream = (int64_t)512 << 20;
+// And if whole lines of 128 bytes are stored at a time, as pieces of lines are joined in the caches only: rotations by halves of 64 pairs, or none.
+// Halves of 32 pairs, 32,760 tokens of 80 + 40 heads of 64 215 / 238, gradients 178 / 192; of 64 pairs at d = 128 264 / 249, 224 / 214.
+constexpr bool row_lines_whole(bool halves, int turned) { return !halves || turned == 64; }
 
 // One of a launch's tensors: queries, keys, or (appended) values, whose heads are dealt to `groups` workgroups, `per` each.
 struct dbsp_rows_part {

@@ -306,8 +306,9 @@ def test_zero_rows_and_large_ones():
     np.testing.assert_allclose((host(got)[0, 0, 1] ** 2).sum(), 64, rtol=64 * 2.0 ** -11)
 
 
-def test_large_tensors_are_their_pieces():
-    # 40 + 40 heads of 14,001 tokens (573 MB in and out, past the caches) against thirds of them, which go through the caches: the same bits
+@pytest.mark.parametrize("pairs, halves", [((22, 21, 21), False), ((22, 21, 21), True), ((20, 21, 11), True)])
+def test_large_tensors_are_their_pieces(pairs, halves):
+    # 40 + 40 heads of 14,001 tokens (573 MB in and out, past the caches where lines are stored whole) against thirds of them, which go through the caches: the same bits
     import torch
     import paper_2511_23113_amd as dbsp
     N, d = 14001, 128
@@ -315,7 +316,7 @@ def test_large_tensors_are_their_pieces():
     x = torch.randn(1, N, 80, d, device="cuda", generator=g).bfloat16()
     dy = torch.randn(1, 80, N, d, device="cuda", generator=g).bfloat16()
     norm = dbsp.HeadNorm(*(1 + 0.1 * torch.randn(2, d, device="cuda", generator=g)))
-    rotary = dbsp.Rotary((22, 21, 21))
+    rotary = dbsp.Rotary(pairs, halves=halves)
     pos = torch.randint(0, 100, (N, 3), device="cuda", generator=g, dtype=torch.int32)
 
     def both(a, b):
