@@ -39,7 +39,7 @@ int lay_out(const char* who, const dbsp_paged_cache* c, int32_t H, int32_t Nq, C
   p.n_pages = c->n_pages; p.page_size = c->page_size; p.max_pages = c->max_pages; p.cap = c->max_pages * c->page_size;
   const int64_t rows = (int64_t)Nq * p.G, q_rows = (int64_t)p.B * H * Nq;
   if (rows > kMost || q_rows > kMost) return fail(who, DBSP_ESHAPE, "too many queries");
-  const int tile_rows = paged_tile_rows(rows, c->d);
+  const int tile_rows = paged_tile_rows(rows);
   const int64_t row_tiles = (rows + tile_rows - 1) / tile_rows, all = row_tiles * p.B * p.Hk, tiles = (p.cap + kPagedKeys - 1) / kPagedKeys;
   p.row_tiles = (int32_t)row_tiles;
   p.own_rows = (int32_t)std::min<int64_t>(rows, tile_rows);

@@ -530,7 +530,7 @@ __global__ __launch_bounds__(256) void dbsp_paged_merge_kernel(const dbsp_paged_
 
 template <class T, int D>
 hipError_t launch(const dbsp_paged_attn_params& p, int grid, hipStream_t stream) {
-  const int tile_rows = paged_tile_rows((int64_t)p.Nq * p.G, D);
+  const int tile_rows = paged_tile_rows((int64_t)p.Nq * p.G);
   if (tile_rows == 16) dbsp_paged_attn_kernel<T, D, 1><<<grid, 256, 0, stream>>>(p);
   else if (tile_rows == 32) dbsp_paged_attn_kernel<T, D, 2><<<grid, 256, 0, stream>>>(p);
   else if (tile_rows == 48) dbsp_paged_attn_kernel<T, D, 3><<<grid, 256, 0, stream>>>(p);

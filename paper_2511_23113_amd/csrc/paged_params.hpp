@@ -9,7 +9,7 @@ constexpr int64_t kMostSlots = (int64_t)1 << 30;      // of a sequence, and less
 constexpr int kPagedKeys = 64;         // keys of a tile, 16 a wave
 // Rows of a row tile, by how many there are.  At d = 128 more than 32 take the registers of one wave a SIMD: 256 (sequence, KV head) pairs of 41 tiles
 // and 40 rows 89.6 us, with two row tiles of 32 116; 128 of them with 48 53.7, 64; 64 of 80 and 100 rows 79.4, 92; 40 of 78 and 64 rows 42.4, 43.2.
-constexpr int paged_tile_rows(int64_t rows, int d) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 ? 48 : 64; }
+constexpr int paged_tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 ? 48 : 64; }
 constexpr int kPagedWhole = 10;        // tiles that a row tile may have at most where each goes to a workgroup of its own, without a merge
 
 // slot / page_size as slot * mul >> shift, for slots below 2^31: with 2^s >= page_size, mul = 2^(31 + s) / page_size rounded up is too large by
