@@ -17,7 +17,8 @@
 // 16 bytes: a page may end anywhere.  Slots without a key, behind the length or of a page that is not there, are copied from a row of
 // zeros, as what lies in their place could be infinite or a NaN.  Products are formed transposed, S^T = K Q^T and O^T = V^T P^T, with 16 x 16
 // MFMAs: lane (n, g) of 16 x 4 has row n and keys 4 g .. 4 g + 3, and the packed probabilities are the second product's operand as they lie.
-// Probabilities are rounded to the inputs' type for it, half a step of it relative to each; LSE's sums are of the f32 values.
+// For it each probability is the sum of two numbers of the inputs' type (see Halves), beside one another along the keys against V twice: an MFMA over
+// 32 products takes as long as one over 16.  LSE's sums, which O is divided by, are of the f32 values.
 //
 // Bound by reading K and V once: 32 sequences of 40 heads on 8 KV heads, 880 to 4400 keys each (347 MB on average) 65 us and 4.7 for the merge; two
 // sequences of some 111,000 keys and 4 KV heads (456 MB) 79 us, 5.8 TB/s, and 4.8.  Where there are few tiles a workgroup, by latencies: lengths,
@@ -197,6 +198,23 @@ __device__ __forceinline__ void to_next(const dbsp_paged_attn_params& p, int uni
   x.listed = listed_tiles(x.len, paged_q_len(p, x.b));
 }
 
+// Probabilities p >= 0 as sums of two numbers of 16 bits.  bf16 has f32's exponents: the sum is off by 2^-16 p at most, half a step of the second
+// number.  fp16 has steps of 2^-24: the sum is off by 2^-21 p, and by half such a step where that is more.
+template <class T> struct Halves;
+template <> struct Halves<Bf16> {
+  static __device__ __forceinline__ void split(float a, float b, uint32_t& x, uint32_t& rest) {
+    x = Bf16::pack(a, b);
+    rest = Bf16::pack(a - __builtin_bit_cast(float, x << 16), b - __builtin_bit_cast(float, x & 0xffff0000u));
+  }
+};
+template <> struct Halves<Fp16> {
+  static __device__ __forceinline__ void split(float a, float b, uint32_t& x, uint32_t& rest) {
+    const f16x2 cut = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(a, b));
+    x = __builtin_bit_cast(uint32_t, cut);
+    rest = Fp16::pack(a - (float)cut.x, b - (float)cut.y);
+  }
+};
+
 template <class T, int D, int NR>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 && NR > 2 ? 1 : 2)))
 void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
@@ -204,7 +222,7 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
   constexpr int KS = D / 32, DT = D / 16, CH = D / 4, ROWS = 16 * NR;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * L::TILE];      // [buffer][K, V]
   __shared__ int page_ids[4][2][64];
-  __shared__ float mcs[4][16], sums[4][16], rounds[4][16];
+  __shared__ float mcs[4][16], sums[4][16];
   const Run run = find_run(p);
   const int left = __builtin_amdgcn_readfirstlane(run.left), run_n = __builtin_amdgcn_readfirstlane(run.n), unit = p.Hk * p.row_tiles;
   if (left == 0) return;
@@ -240,7 +258,6 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) v_rd[dt] = mine + L::TILE + key * L::ROWB + (((2 * dt + (a4 >> 1)) ^ L::v_swz(key)) << 4) + (a4 & 1) * 8;
   }
-  const u32x2 ones = {T::pack(1.f, 1.f), T::pack(1.f, 1.f)};
   const float c = p.scale_log2;
   const int row_in = l / L::NCH, pch = l % L::NCH;
   const uint64_t zeros = (uint64_t)(uintptr_t)kZeros + (pch << 4);
@@ -286,9 +303,7 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
   int limit[NR], all_see, row0, hk;
   bool valid[NR];
   u32x4 q[NR][KS];
-  // rounded[y]: sums of the rounded probabilities, by one more MFMA against ones, all four alike.  O is divided by them, so that the
-  // rounding of a key that has most of its row's attention drops out; LSE is of `sum`.
-  f32x4 o[NR][DT], rounded[NR];
+  f32x4 o[NR][DT];
   float mc[NR], sum[NR];                   // the max starts at the lowest finite value: scores of -inf then have probability 0
   // the queries and limits of a row tile, and statistics of nothing yet
   auto begin = [&](const At& x) __attribute__((always_inline)) {
@@ -306,7 +321,6 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
       for (int ks = 0; ks < KS; ++ks) q[y][ks] = *reinterpret_cast<const u32x4*>(src + 32 * ks + 8 * g);
       mc[y] = -FLT_MAX;
       sum[y] = 0.f;
-      rounded[y] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[y][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -338,7 +352,8 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
     const uint32_t off = buf * 2 * L::TILE;
     const int key = at.t * kPagedKeys + 16 * w + 4 * g;
     u32x4 kf[KS];
-    u32x2 vf[DT], pb[NR];
+    u32x2 vf[DT];
+    u32x4 pb[NR];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) kf[ks] = *(LDS_PTR(u32x4))(uintptr_t)(k_rd[ks] + off);
 #pragma unroll
@@ -365,21 +380,21 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
         const float to = fmaxf(mc[y], top * c), f = __builtin_amdgcn_exp2f(mc[y] - to);
         mc[y] = to;
         sum[y] *= f;
-        rounded[y] *= f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[y][dt] *= f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -to));
       }
       sum[y] += (pr[0] + pr[1]) + (pr[2] + pr[3]);
-      pb[y] = u32x2{T::pack(pr[0], pr[1]), T::pack(pr[2], pr[3])};
+      uint32_t x01, x23, rest01, rest23;
+      Halves<T>::split(pr[0], pr[1], x01, rest01);
+      Halves<T>::split(pr[2], pr[3], x23, rest23);
+      pb[y] = u32x4{x01, x23, rest01, rest23};
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int y = 0; y < NR; ++y) o[y][dt] = T::mfma16(vf[dt], pb[y], o[y][dt]);
-#pragma unroll
-    for (int y = 0; y < NR; ++y) rounded[y] = T::mfma16(ones, pb[y], rounded[y]);
+      for (int y = 0; y < NR; ++y) o[y][dt] = T::mfma32(u32x4{vf[dt].x, vf[dt].y, vf[dt].x, vf[dt].y}, pb[y], o[y][dt]);
     there = there_next;
     if (j + 1 < left && next.t != 0) {
       at = next;
@@ -400,7 +415,6 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
       if (g == 0) {
         mcs[w][n] = mc[y];
         sums[w][n] = sum[y];
-        rounds[w][n] = rounded[y][0];
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) os[(w * 16 + n) * CH + ((4 * dt + g) ^ n)] = o[y][dt];
@@ -412,17 +426,16 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
         float m = mcs[0][in];
 #pragma unroll
         for (int x = 1; x < 4; ++x) m = fmaxf(m, mcs[x][in]);
-        float all = 0.f, all_rounded = 0.f;
+        float all = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const float f = __builtin_amdgcn_exp2f(mcs[x][in] - m);
           all += f * sums[x][in];
-          all_rounded += f * rounds[x][in];
           acc += f * os[(x * 16 + in) * CH + (ch ^ in)];
         }
         const bool none = __builtin_bit_cast(uint32_t, all) == 0u;      // (by its bits: NaNs are not regarded in this file)
-        acc *= none ? 0.f : 1.f / all_rounded;
+        acc *= none ? 0.f : 1.f / all;
         const float lse2 = none ? -INFINITY : m + __builtin_amdgcn_logf(all);
         if (part) {
           const int64_t pr = slot * p.own_rows + 16 * y + in;
