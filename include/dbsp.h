@@ -419,6 +419,8 @@ int dbsp_paged_append(const dbsp_paged_cache* cache, const dbsp_qk_rows* rows, c
  *
  * q, o, lse, q_lens, H, Nq, causal, softmax_scale, stream: as for dbsp_cache_attn_fwd, with the same limits: K and V are finite in
  *      every used slot whose page is there; nothing else of the pool is read.
+ *      O is rounded once.  Before that it is off by what scores are, by 2^-16 (bf16) or 2^-21 (fp16) of sum exp(s - LSE) |v|, and in fp16 by 2^-35 max |v|
+ *      for each key at most, as probabilities have no smaller parts there: half a step of O from 16 million keys on, if all the same way.
  * workspace: device, 256-byte aligned, of at least the size that dbsp_paged_attn_workspace gives for the same cache, H and Nq (NULL where that
  *      is 0); written by the call, holds nothing between calls.  Calls under way at the same time need one each.
  * The call only enqueues kernels, under capture too; lens, q_lens and pages are read on the device, so that a graph's replays follow what

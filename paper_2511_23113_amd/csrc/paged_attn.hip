@@ -198,17 +198,23 @@ __device__ __forceinline__ void to_next(const dbsp_paged_attn_params& p, int uni
   x.listed = listed_tiles(x.len, paged_q_len(p, x.b));
 }
 
-// Probabilities p >= 0 as sums of two numbers of 16 bits.  bf16 has f32's exponents: the sum is off by 2^-16 p at most, half a step of the second
-// number.  fp16 has steps of 2^-24: the sum is off by 2^-21 p, and by half such a step where that is more.
+// Probabilities p >= 0, times kScale, as sums of two numbers of 16 bits; and what they may be (kRaise) before the running max is raised.  bf16 has
+// f32's exponents: the sum is off by 2^-16 p at most, half a step of the second number.  fp16 has steps of 2^-24 and ends at 65504: the sum is off by
+// 2^-21 p, and by half such a step where that is more, which is 2^-35 of the largest p.  Without the scale keys 17.4 or more below the largest
+// score would be lost, however many they are.
 template <class T> struct Halves;
 template <> struct Halves<Bf16> {
+  static constexpr float kScale = 1.f, kRaise = kRaiseAt;
   static __device__ __forceinline__ void split(float a, float b, uint32_t& x, uint32_t& rest) {
     x = Bf16::pack(a, b);
     rest = Bf16::pack(a - __builtin_bit_cast(float, x << 16), b - __builtin_bit_cast(float, x & 0xffff0000u));
   }
 };
 template <> struct Halves<Fp16> {
+  static constexpr float kScale = 1024.f, kRaise = 32.f;
   static __device__ __forceinline__ void split(float a, float b, uint32_t& x, uint32_t& rest) {
+    a *= kScale;
+    b *= kScale;
     const f16x2 cut = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(a, b));
     x = __builtin_bit_cast(uint32_t, cut);
     rest = Fp16::pack(a - (float)cut.x, b - (float)cut.y);
@@ -373,7 +379,7 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -mc[y]));
       const float top4 = fmaxf(fmaxf(pr[0], pr[1]), fmaxf(pr[2], pr[3]));
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(top4 > kRaiseAt) != 0, 0)) {
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(top4 > Halves<T>::kRaise) != 0, 0)) {
         float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -435,7 +441,7 @@ void dbsp_paged_attn_kernel(const dbsp_paged_attn_params p) {
           acc += f * os[(x * 16 + in) * CH + (ch ^ in)];
         }
         const bool none = __builtin_bit_cast(uint32_t, all) == 0u;      // (by its bits: NaNs are not regarded in this file)
-        acc *= none ? 0.f : 1.f / all;
+        acc *= none ? 0.f : 1.f / Halves<T>::kScale / all;
         const float lse2 = none ? -INFINITY : m + __builtin_amdgcn_logf(all);
         if (part) {
           const int64_t pr = slot * p.own_rows + 16 * y + in;

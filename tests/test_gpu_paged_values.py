@@ -3,7 +3,8 @@
 Queries have one value that is not zero, so a score is one product and its error that of the few roundings behind it.  u = 2^-24.  A score of s is
 off by 3 u |s| (the scale, its product with log2 e, the argument) and by the exponential's unit, so a probability by 2 u (3 |s| + 2), relative
 and with its sum; as two numbers of the inputs' type by 2^-16 more in bf16 (half a step of each, 2^-8 2^-8) and 2^-21 in fp16 (a step of the first,
-2^-10, half a step of the second, 2^-11), or half of fp16's least step, as FLOOR says.  Sums over n keys: (n + 64) u in any order.  O is rounded once: h |O|."""
+2^-10, half a step of the second, 2^-11), or half of fp16's least step, 2^-25, where the largest
+probability is 2^10 (FLOOR).  Sums over n keys: (n + 64) u in any order.  O is rounded once: h |O|."""
 
 import numpy as np
 import pytest
@@ -15,7 +16,7 @@ from test_gpu_rows import host, torch_types
 pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
-FLOOR = {"bf16": 0.0, "fp16": 2.0 ** -25}      # of a probability, in terms of the largest one of the row
+FLOOR = {"bf16": 0.0, "fp16": 2.0 ** -35}      # of a probability, in terms of the largest one of the row
 
 
 def check(got, O, A, seen, s, dtype, top_v):
@@ -64,3 +65,27 @@ def test_o_is_rounded_once(name):
     O, _, A, seen = orows.paged_attention(hq, hk, hv, t, lens, [Nq] * B, False, 0.125)
     top_k, top_v = (np.abs(x[np.isfinite(x)]).max() for x in (hk, hv))
     check(host(o), O, A, seen, 0.125 * hq.max() * top_k, dtype, top_v)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("n, sink", [(64, 0), (64, 63), (2, 0), (3000, 0), (3000, 2999), (640, 333)])
+def test_keys_far_below_the_largest_one(dtype, n, sink):
+    # one key has nearly all of the attention and a value of 0: O is what the others have, each of them 10 to 22 below in its score
+    import torch
+    import paper_2511_23113_amd as dbsp
+    H, d, page = 16, 64, 16
+    per = -(-n // page)
+    k, v = (torch.zeros(per, 1, page, d, dtype=torch_types(dtype), device="cuda") for _ in range(2))
+    t = np.random.default_rng(21).permutation(per).astype(np.int32)[None]
+    k[..., 3], v[:] = -1.0, torch.linspace(100, 60000, d, device="cuda")
+    place = int(t[0, sink // page]), 0, sink % page
+    k[place], v[place] = 0.0, 0.0
+    q = torch.zeros(1, H, 1, d, dtype=k.dtype, device="cuda")
+    q[0, :, 0, 3] = 10 + 0.75 * torch.arange(H, device="cuda")
+    cache = dbsp.PagedKVCache(k, v, torch.from_numpy(t).cuda(), torch.tensor([n], dtype=torch.int32, device="cuda"))
+    o, lse = dbsp.paged_attn_fwd(cache, q, softmax_scale=1.0)
+    O, LSE, A, seen = orows.paged_attention(host(q), host(k), host(v), t, [n], [1], True, 1.0)
+    check(host(o), O, A, seen, 21.25, dtype, float(v.max()))
+    # the sum: a lane adds four keys a tile, so n / 64 additions in turn and 2 + 2 + 2 + 8 in trees and merges, u of it each; the largest score is 0 and the
+    # others' errors, 2 u (3 * 21.25 + 2) of less than 0.14, are below 19 u; 4 u for the logarithm, its factor and rounding
+    assert np.abs(host(lse) - LSE).max() <= (n / 64 + 37) * U
