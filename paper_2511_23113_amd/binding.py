@@ -543,12 +543,28 @@ def cache_evict(cache: KVCache, budget: int, sinks: int = 0, keep_from=None, str
         _check(rc)
 
 
+class _Kept:
+    """What keeps tensors of the caller and describes them to the library by their addresses.  A tensor may be given other memory (x.data = y, as a
+    module's half() and to() do with its parameters; resize_()): then its address is another one, as what is described is held until the next call."""
+
+    def _keep(self, *tensors):
+        self._described = tuple((x.data_ptr, x.data_ptr()) for x in tensors)
+        self._held = tuple(x.detach() for x in tensors)
+
+    def _moved(self):
+        for address, was in self._described:
+            if address() != was:
+                return True
+        return False
+
+
 _NORMS = {"rms": 1, "layer": 2}
 
 
-class HeadNorm:
+class HeadNorm(_Kept):
     """The norm of each head of queries and keys (see dbsp.h: dbsp_head_norm): kind "rms" or "layer"; gains and biases are [d] tensors on the
-    GPU, all f32 or all of the rows' type, and a missing one is 1 or 0.  The object keeps the tensors, which the caller goes on writing."""
+    GPU, all f32 or all of the rows' type, and a missing one is 1 or 0.  The object keeps the tensors, which the caller goes on writing, and every call
+    goes by the memory that they have then."""
 
     def __init__(self, q_gain=None, k_gain=None, q_bias=None, k_bias=None, kind: str = "rms", eps: float = 1e-6):
         torch = _torch_module()
@@ -565,12 +581,15 @@ class HeadNorm:
                 raise ValueError("gains and biases differ in type, device or size")
             self.dtype, self.device, self.d = x.dtype, x.device, x.shape[0]
             setattr(desc, name, x.data_ptr())
-        self._wide, self._index = self.dtype is torch.float32, None if self.device is None else self.device.index
+        self._wide, self._index = self.dtype is torch.float32, None if self.device is None else x.get_device()
         desc.gains_f32 = self._wide
         self._desc, self._at = desc, C.byref(desc)
+        self._keep(*self.given.values())
 
     def _of(self, x):
         """What a call on tensors like x passes on."""
+        if self._moved():
+            self.__init__(**self.given, kind=self.kind, eps=self.eps)
         if self.d is not None and (self._index != x.get_device() or self.d != x.shape[-1] or not (self._wide or self.dtype is x.dtype)):
             raise ValueError("gains and biases must be [d], f32 or of the rows' type, on their GPU")
         return self._at
