@@ -427,13 +427,29 @@ class _OnDevice:
         return workspace, workspace.data_ptr(), workspace.numel()
 
 
-class KVCache(_OnDevice):
+class _Kept:
+    """What keeps tensors of the caller and describes them to the library by their addresses.  A tensor may be given other memory (x.data = y, as a
+    module's half() and to() do with its parameters; resize_()): then its address is another one, as what is described is held until the next call."""
+
+    def _keep(self, *tensors):
+        self._described = tuple((x.data_ptr, x.data_ptr()) for x in tensors)
+        self._held = tuple(x.detach() for x in tensors)
+
+    def _moved(self):
+        for address, was in self._described:
+            if address() != was:
+                return True
+        return False
+
+
+class KVCache(_OnDevice, _Kept):
     """A key/value cache of the caller's tensors (see dbsp.h: dbsp_cache), for cache_attn_fwd and cache_evict.
 
     k, v: [B, Hk, capacity, d], bf16 or fp16 on one GPU, d in (64, 128) dense, other strides multiples of 8 elements; the first
     lens[b] (int32 [B] there) slots of sequence b are used.  prefix_k, prefix_v: [Hk, P, d], shared by all sequences.  Either
     pair may be missing.  weights: f32 [B, Hk, capacity], positions: int32 [B, Hk, capacity], both contiguous.  The object keeps the
-    tensors, which the caller goes on writing; it copies nothing, and other tensors make another object."""
+    tensors, which the caller goes on writing, and every call goes by the memory that they have then (what they had before is held until that call);
+    it copies nothing, and other tensors make another object."""
 
     def __init__(self, k=None, v=None, lens=None, prefix_k=None, prefix_v=None, weights=None, positions=None):
         torch = _torch_module()
@@ -472,7 +488,13 @@ class KVCache(_OnDevice):
             setattr(desc, name, x.data_ptr())
         self.k, self.v, self.lens, self.prefix_k, self.prefix_v, self.weights, self.positions = k, v, lens, prefix_k, prefix_v, weights, positions
         self.B, self.Hk, self.d, self.capacity, self.n_prefix = desc.B if k is not None else None, desc.Hk, d, desc.capacity, desc.n_prefix
-        self._desc, self._at, self._bytes, self._index = desc, C.byref(desc), {}, self.device.index
+        self._desc, self._at, self._bytes, self._index = desc, C.byref(desc), {}, some.get_device()
+        self._keep(*(x for x in (k, v, lens, prefix_k, prefix_v, weights, positions) if x is not None))
+
+    def _now(self):
+        """Describes the tensors anew where one of them has been given other memory."""
+        if self._moved():
+            self.__init__(self.k, self.v, self.lens, self.prefix_k, self.prefix_v, self.weights, self.positions)
 
     def _for(self, B):
         """The same prefix for B sequences."""
@@ -491,6 +513,7 @@ def cache_attn_fwd(cache: KVCache, q, q_lens=None, causal: bool = True, decay=No
     weights hold, to which this call's attention is added.  Enqueues on `stream` (default: torch's current stream) and
     returns (o, lse)."""
     torch = _torch
+    cache._now()
     shape, q_s = q.shape, q.stride()
     if len(shape) != 4 or q.dtype != cache.dtype or q.device != cache.device or shape[3] != cache.d or q_s[3] != 1:
         raise ValueError("q must be [B, H, Nq, d] of the cache's type and head dim on its GPU, with a dense last dimension")
@@ -534,6 +557,7 @@ def cache_evict(cache: KVCache, budget: int, sinks: int = 0, keep_from=None, str
     if cache.k is None:
         raise ValueError("the cache has no keys of its own")
     torch = _torch
+    cache._now()
     raw, elsewhere = cache._on(stream)
     if keep_from is not None and (keep_from.shape != (cache.B,) or keep_from.dtype != torch.int32 or keep_from.device != cache.device or not keep_from.is_contiguous()):
         raise ValueError("keep_from must be a contiguous int32 tensor of [B] on the cache's GPU")
@@ -541,21 +565,6 @@ def cache_evict(cache: KVCache, budget: int, sinks: int = 0, keep_from=None, str
     rc = _lib.dbsp_cache_evict(cache._at, budget, sinks, None if keep_from is None else keep_from.data_ptr(), at, size, raw)
     if rc:
         _check(rc)
-
-
-class _Kept:
-    """What keeps tensors of the caller and describes them to the library by their addresses.  A tensor may be given other memory (x.data = y, as a
-    module's half() and to() do with its parameters; resize_()): then its address is another one, as what is described is held until the next call."""
-
-    def _keep(self, *tensors):
-        self._described = tuple((x.data_ptr, x.data_ptr()) for x in tensors)
-        self._held = tuple(x.detach() for x in tensors)
-
-    def _moved(self):
-        for address, was in self._described:
-            if address() != was:
-                return True
-        return False
 
 
 _NORMS = {"rms": 1, "layer": 2}
@@ -740,13 +749,13 @@ def _grads_workspace(_, *sizes):
     return _lib.dbsp_qk_norm_rope_bwd_workspace(*sizes)
 
 
-class PagedKVCache(_OnDevice):
+class PagedKVCache(_OnDevice, _Kept):
     """A key/value cache in pages of the caller's tensors (see dbsp.h: dbsp_paged_cache), for paged_append and paged_attn_fwd.
 
     k, v: the pool, [n_pages, Hk, page_size, d], bf16 or fp16 on one GPU, d in (64, 128) dense, other strides multiples of 8 elements (a pool of
     [n_pages, page_size, Hk, d] goes in as its transpose(1, 2)).  pages: int32 [B, max_pages], the pages of each sequence's slots, an entry that
-    is no page where a sequence has none.  lens: int32 [B], used slots.  The object keeps the tensors, which the caller goes on writing;
-    other tensors make another object."""
+    is no page where a sequence has none.  lens: int32 [B], used slots.  The object keeps the tensors, which the caller goes on writing, and
+    every call goes by the memory that they have then (what they had before is held until that call); other tensors make another object."""
 
     def __init__(self, k, v, pages, lens):
         torch = _torch_module()
@@ -761,13 +770,19 @@ class PagedKVCache(_OnDevice):
         if lens.shape != pages.shape[:1] or lens.dtype != torch.int32 or lens.device != k.device or not lens.is_contiguous():
             raise ValueError("lens must be a contiguous int32 tensor of [B] on the cache's GPU")
         self.k, self.v, self.pages, self.lens = k, v, pages, lens
-        self.dtype, self.device, self._index = k.dtype, k.device, k.device.index
+        self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
         self.B, self.max_pages = pages.shape
         self.n_pages, self.Hk, self.page_size, self.d = k.shape
         desc = PagedCacheDesc(dtype=k.dtype == torch.float16, B=self.B, Hk=self.Hk, d=self.d, n_pages=self.n_pages, page_size=self.page_size,
                               max_pages=self.max_pages, k=k.data_ptr(), v=v.data_ptr(), pages=pages.data_ptr(), pages_stride=pages.stride(0), lens=lens.data_ptr())
         desc.k_stride[:], desc.v_stride[:] = k.stride()[:3], v.stride()[:3]
         self._desc, self._at, self._bytes = desc, C.byref(desc), {}
+        self._keep(k, v, pages, lens)
+
+    def _now(self):
+        """Describes the tensors anew where one of them has been given other memory."""
+        if self._moved():
+            self.__init__(self.k, self.v, self.pages, self.lens)
 
 
 def paged_append(cache: PagedKVCache, k, v, new_lens=None, q=None, q_out=None, norm: HeadNorm = None, rotary: Rotary = None, positions=None, stream=None):
@@ -775,6 +790,7 @@ def paged_append(cache: PagedKVCache, k, v, new_lens=None, q=None, q_out=None, n
     with norm and rotation on the way, and beside them the tokens' queries q [B, H, Nn, d] into q_out (see dbsp.h: dbsp_paged_append).  new_lens:
     int32 [B] on the GPU, if not all Nn tokens are there; the others' rows of q_out are left as they were, so pass it then.  positions:
     int32 [Nn, axes] or [B, Nn, axes], None with one axis: the tokens' slots.  Enqueues on `stream` and returns q_out (None without q)."""
+    cache._now()
     B, Hk, d, dtype, index = cache.B, cache.Hk, cache.d, cache.dtype, cache._index
     if k.dim() != 4:
         raise ValueError("k must be [B, Hk, Nn, d]")
@@ -810,6 +826,7 @@ def paged_attn_fwd(cache: PagedKVCache, q, q_lens=None, causal: bool = True, o=N
     """Attention of each sequence's newest tokens, q [B, H, Nq, d], over its pages (see dbsp.h: dbsp_paged_attn_fwd; the new tokens' keys are written
     before).  q_lens: int32 [B] on the GPU, if not all Nq tokens are there; the others' rows of o and lse are left as they were, so pass o
     and lse then.  Enqueues on `stream` (default: torch's current stream) and returns (o, lse)."""
+    cache._now()
     shape, q_s, dtype, index = q.shape, q.stride(), cache.dtype, cache._index
     if len(shape) != 4 or q.dtype is not dtype or q.get_device() != index or shape[0] != cache.B or shape[3] != cache.d or q_s[3] != 1:
         raise ValueError("q must be [B, H, Nq, d] of the cache's sequences, type and head dim on its GPU, with a dense last dimension")

@@ -117,3 +117,66 @@ def test_memory_that_a_description_names_is_kept(lib):
     assert at not in [y.data_ptr() for y in taken]
     B.qk_norm_rope_fwd(*rows(), norm=norm)
     assert norm_given(lib).q_gain == gain.data_ptr() != at
+
+
+def paged():
+    x = {"k": torch.zeros(9, 1, 16, 64, dtype=torch.bfloat16), "v": torch.zeros(9, 1, 16, 64, dtype=torch.bfloat16), "pages": torch.zeros(1, 4, dtype=torch.int32),
+         "lens": torch.zeros(1, dtype=torch.int32)}
+    return {n: on_gpu(y) for n, y in x.items()}
+
+
+def contiguous():
+    x = {"k": torch.zeros(1, 1, 40, 64, dtype=torch.bfloat16), "v": torch.zeros(1, 1, 40, 64, dtype=torch.bfloat16), "lens": torch.zeros(1, dtype=torch.int32),
+         "prefix_k": torch.zeros(1, 9, 64, dtype=torch.bfloat16), "prefix_v": torch.zeros(1, 9, 64, dtype=torch.bfloat16), "weights": torch.zeros(1, 1, 40),
+         "positions": torch.zeros(1, 1, 40, dtype=torch.int32)}
+    return {n: on_gpu(y) for n, y in x.items()}
+
+
+def calls_of(cache):
+    q, k = rows()
+    if isinstance(cache, B.PagedKVCache):
+        return [lambda: B.paged_append(cache, k, k), lambda: B.paged_attn_fwd(cache, q[:, :, :1])]
+    return [lambda: B.cache_attn_fwd(cache, q[:, :, :1], decay=1.0), lambda: B.cache_evict(cache, 20)]
+
+
+@pytest.mark.parametrize("make, of, which", [(paged, B.PagedKVCache, n) for n in paged()] + [(contiguous, B.KVCache, n) for n in contiguous()])
+def test_a_caches_tensors_that_move(lib, make, of, which):
+    given = make()
+    cache = of(**given)
+    for call in calls_of(cache):
+        given[which].data = given[which].data.clone()
+        call()
+        desc = lib.calls[-1][1][0]._obj
+        for name, x in given.items():
+            assert getattr(desc, name) == x.data_ptr()
+
+
+def test_a_cache_of_other_sizes(lib):
+    # the pool grows, its pages are wider, and the table gets longer
+    given = paged()
+    cache = B.PagedKVCache(**given)
+    attend = calls_of(cache)[1]
+    attend()
+    given["k"].data, given["v"].data = (torch.zeros(30, 24, 1, 64, dtype=torch.bfloat16).transpose(1, 2) for _ in range(2))
+    given["pages"].data = torch.zeros(1, 7, dtype=torch.int32)
+    attend()
+    desc = lib.calls[-1][1][0]._obj
+    assert (desc.n_pages, desc.page_size, desc.max_pages, desc.pages_stride, cache.page_size) == (30, 24, 7, 7, 24) and list(desc.k_stride) == [24 * 64, 64, 64]
+    given["lens"].data = torch.zeros(2, dtype=torch.int32)
+    for _ in range(2):
+        with pytest.raises(ValueError, match="lens"):
+            attend()
+    given["lens"].data = torch.zeros(1, dtype=torch.int32)
+    given["v"].data = given["v"].data.half()
+    with pytest.raises(ValueError, match="v must"):
+        attend()
+
+
+def test_a_prefix_that_moves_serves_other_batches(lib):
+    given = {n: x for n, x in contiguous().items() if n.startswith("prefix")}
+    cache = B.KVCache(**given)
+    for b in (1, 3):
+        given["prefix_v"].data = given["prefix_v"].data.clone()
+        B.cache_attn_fwd(cache, torch.zeros(b, 2, 1, 64, dtype=torch.bfloat16))
+        desc = lib.calls[-1][1][0]._obj
+        assert desc.B == b and desc.prefix_v == given["prefix_v"].data_ptr()

@@ -36,3 +36,24 @@ def test_gains_of_a_module():
     with torch.no_grad():                  # and in place, as an optimizer's step
         gains["q_gain"].mul_(0.5)
     same()
+
+
+def test_caches_whose_tensors_move():
+    import torch
+    import paper_2511_23113_amd as dbsp
+    torch.manual_seed(1)
+    rand = lambda *s: torch.randn(*s, device="cuda").bfloat16()      # noqa: E731
+    of_pages = [rand(12, 2, 16, 64), rand(12, 2, 16, 64), torch.randperm(12, device="cuda").int().view(2, 6), torch.tensor([90, 33], dtype=torch.int32, device="cuda")]
+    of_slots = [rand(2, 2, 96, 64), rand(2, 2, 96, 64), torch.tensor([90, 33], dtype=torch.int32, device="cuda")]
+    paged, slots, q, k, v = dbsp.PagedKVCache(*of_pages), dbsp.KVCache(*of_slots), rand(2, 4, 1, 64), rand(2, 2, 1, 64), rand(2, 2, 1, 64)
+    for x in of_pages + of_slots:
+        was = x.detach()
+        x.data = x.data.clone()
+        was.fill_(-1 if was.dtype == torch.int32 else float("nan"))
+        others = [y.clone() for y in of_pages]
+        dbsp.paged_append(paged, k, v)
+        dbsp.paged_append(dbsp.PagedKVCache(*others), k, v)
+        assert all(torch.equal(y, z) for y, z in zip(of_pages, others))
+        for got, want in ((dbsp.paged_attn_fwd(paged, q), dbsp.paged_attn_fwd(dbsp.PagedKVCache(*others), q)),
+                          (dbsp.cache_attn_fwd(slots, q), dbsp.cache_attn_fwd(dbsp.KVCache(*(y.clone() for y in of_slots)), q))):
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool(torch.isfinite(got[1]).all())
