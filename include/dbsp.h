@@ -346,7 +346,7 @@ typedef struct dbsp_qk_rows {
  *
  * q_out, k_out: written, no two elements of one in one place.  They overlap no input, but may be q and k themselves with the same strides.
  * norm, rotary: host, may be NULL (none).  All structs are read during the call only.
- * An infinite value or a NaN spoils its own row only.  With a norm, bf16 values of 2^60 or more in magnitude overflow its sums.
+ * An infinite value or a NaN spoils its own row with a norm, its own pair without, and a place from 2R on nothing but itself.  With a norm, bf16 values of 2^60 or more in magnitude overflow its sums.
  * stream: a hipStream_t (NULL = default stream).  The call only enqueues one kernel, under capture too.
  * Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large), DBSP_EHIP.
  */

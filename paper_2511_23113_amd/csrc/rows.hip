@@ -147,14 +147,25 @@ __device__ __forceinline__ float normalise(Pairs& x, float eps) {
   return r;
 }
 
-struct Turn { f32x4 c, s; };
+// Pairs that are not turned are `still`: their cosine is 1 and their sine 0, but 0 times an infinite neighbour would not be nothing.
+struct Turn {
+  f32x4 c, s;
+  bool still[4];
+};
 template <bool BACK>
-__device__ __forceinline__ void rotate(Pairs& x, const Turn& t) {
+__device__ __forceinline__ void rotate(Pairs& x, const Turn& t, bool all_turned) {
+  const Pairs was = x;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float a = x.a[i], b = x.b[i], s = BACK ? -t.s[i] : t.s[i];
     x.a[i] = __builtin_fmaf(a, t.c[i], -(b * s));
     x.b[i] = __builtin_fmaf(b, t.c[i], a * s);
+  }
+  if (all_turned) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x.a[i] = t.still[i] ? was.a[i] : x.a[i];
+    x.b[i] = t.still[i] ? was.b[i] : x.b[i];
   }
 }
 
@@ -186,6 +197,7 @@ __device__ __forceinline__ Turn turn_of(const dbsp_rows_params& p, int c, int b,
   for (int i = 0; i < 4; ++i) {
     const int pair = 4 * c + i, axis = (pair >= p.ends[0]) + (pair >= p.ends[1]) + (pair >= p.ends[2]);
     turns[i] = p.turns[pair];              // (0 from p.turned on)
+    t.still[i] = pair >= p.turned;
     at[i] = place;
     if (p.positions) at[i] = here[pair < p.turned ? axis : 0];
   }
@@ -240,16 +252,19 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8))
   // Gain, bias and rotation in one: y1 = n1 (g1 cos) - n2 (g2 sin) + (b1 cos - b2 sin) and so on, of the normed values n
   Turn t;
   Pairs cosines, sines, bias;
+  const bool all_turned = 2 * p.turned == D;
   if (!part.plain) {
     t = turn_of(p, c, b, n, place);
-    cosines = {t.c, t.c};
-    sines = {t.s, t.s};
     if constexpr (KIND != 0) {
       const Pairs gain = weights_of<T, HALVES>(part.gain, p.gains_f32, 1.f, lane);
       bias = weights_of<T, HALVES>(part.bias, p.gains_f32, 0.f, lane);
-      rotate<false>(bias, t);
+      rotate<false>(bias, t, all_turned);
       cosines = {gain.a * t.c, gain.b * t.c};
-      sines = {gain.a * t.s, gain.b * t.s};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sines.a[e] = t.still[e] ? 0.f : gain.a[e] * t.s[e];
+        sines.b[e] = t.still[e] ? 0.f : gain.b[e] * t.s[e];
+      }
     }
   }
   for (int h = at.h0; h < at.h1; h += U) {
@@ -266,12 +281,16 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8))
       u32x4 out = in[u];
       if (!part.plain) {
         Pairs x = unpack<T, HALVES>(in[u]);
-        if constexpr (KIND != 0) normalise<D, KIND>(x, p.eps);
+        if constexpr (KIND != 0) {
+          normalise<D, KIND>(x, p.eps);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float n1 = x.a[e], n2 = x.b[e];
-          x.a[e] = __builtin_fmaf(n1, cosines.a[e], KIND != 0 ? __builtin_fmaf(-n2, sines.b[e], bias.a[e]) : -(n2 * sines.b[e]));
-          x.b[e] = __builtin_fmaf(n2, cosines.b[e], KIND != 0 ? __builtin_fmaf(n1, sines.a[e], bias.b[e]) : n1 * sines.a[e]);
+          for (int e = 0; e < 4; ++e) {
+            const float n1 = x.a[e], n2 = x.b[e];
+            x.a[e] = __builtin_fmaf(n1, cosines.a[e], __builtin_fmaf(-n2, sines.b[e], bias.a[e]));
+            x.b[e] = __builtin_fmaf(n2, cosines.b[e], __builtin_fmaf(n1, sines.a[e], bias.b[e]));
+          }
+        } else {
+          rotate<false>(x, t, all_turned);
         }
         out = pack<T, HALVES>(x);
       }
@@ -291,6 +310,7 @@ __global__ __launch_bounds__(kRowThreads) void dbsp_rows_grad_kernel(const dbsp_
   const dbsp_rows_part& part = p.part[at.part];
   const unsigned all = (unsigned)p.B * p.N;
   const Place lane = place_of<HALVES>(c, p.turned);
+  const bool all_turned = 2 * p.turned == D;
   Pairs gain, d_gain = {}, d_bias = {};
   if constexpr (KIND != 0) gain = weights_of<T, HALVES>(part.gain, p.gains_f32, 1.f, lane);
   for (int tile = walker; tile < p.tiles; tile += p.walkers) {
@@ -322,7 +342,7 @@ __global__ __launch_bounds__(kRowThreads) void dbsp_rows_grad_kernel(const dbsp_
       for (int u = 0; u < U; ++u) {
         if (h + u >= at.h1) break;
         Pairs dn = unpack<T, HALVES>(dy_now[u]);
-        rotate<true>(dn, t);
+        rotate<true>(dn, t, all_turned);
         if constexpr (KIND != 0) {
           Pairs hat = unpack<T, HALVES>(x_now[u]);
           const float r = normalise<D, KIND>(hat, p.eps);
