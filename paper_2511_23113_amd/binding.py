@@ -799,6 +799,8 @@ def paged_append(cache: PagedKVCache, k, v, new_lens=None, q=None, q_out=None, n
     raw, elsewhere = cache._on(stream)
     H, q_at, o_at = 0, _NO_HEADS, _NO_HEADS
     if q is not None:
+        if q.dim() != 4:
+            raise ValueError("q must be [B, H, Nn, d]")
         H = q.shape[1]
         shape_q = (B, H, Nn, d)
         q_at = _heads("q", q, shape_q, dtype, index)

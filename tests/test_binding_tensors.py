@@ -180,3 +180,13 @@ def test_a_prefix_that_moves_serves_other_batches(lib):
         B.cache_attn_fwd(cache, torch.zeros(b, 2, 1, 64, dtype=torch.bfloat16))
         desc = lib.calls[-1][1][0]._obj
         assert desc.B == b and desc.prefix_v == given["prefix_v"].data_ptr()
+
+
+@pytest.mark.parametrize("dims", range(6))
+def test_appended_rows_of_other_dimensions(lib, dims):
+    cache, k = B.PagedKVCache(**paged()), rows()[1]
+    x = torch.zeros((1, 1, 8, 64, 1, 1)[:dims], dtype=torch.bfloat16)
+    for bad in (dict(q=x), dict(k=x), dict(v=x), dict(q=k, q_out=x), dict(positions=x.int(), rotary=B.Rotary((8, 8)))):
+        if dims != 4 or "positions" in bad:
+            with pytest.raises(ValueError):
+                B.paged_append(cache, **{"k": k, "v": k, **bad})
