@@ -405,7 +405,8 @@ typedef struct dbsp_paged_cache {
  *       of q_out are left as they were; so are the rows of tokens whose slot would lie before slot 0 (new_lens[b] > lens[b]).
  * norm, rotary: as for dbsp_qk_norm_rope_fwd.
  * Tokens whose page is none (see dbsp_paged_cache) are not written; their queries are.  Where two tokens have one place, by a page that two sequences
- * share, either of them is there afterwards.
+ * share or that a table names twice, what is there afterwards is not specified: keys, values and heads, or pieces of them, may be one token's and
+ * the others the other's.  Before two sequences with the same beginning go on in a page that both name, one of them gets a copy of it.
  * stream: as above; enqueues one kernel.  Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large, or not the cache's), DBSP_EHIP.
  */
 int dbsp_paged_append(const dbsp_paged_cache* cache, const dbsp_qk_rows* rows, const dbsp_heads* v, const int32_t* new_lens,
