@@ -302,7 +302,9 @@ int dbsp_cache_evict_workspace(const dbsp_cache* cache, int32_t budget, int64_t*
 
 /*
  * Queries and keys as attention takes them, out of a projection's output: each head's norm and the rotation by its token's position in one
- * pass, from any strides to any strides.  A row is one head of one token, x[0 .. d - 1]:
+ * pass, from any strides to any strides.  Each head is normed by itself: a norm over all heads of a token together (one mean over H d values and a gain
+ * of H d, before a projection's output is split into heads, as some video models have it) is not among these, and its layers come here with their
+ * rows normed already and DBSP_NORM_NONE.  A row is one head of one token, x[0 .. d - 1]:
  *   norm:      n = (x - mu) r gain + bias,  r = 1 / sqrt(mean((x - mu)^2) + eps),  mu = 0 (DBSP_NORM_RMS) or mean(x) (DBSP_NORM_LAYER);
  *              n = x (DBSP_NORM_NONE);
  *   rotation:  pair p (of R = sum of pairs[]; the first pairs[0] belong to axis 0, and so on) has the angle
@@ -346,7 +348,8 @@ typedef struct dbsp_qk_rows {
  *
  * q_out, k_out: written, no two elements of one in one place.  They overlap no input, but may be q and k themselves with the same strides.
  * norm, rotary: host, may be NULL (none).  All structs are read during the call only.
- * An infinite value or a NaN spoils its own row with a norm, its own pair without, and a place from 2R on nothing but itself.  With a norm, bf16 values of 2^60 or more in magnitude overflow its sums.
+ * An infinite value or a NaN spoils its own row where there is a norm, else its own pair, or at a place that does not turn itself only.  With a
+ * norm, bf16 values of 2^60 or more in magnitude overflow its sums.
  * stream: a hipStream_t (NULL = default stream).  The call only enqueues one kernel, under capture too.
  * Errors: DBSP_EINVAL, DBSP_ESHAPE (sizes too large), DBSP_EHIP.
  */

@@ -386,14 +386,14 @@ class _OnDevice:
         """The raw stream, and whether tensors made on torch's current one are used on another."""
         torch = _torch
         if self._index != torch._C._cuda_getDevice():
-            raise ValueError("the cache lives on another device than the current one")
+            raise ValueError("the tensors live on another device than the current one")
         now = torch._C._cuda_getCurrentRawStream(self._index)
         if stream is None:
             return now, False
         if isinstance(stream, int):
             return stream, stream != now
         if getattr(stream, "device", self.device) != self.device:
-            raise ValueError("the stream is of another device than the cache")
+            raise ValueError("the stream is of another device than the tensors")
         raw = stream.cuda_stream
         return raw, raw != now
 
@@ -571,8 +571,8 @@ _NORMS = {"rms": 1, "layer": 2}
 
 
 class HeadNorm(_Kept):
-    """The norm of each head of queries and keys (see dbsp.h: dbsp_head_norm): kind "rms" or "layer"; gains and biases are [d] tensors on the
-    GPU, all f32 or all of the rows' type, and a missing one is 1 or 0.  The object keeps the tensors, which the caller goes on writing, and every call
+    """The norm of each head of queries and keys by itself (see dbsp.h: dbsp_head_norm; not that of all heads of a token together, with a gain of
+    [H d], which some models have): kind "rms" or "layer"; gains and biases are [d] tensors on the GPU, all f32 or all of the rows' type, and a missing one is 1 or 0.  The object keeps the tensors, which the caller goes on writing, and every call
     goes by the memory that they have then."""
 
     def __init__(self, q_gain=None, k_gain=None, q_bias=None, k_bias=None, kind: str = "rms", eps: float = 1e-6):
@@ -672,7 +672,7 @@ def _positions(positions, rotary, B, N, index):
 def qk_norm_rope_fwd(q, k=None, norm: HeadNorm = None, rotary: Rotary = None, positions=None, q_out=None, k_out=None, stream=None):
     """Queries [B, H, N, d] and keys [B, Hk, N, d] of a projection (any strides: views into its output) with each head's norm and the rotation
     by positions (int32 [N, axes] or [B, N, axes]; None with one axis: 0 .. N - 1), as contiguous tensors or in q_out and k_out
-    (see dbsp.h: dbsp_qk_norm_rope_fwd).  Enqueues on `stream` (default: torch's current stream) and returns (q_out, k_out)."""
+    (see dbsp.h: dbsp_qk_norm_rope_fwd).  Autograd does not see the call: gradients are qk_norm_rope_bwd's.  Enqueues on `stream` (default: torch's current stream) and returns (q_out, k_out)."""
     here = _on_rows(q)
     raw, elsewhere = here._on(stream)
     shape, dtype, index = q.shape, q.dtype, here._index
