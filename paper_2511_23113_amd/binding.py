@@ -435,11 +435,12 @@ class _Kept:
         self._described = tuple((x.data_ptr, x.data_ptr()) for x in tensors)
         self._held = tuple(x.detach() for x in tensors)
 
-    def _moved(self):
+    def _now(self):
+        """Describes the tensors anew, and checks them again, where one of them has been given other memory."""
         for address, was in self._described:
             if address() != was:
-                return True
-        return False
+                self._again()
+                break
 
 
 class KVCache(_OnDevice, _Kept):
@@ -491,10 +492,8 @@ class KVCache(_OnDevice, _Kept):
         self._desc, self._at, self._bytes, self._index = desc, C.byref(desc), {}, some.get_device()
         self._keep(*(x for x in (k, v, lens, prefix_k, prefix_v, weights, positions) if x is not None))
 
-    def _now(self):
-        """Describes the tensors anew where one of them has been given other memory."""
-        if self._moved():
-            self.__init__(self.k, self.v, self.lens, self.prefix_k, self.prefix_v, self.weights, self.positions)
+    def _again(self):
+        self.__init__(self.k, self.v, self.lens, self.prefix_k, self.prefix_v, self.weights, self.positions)
 
     def _for(self, B):
         """The same prefix for B sequences."""
@@ -595,10 +594,12 @@ class HeadNorm(_Kept):
         self._desc, self._at = desc, C.byref(desc)
         self._keep(*self.given.values())
 
+    def _again(self):
+        self.__init__(**self.given, kind=self.kind, eps=self.eps)
+
     def _of(self, x):
         """What a call on tensors like x passes on."""
-        if self._moved():
-            self.__init__(**self.given, kind=self.kind, eps=self.eps)
+        self._now()
         if self.d is not None and (self._index != x.get_device() or self.d != x.shape[-1] or not (self._wide or self.dtype is x.dtype)):
             raise ValueError("gains and biases must be [d], f32 or of the rows' type, on their GPU")
         return self._at
@@ -779,10 +780,8 @@ class PagedKVCache(_OnDevice, _Kept):
         self._desc, self._at, self._bytes = desc, C.byref(desc), {}
         self._keep(k, v, pages, lens)
 
-    def _now(self):
-        """Describes the tensors anew where one of them has been given other memory."""
-        if self._moved():
-            self.__init__(self.k, self.v, self.pages, self.lens)
+    def _again(self):
+        self.__init__(self.k, self.v, self.pages, self.lens)
 
 
 def paged_append(cache: PagedKVCache, k, v, new_lens=None, q=None, q_out=None, norm: HeadNorm = None, rotary: Rotary = None, positions=None, stream=None):
