@@ -20,9 +20,9 @@
 // For it each probability is the sum of two numbers of the inputs' type (see Halves), beside one another along the keys against V twice: an MFMA over
 // 32 products takes as long as one over 16.  LSE's sums, which O is divided by, are of the f32 values.
 //
-// Bound by reading K and V once: 32 sequences of 40 heads on 8 KV heads, 880 to 4400 keys each (347 MB on average) 65 us and 4.7 for the merge; two
-// sequences of some 111,000 keys and 4 KV heads (456 MB) 79 us, 5.8 TB/s, and 4.8.  Where there are few tiles a workgroup, by latencies: lengths,
-// pages, first tile, some 4 us before anything is computed (24 sequences of 10 KV heads and 21 rows over 39 to 750 keys, 50 MB: 15.5 us and 4).
+// Bound by reading K and V once: 32 sequences of 40 heads on 8 KV heads, 880 to 4400 keys each (347 MB on average) 65 us and 4.8 for the merge; two
+// sequences of some 111,000 keys and 4 KV heads (456 MB) 79 us, 5.8 TB/s, and 5.0.  Where there are few tiles a workgroup, by latencies: lengths,
+// pages, first tile, some 4 us before anything is computed (24 sequences of 10 KV heads and 21 rows over 39 to 750 keys, 50 MB: 15.9 us and 4).
 #include <hip/hip_runtime.h>
 
 #include "cache_attn.hpp"
