@@ -587,6 +587,8 @@ class HeadNorm(_Kept):
                 raise ValueError(f"{name} must be a contiguous [d] tensor of f32, bf16 or fp16 on the GPU")
             if self.dtype is not None and (x.dtype != self.dtype or x.device != self.device or x.shape[0] != self.d):
                 raise ValueError("gains and biases differ in type, device or size")
+            if not x.data_ptr():
+                raise ValueError(f"{name} has no memory")
             self.dtype, self.device, self.d = x.dtype, x.device, x.shape[0]
             setattr(desc, name, x.data_ptr())
         self._wide, self._index = self.dtype is torch.float32, None if self.device is None else x.get_device()

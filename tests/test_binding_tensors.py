@@ -190,3 +190,16 @@ def test_appended_rows_of_other_dimensions(lib, dims):
         if dims != 4 or "positions" in bad:
             with pytest.raises(ValueError):
                 B.paged_append(cache, **{"k": k, "v": k, **bad})
+
+
+def test_a_gain_whose_memory_is_gone(lib):
+    # (its address is NULL then, which would pass for a gain that is not given)
+    gain = on_gpu(torch.ones(64))
+    norm = B.HeadNorm(gain)
+    gain.untyped_storage().resize_(0)
+    for call in (lambda: B.qk_norm_rope_fwd(*rows(), norm=norm), lambda: B.HeadNorm(gain)):
+        with pytest.raises(ValueError, match="memory"):
+            call()
+    gain.untyped_storage().resize_(256)
+    B.qk_norm_rope_fwd(*rows(), norm=norm)
+    assert norm_given(lib).q_gain == gain.data_ptr() != 0
